@@ -29,7 +29,8 @@
  *    On an error nothing has been enqueued, except LAPSUM_ERR_HIP, which can
  *    follow earlier launches of the same call.
  *  - Scores must be finite; NaN or infinite scores give unspecified outputs
- *    (they are not scanned for), except in lapsum_hard_mask.
+ *    (they are not scanned for), except in lapsum_hard_mask and in the hard
+ *    selections of a language model.
  *  - workspace: caller-owned scratch of at least the size the matching
  *    *_workspace_size function returns, aligned to 256 bytes.  Its content
  *    on entry does not matter.  Two calls that overlap in time (different
@@ -398,6 +399,202 @@ int lapsum_backward_band(const float* grad_p, const float* p, const void* band,
                          double alpha, float* grad_r, double* grad_k,
                          double* grad_alpha, void* workspace,
                          size_t workspace_bytes, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Hard selections of a language model: which experts a token goes to, which
+ * continuations a beam search keeps, which entries of a key-value cache stay.
+ *
+ * Shared by the entry points below:
+ *  - Larger values come first, equal ones (both zeros are equal) by the lowest
+ *    index.  NaN is never taken before a number.  NaN and infinities are
+ *    allowed everywhere; what they do is said at each call.
+ *  - Elements are float32, bfloat16 or float16 (lapsum_dtype) and count in
+ *    float32; what a selection compares is held in float32.
+ *  - Strides are in elements unless said to be in bytes; the last dimension
+ *    of an array is dense, and arrays need no alignment beyond their elements'.
+ *  - tokens, batch and lengths of 0 are allowed where a call says so.
+ * ------------------------------------------------------------------------ */
+typedef enum lapsum_dtype {
+    LAPSUM_F32 = 0,
+    LAPSUM_BF16 = 1,
+    LAPSUM_F16 = 2
+} lapsum_dtype;
+
+/* ------------------------------------------------------------------------
+ * Routing of tokens to experts.  With x a token's logits, s = softmax(x) or
+ * s_e = 1 / (1 + e^-x_e), and c = s + bias what the selection compares
+ * (softmax without a bias compares x, which has the same order):
+ *   1. the experts are `groups` groups of consecutive ones; a group's score is
+ *      the sum of its group_top (1 or 2) largest c (softmax without a bias:
+ *      x itself for 1, e^(x - max x) for 2), and the topk_groups best groups stay;
+ *   2. the top_k experts of the largest c in them are chosen;
+ *   3. w_j = scale s_j, or with renormalise scale s_j / sum of the chosen s
+ *      (0 where that sum is 0).
+ * An expert whose logit or c is -inf or NaN is never chosen, and such a
+ * logit has no share in a softmax; a logit of +inf counts as the largest float.  A place
+ * that no expert is left for gets index -1 and weight 0, so a token with
+ * every logit masked gets only such places.
+ *
+ *   logits       [tokens] rows of `experts` elements, row_stride apart;
+ *                tokens >= 0, 1 <= experts <= 2048, row_stride >= experts
+ *   score        0 softmax, 1 sigmoid
+ *   bias         [experts] float32, or NULL
+ *   groups       divides experts, at most 64; 1 <= topk_groups <= groups;
+ *                group_top at most experts / groups
+ *   top_k        1 .. 64, at most topk_groups * (experts / groups)
+ *   scale        finite
+ *   weights      [tokens, top_k] float32, in the order of the choice
+ *   indices      [tokens, top_k] int32
+ *   counts       NULL, or [experts] int32: tokens per expert
+ *   workspace    lapsum_route_forward_workspace_size bytes (0 without counts)
+ *
+ * Backward: the gradient of the weights with respect to the logits, the
+ * indices held fixed (the bias has none):
+ *   sigmoid               dx_j = scale g_j s_j (1 - s_j)
+ *   sigmoid, renormalise  dx_j = scale s_j (1 - s_j) (g_j - sum g_i s_i / S) / S,
+ *                         S the sum of the chosen s
+ *   softmax               dx_e = scale s_e ([e chosen] g_e - sum_j g_j s_j)
+ *   softmax, renormalise  dx_j = scale q_j (g_j - sum g_i q_i), q the softmax
+ *                         over the chosen
+ * and 0 for every other expert.
+ *   grad_weights  [tokens, top_k] float32
+ *   logits, indices, score, renormalise, scale   as in the forward; an index
+ *                 outside [0, experts) is a place without an expert
+ *   grad_logits   [tokens, experts] dense, the logits' type, all of it written
+ * ------------------------------------------------------------------------ */
+size_t lapsum_route_forward_workspace_size(int64_t tokens, int64_t experts,
+                                           int64_t top_k, int64_t groups,
+                                           int with_counts);
+
+int lapsum_route_forward(const void* logits, int dtype, int64_t tokens,
+                         int64_t experts, int64_t row_stride, int score,
+                         const float* bias, int64_t groups, int64_t topk_groups,
+                         int64_t group_top, int64_t top_k, int renormalise,
+                         double scale, float* weights, int32_t* indices,
+                         int32_t* counts, void* workspace,
+                         size_t workspace_bytes, hipStream_t stream);
+
+int lapsum_route_backward(const float* grad_weights, const void* logits,
+                          int dtype, int64_t tokens, int64_t experts,
+                          int64_t row_stride, const int32_t* indices, int score,
+                          int64_t top_k, int renormalise, double scale,
+                          void* grad_logits, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Beam search: the num best continuations of each request over its beams and
+ * the vocabulary.  With x the logits of beam w and cum_w its score so far,
+ *   lse_w = log sum_v e^x_wv,   s(w, v) = cum_w + (x_wv - lse_w),
+ * each step rounded to float32; equal s by the lowest w * vocab + v.  A
+ * continuation whose s is NaN or -inf is none: a logit of -inf is masked, a
+ * beam with cum -inf or NaN, or with a logit of NaN or +inf, offers nothing.
+ * Where fewer than num are left the rest gets score -inf, token -1 and parent -1.
+ *
+ *   logits     [batch * beams] rows of `vocab` elements, row_stride apart
+ *   beam_scores  [batch, beams] float32, cum
+ *   num        1 .. 32; beams 1 .. 32; batch >= 0, batch * beams <= 65535;
+ *              beams * vocab <= 2^31 - 1
+ *   scores, tokens, parents   [batch, num] float32, int32, int32
+ *   workspace  lapsum_beam_select_workspace_size bytes
+ *
+ * lapsum_beam_reorder moves states to the beams they go on in:
+ * state[b, i] <- state[b, parents[b, i]] for `count` states of batch * beams
+ * rows each.  Of a row, the `outer` pieces of live_bytes, outer_stride bytes
+ * apart, are moved (keys of one layer as [heads, room, dim]: outer = heads,
+ * live_bytes = length * dim * size, outer_stride = room * dim * size).  in == out
+ * reorders in place; else the two must not overlap.  A parent outside
+ * [0, beams) leaves the row what it is (copies it).
+ *   states         host array, read before the call returns
+ *   parents        int32, rows parent_stride apart (>= beams)
+ * ------------------------------------------------------------------------ */
+size_t lapsum_beam_select_workspace_size(int64_t batch, int64_t beams,
+                                         int64_t vocab, int64_t num);
+
+int lapsum_beam_select(const void* logits, int dtype, int64_t batch,
+                       int64_t beams, int64_t vocab, int64_t row_stride,
+                       const float* beam_scores, int64_t num, float* scores,
+                       int32_t* tokens, int32_t* parents, void* workspace,
+                       size_t workspace_bytes, hipStream_t stream);
+
+typedef struct lapsum_beam_state {
+    const void* in;
+    void* out;
+    int64_t row_bytes;      /* from one beam's row to the next */
+    int64_t outer;          /* pieces of a row, >= 0 */
+    int64_t outer_stride;   /* bytes from one piece to the next */
+    int64_t live_bytes;     /* of a piece, >= 0 */
+} lapsum_beam_state;
+
+int lapsum_beam_reorder(const lapsum_beam_state* states, int64_t count,
+                        const int32_t* parents, int64_t parent_stride,
+                        int64_t batch, int64_t beams, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * A key-value cache of bounded size by accumulated attention weight.
+ *
+ * lapsum_cache_accumulate: acc[b, h, s] = (acc_in[b, h, s], or 0) + the sum of
+ * the weights w[b, h G + g, q, s] over the G = heads / kv_heads query heads that share
+ * h and all queries q, for s < seen[b]; formed in float64 and rounded once.
+ * Columns from seen[b] on are not read: they keep acc_in, or get 0.
+ *   weights   [batch, heads, queries] rows of `keys` elements by three strides
+ *   seen      [batch] int32, or NULL (all of the columns)
+ *   acc_in    [batch, kv_heads, keys] float32, or NULL; may be acc
+ *   acc       [batch, kv_heads, keys] float32
+ * batch, queries and keys may be 0.
+ *
+ * lapsum_cache_evict: of each (sequence, head) the `budget` entries that stay,
+ * copied in the order of their slots.  A sequence has seen positions 0 ..
+ * seen[b] - 1; the first `sink` and the last `recent` of them always stay, the
+ * others by the largest acc.  With pos NULL slot s holds position s, and slots
+ * from seen[b] on are empty; else a slot is empty where its pos is negative.  NaN in
+ * acc goes first.  Where fewer than budget entries are there the rest of the
+ * new cache gets zeros, and position -1.
+ *   k, v          rows of row_bytes by (batch, head, slot) strides in BYTES,
+ *                 host arrays of three
+ *   acc, pos      [batch, kv_heads, slots] float32, int32
+ *   k_out, v_out  [batch, kv_heads, budget] dense rows; they overlap no input
+ *   acc_out, pos_out   [batch, kv_heads, budget]
+ *   budget >= 1, sink >= 0, recent >= 0, sink + recent <= budget
+ *   workspace     lapsum_cache_evict_workspace_size bytes
+ *
+ * lapsum_cache_step: one generated token.  acc += the token's attention
+ * weights over the cache, summed over the heads that share one as above (slots with a
+ * negative pos are not read into); then the new key and value take the first
+ * empty slot, or else that of the smallest acc (NaN first) among the positions
+ * outside the first `sink` and the last `recent` (the new one counts; should
+ * every entry be inside, the first slot), with acc 0 and position seen[b].
+ *   weights       [batch, heads] rows of `slots` elements by two strides
+ *   k_new, v_new  [batch, kv_heads] dense rows of row_bytes
+ *   k, v, acc, pos   the cache, changed in place
+ *   slot          [batch, kv_heads] int32 output
+ *   seen          [batch] int32, the new token's position
+ *   sink >= 0, recent >= 1, sink + recent <= slots
+ * ------------------------------------------------------------------------ */
+int lapsum_cache_accumulate(const void* weights, int dtype, int64_t batch,
+                            int64_t heads, int64_t kv_heads, int64_t queries,
+                            int64_t keys, int64_t stride_batch,
+                            int64_t stride_head, int64_t stride_query,
+                            const int32_t* seen, const float* acc_in,
+                            float* acc, hipStream_t stream);
+
+size_t lapsum_cache_evict_workspace_size(int64_t batch, int64_t kv_heads,
+                                         int64_t slots, int64_t budget);
+
+int lapsum_cache_evict(const void* k, const int64_t* k_strides, const void* v,
+                       const int64_t* v_strides, int64_t row_bytes,
+                       const float* acc, const int32_t* pos,
+                       const int32_t* seen, int64_t batch, int64_t kv_heads,
+                       int64_t slots, int64_t budget, int64_t sink,
+                       int64_t recent, void* k_out, void* v_out, float* acc_out,
+                       int32_t* pos_out, void* workspace,
+                       size_t workspace_bytes, hipStream_t stream);
+
+int lapsum_cache_step(const void* weights, int dtype, int64_t stride_batch,
+                      int64_t stride_head, const void* k_new, const void* v_new,
+                      const int32_t* seen, void* k, const int64_t* k_strides,
+                      void* v, const int64_t* v_strides, int64_t row_bytes,
+                      float* acc, int32_t* pos, int64_t batch, int64_t heads,
+                      int64_t kv_heads, int64_t slots, int64_t sink,
+                      int64_t recent, int32_t* slot, hipStream_t stream);
 
 /* ------------------------------------------------------------------------
  * Diagnostics: per-kernel timing with HIP events.  Off by default.  While

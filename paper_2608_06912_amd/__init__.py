@@ -10,6 +10,9 @@ not built, or the tensors are not on a gfx950 device, the calls raise.
     grad_r = lapsum_backward(grad_p, p, b, alpha)           # Eq. (5) VJP
     p, b, info, m_idx = lapsum_forward_bracketed(scores, k, alpha, noise)
 
+The hard selections of a language model (routing to experts, beam search, a
+bounded key-value cache) are in selection.py and exported here too.
+
 `scores` is a float32 CUDA tensor of shape [n] or [batch, n]; k and alpha
 are Python floats with 0 < k < n and alpha < 0.
 """
@@ -600,3 +603,9 @@ def lapsum_profile_stop() -> dict:
                "lapsum_profile_entry")
         out[buf.value.decode()] = (int(launches.value), float(ms.value))
     return out
+
+
+from .selection import *            # noqa: E402,F401,F403  (it uses what stands above)
+from .selection import __all__ as _selection_names   # noqa: E402
+
+__all__ += _selection_names

@@ -28,10 +28,12 @@ import os
 import torch
 
 from . import (HERE, LapsumError, lapsum_backward, lapsum_backward_band, lapsum_bracket_noise,
-               lapsum_forward, lapsum_forward_bracketed, lapsum_hard_mask, load, new_band)
+               lapsum_forward, lapsum_forward_bracketed, lapsum_hard_mask, lapsum_route_backward,
+               lapsum_route_forward, load, new_band)
 
 __all__ = ["soft_topk", "hard_topk_mask", "straight_through", "choose_path", "sample_size",
-           "bracket_noise", "bracket_indices", "LapSumFunction", "FULL_SORT_MAX_N"]
+           "bracket_noise", "bracket_indices", "LapSumFunction", "FULL_SORT_MAX_N", "route_topk",
+           "RouteFunction"]
 
 # A row up to this length takes the full path (which sorts only for a
 # permutation; the names are older); longer rows the sample bracket.
@@ -290,3 +292,39 @@ def soft_topk(scores, k, alpha, *, path: str = "auto", sample: str = "n23", z: f
     K = sample_size(n, sample) if path == "bracketed" else 0
     p = LapSumFunction.apply(scores, k, alpha, path, K, z, noise_seed, False, sampler)
     return straight_through(p, hard_topk_mask(scores.detach(), int(float(k)))) if ste else p
+
+
+class RouteFunction(torch.autograd.Function):
+    """The weights of lapsum_route_forward as an autograd node: the gradient
+    with respect to the logits, the chosen experts held fixed."""
+
+    @staticmethod
+    def forward(ctx, logits, top_k, options, counts):
+        out = lapsum_route_forward(logits.detach(), top_k, counts=counts, **options)
+        ctx.options = {name: options[name] for name in ("score", "renormalise", "scale")}
+        ctx.save_for_backward(logits, out[1])
+        ctx.mark_non_differentiable(*out[1:])
+        return out
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad_weights, *unused):
+        logits, indices = ctx.saved_tensors
+        g = grad_weights
+        if g.dtype != torch.float32:
+            g = g.float()
+        grad = lapsum_route_backward(g.contiguous(), logits.detach(), indices, **ctx.options)
+        return grad, None, None, None
+
+
+def route_topk(logits, top_k: int, *, score: str = "softmax", bias=None, groups: int = 1,
+               topk_groups: int | None = None, group_top: int = 1, renormalise: bool = False,
+               scale: float = 1.0, counts: bool = False):
+    """The top_k experts of each token and their weights, differentiable in the
+    logits (soft_topk trains the choice itself, this its weights).  Arguments
+    and results as lapsum_route_forward: (weights, indices[, counts])."""
+    options = {"score": score, "bias": bias, "groups": groups, "topk_groups": topk_groups,
+               "group_top": group_top, "renormalise": renormalise, "scale": scale}
+    if torch.is_grad_enabled() and isinstance(logits, torch.Tensor) and logits.requires_grad:
+        return RouteFunction.apply(logits, top_k, options, counts)
+    return lapsum_route_forward(logits, top_k, counts=counts, **options)

@@ -389,4 +389,113 @@ hipError_t launch_bucket_solve(const PartSource& ps, int64_t m_cap, BucketAcc ac
 hipError_t launch_write_m_idx(const int32_t* sorted_idx, int64_t m_len, int64_t m_capacity,
                               int32_t* out, hipStream_t s);
 
+// ------------------------------------------------------- hard selections ---
+// Routing.  logits: rows of `experts` elements, `stride` apart.
+constexpr int kRouteMaxExperts = 2048;
+constexpr int kRouteMaxTop = 64;
+constexpr int kRouteMaxGroups = 64;
+constexpr int64_t kRouteBlocks = 2048;   // most workgroups of a call
+struct RouteArgs {
+  const void* logits;
+  int64_t tokens, stride;
+  int experts, score, renorm, top_k, groups, topk_groups, group_top;
+  float scale;
+  const float* bias;
+  float* weights;
+  int32_t* indices;
+  int* counts;               // [experts], or null
+  int sub, group_size;       // set by the launcher
+};
+struct RouteGradArgs {
+  const void* logits;
+  int64_t tokens, stride;
+  int experts, score, renorm, top_k;
+  float scale;
+  const float* grad;
+  const int32_t* indices;
+  void* grad_logits;         // [tokens, experts], the logits' type
+};
+int64_t route_blocks(int64_t tokens, int experts, int top_k, int groups);
+// parts: [route_blocks][experts], needed for counts where that is above one.
+hipError_t launch_route_forward(RouteArgs a, int dtype, int* parts, hipStream_t s);
+hipError_t launch_route_backward(const RouteGradArgs& a, int dtype, hipStream_t s);
+
+// Beam search.
+constexpr int kBeamMaxNum = 32;
+constexpr int kBeamMaxBeams = 32;
+constexpr int kBeamMaxParts = 64;
+struct BeamArgs {
+  const void* logits;        // [batch beams] rows of vocab, `stride` apart
+  int64_t stride, vocab, batch;
+  int beams, num;
+  const float* cum;          // [batch, beams]
+  float* scores;             // [batch, num]
+  int32_t *tokens, *parents;
+  int steps, parts;          // beam_plan
+  int64_t row_steps;
+  uint64_t* lists;           // [batch beams][parts][num]
+  float* refs;               // [batch beams][parts]
+  double* sums;
+};
+void beam_plan(int64_t rows, int64_t vocab, int* steps, int64_t* row_steps, int* parts);
+hipError_t launch_beam_select(BeamArgs a, int dtype, hipStream_t s);
+
+// States of a reorder launch, sizes in vectors of the launch's width.
+constexpr int kReorderStates = 16;
+struct ReorderState {
+  const void* in;
+  void* out;
+  int64_t row, outer, outer_stride, live;
+  uint32_t block0;           // set by the launcher
+};
+struct ReorderArgs {
+  ReorderState state[kReorderStates];
+  int count, beams;
+  const int32_t* parents;
+  int64_t parent_stride;
+};
+hipError_t launch_beam_reorder(ReorderArgs& a, int64_t batch, int width, hipStream_t s);
+
+// Cache entries by accumulated attention weight.
+struct AccumulateArgs {
+  const void* weights;
+  int64_t stride_b, stride_h, stride_q;
+  int64_t batch, kv, group, queries, keys;
+  const int32_t* seen;
+  const float* acc;          // null: from zero
+  float* out;
+  int64_t tiles;             // set by the launcher
+};
+hipError_t launch_cache_accumulate(AccumulateArgs a, int dtype, hipStream_t s);
+struct EvictArgs {
+  const void *k, *v;
+  int64_t k_b, k_h, k_s, v_b, v_h, v_s, row;   // in vectors
+  const float* acc;
+  const int32_t* pos;        // null: the slots
+  const int32_t* seen;
+  int64_t batch, kv, room, budget;
+  int sink, recent;
+  void *k_out, *v_out;
+  float* acc_out;
+  int32_t* pos_out;
+  int32_t* slots;            // [batch, kv, budget] scratch
+  int team;                  // set by the launcher
+};
+hipError_t launch_cache_evict(EvictArgs a, int width, hipStream_t s);
+struct StepArgs {
+  const void* weights;
+  int64_t stride_b, stride_h;
+  int64_t batch, kv, group, room;
+  const void *k_new, *v_new;
+  const int32_t* seen;
+  void *k, *v;
+  int64_t k_b, k_h, k_s, v_b, v_h, v_s, row;   // in bytes
+  int words;                 // rows, strides and addresses are multiples of 4
+  float* acc;
+  int32_t* pos;
+  int sink, recent;
+  int32_t* slot;
+};
+hipError_t launch_cache_step(const StepArgs& a, int dtype, hipStream_t s);
+
 }  // namespace lapsum
