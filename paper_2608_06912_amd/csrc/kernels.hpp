@@ -404,7 +404,8 @@ struct RouteArgs {
   float* weights;
   int32_t* indices;
   int* counts;               // [experts], or null
-  int sub, group_size;       // set by the launcher
+  int sub, group_size, wide; // set by the launcher
+  uint32_t group_inv;
 };
 struct RouteGradArgs {
   const void* logits;

@@ -21,14 +21,19 @@
 //                       the chosen
 //
 // A team of LT lanes takes a token: 16 lanes (four tokens a wave) for up to
-// 512 experts and 8 chosen, else the wave.  A lane holds every LT-th dword of the row, so
-// the best experts of a group are spread over the team.  The k-th largest of the lanes'
-// maxima bounds the k-th largest c from below; what is not below it, little
-// more than k values, is ranked by counting.  The rare row with more such
-// values than lanes is chosen one maximum at a time.
+// 512 experts and 8 chosen, else the wave.  A lane holds every LT-th dword of
+// the row, so the best experts of a group are spread over the team.  The k-th
+// largest of the lanes' maxima bounds the k-th largest c from below; what is not
+// below it, little more than k values, goes one to a lane and is ranked by
+// counting.  The rare row with more such values than lanes is chosen one
+// maximum at a time.
 //
-// Sigmoid scores are compared in float32, so the selection depends on their
-// rounding: 1/(1 + e^-x) is formed by expf and a correctly rounded division.
+// Sigmoid scores are compared in float32, so the choice depends on their
+// rounding: 1/(1 + e^-x) by expf and a correctly rounded division.  Two exact
+// scores per logit would be most of the work, so all of a row gets an approximate
+// one first (the hardware's 2^x and 1/x, within kNear), which settles what
+// cannot be chosen; the candidates, and rows whose groups are closer than that,
+// get the exact one.
 #include "select_common.hpp"
 
 namespace lapsum {
@@ -36,156 +41,264 @@ namespace lapsum {
 namespace {
 constexpr int BT = 256;
 
+// Elements of a dword: what a lane holds of a row at a time.
+template <int DT>
+constexpr int kPer = DT == 0 ? 1 : 2;
+
 __device__ __forceinline__ float sigmoid_f32(float x) { return 1.0f / (1.0f + expf(-x)); }
 
-// Experts' logits of a lane's items: item i, part v is expert (i LT + l) V + v.
-template <int DT, int V, int IT, int LT>
+// An approximate sigmoid, 1 / (1 + 2^(-x log2 e)) by the hardware's functions, is
+// within kNear of the exact one: the product's, the exponential's, the sum's
+// and the reciprocal's rounding, each weighted by s (1 - s) or s, are below
+// 3e-7.  Comparisons of c leave twice that much, and four roundings of c itself.
+constexpr float kNear = 1e-6f;
+__device__ __forceinline__ float near_margin(float c) { return 2.0f * kNear + 5e-7f * fabsf(c); }
+
+// A logit as it counts: NaN is masked, +inf the largest float.
+__device__ __forceinline__ float clean(float x) { return x > -INFINITY ? fminf(x, FLT_MAX) : -INFINITY; }
+
+// The team's row, a lane every LT-th dword; what lies past the row is of its
+// end, no masked value.
+template <int DT, int IT, int LT>
 __device__ __forceinline__ void load_row(const typename Elem<DT>::raw* __restrict__ row, int E, int l,
-                                         float (&x)[IT][V]) {
+                                         float (&x)[IT][kPer<DT>]) {
+  constexpr int V = kPer<DT>;
+  uint32_t u[IT];
+  if (E == IT * LT * V) {   // (the whole of every lane: one address, fixed offsets)
+    const char* p = reinterpret_cast<const char*>(row) + l * 4;
+#pragma unroll
+    for (int i = 0; i < IT; ++i) __builtin_memcpy(&u[i], p + i * LT * 4, 4);
+  } else {
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {
+      const int e = (i * LT + l) * V;
+      // an odd row's last element is the upper half of the last whole dword
+      const int at = e + V <= E ? e : E - V;
+      if (V == 2 && E == 1) u[i] = row[0];
+      else __builtin_memcpy(&u[i], row + at, 4);
+      if (V == 2 && e + 1 == E && E > 1) u[i] >>= 16;
+    }
+  }
 #pragma unroll
   for (int i = 0; i < IT; ++i) {
-    const int e = (i * LT + l) * V;
-    const int at = e < E ? e : 0;   // (V divides E)
     if constexpr (V == 2) {
-      uint32_t u;
-      __builtin_memcpy(&u, row + at, 4);
-      x[i][0] = Elem<DT>::get(u & 0xffffu);
-      x[i][1] = Elem<DT>::get(u >> 16);
+      x[i][0] = Elem<DT>::get(u[i] & 0xffffu);
+      x[i][1] = Elem<DT>::get(u[i] >> 16);
     } else {
-      x[i][0] = Elem<DT>::get(row[at]);
-    }
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      // NaN counts as -inf (not chosen, no share), +inf as the largest float
-      x[i][v] = x[i][v] == x[i][v] ? fminf(x[i][v], FLT_MAX) : -INFINITY;
-      if (e >= E) x[i][v] = -INFINITY;
+      x[i][0] = Elem<DT>::get(u[i]);
     }
   }
 }
+// f(value, expert) for all of a lane's places, past the row too.
+template <int IT, int LT, int V, class F>
+__device__ __forceinline__ void each_item(float (&x)[IT][V], int l, F&& f) {
+#pragma unroll
+  for (int i = 0; i < IT; ++i)
+#pragma unroll
+    for (int v = 0; v < V; ++v) f(x[i][v], (i * LT + l) * V + v);
+}
 
 // max and sum of e^{x - max} over the team's row; a row without a finite
-// logit has sum 0.
-template <int V, int IT, int LT>
-__device__ __forceinline__ void softmax_stats(const float (&x)[IT][V], float* m_out, float* sum_out) {
-  float m = -INFINITY;
-#pragma unroll
-  for (int i = 0; i < IT; ++i)
-#pragma unroll
-    for (int v = 0; v < V; ++v) m = fmaxf(m, x[i][v]);
-  m = team_max<LT>(m);
-  const float at = m == -INFINITY ? 0.0f : m;
-  float s = 0.0f;
-#pragma unroll
-  for (int i = 0; i < IT; ++i)
-#pragma unroll
-    for (int v = 0; v < V; ++v) s += expf(x[i][v] - at);
-  *m_out = at;
-  *sum_out = team_sum<LT>(s);
+// logit has max 0 and sum 0.  NaN and +inf, which make the sum NaN, are
+// cleaned from x first where there are any.
+template <int IT, int LT, int V>
+__device__ __forceinline__ void softmax_stats(float (&x)[IT][V], int l, float* m_out, float* sum_out) {
+  for (;;) {
+    float m = -INFINITY;
+    each_item<IT, LT>(x, l, [&](float& y, int) { m = fmaxf(m, y); });
+    m = team_max<LT>(m);
+    m = m == -INFINITY ? 0.0f : m;
+    float s = 0.0f;
+    each_item<IT, LT>(x, l, [&](float& y, int) { s += expf(y - m); });
+    s = team_sum<LT>(s);
+    if (!__any(s != s)) {
+      *m_out = m;
+      *sum_out = s;
+      return;
+    }
+    each_item<IT, LT>(x, l, [&](float& y, int) { y = clean(y); });
+  }
 }
-}  // namespace
 
 // LDS of a team.
 template <int LT>
 struct RouteTeam {
-  float cand[LT];
   int at[LT];
-  int sel[LT];
-  float gscore[LT];
+  float gscore[64];
 };
 
-template <int DT, int V, int IT, int LT>
-__global__ __launch_bounds__(BT) void route_forward_kernel(RouteArgs a) {
-  constexpr int R = BT / LT;   // tokens a workgroup takes at a time
-  using raw = typename Elem<DT>::raw;
-  __shared__ RouteTeam<LT> teams[R];
-  extern __shared__ float dyn[];   // [R][E] c (groups), then [E] counts
-  const int l = threadIdx.x % LT;
-  const int r = threadIdx.x / LT;
-  const int E = a.experts, k = a.top_k;
-  RouteTeam<LT>& tm = teams[r];
-  float* crow = dyn + static_cast<int64_t>(r) * (E | 1);
-  int* hist = reinterpret_cast<int*>(dyn + (a.groups > 1 ? R * (E | 1) : 0));
-  if (a.counts) {
-    for (int e = threadIdx.x; e < E; e += BT) hist[e] = 0;
-    __syncthreads();
+// Floats from one token's c in LDS to the next (whole 16-byte words).
+template <int DT, int IT, int LT>
+constexpr int kRow = IT * LT * kPer<DT> + 4;
+
+// Whether the group that this lane takes part in (l / sub) stays, on the lane
+// that speaks for it (l = g sub), from the row's values in LDS; *score_out: the
+// group's score.
+template <int LT>
+__device__ __forceinline__ bool group_kept(const RouteArgs& a, const float* crow, float* gscore, int l,
+                                           float* score_out) {
+  const int sub = a.sub, size = a.group_size;
+  const int g = l / sub;
+  float t1 = -INFINITY, t2 = -INFINITY;
+  const auto take = [&](float y) {   // (no NaN comes here)
+    t2 = __builtin_amdgcn_fmed3f(t1, t2, y);
+    t1 = fmaxf(t1, y);
+  };
+  if (g < a.groups) {
+    if (a.wide) {   // whole 16-byte words of a group for each lane
+      const int part = size / sub;
+      const float4* from = reinterpret_cast<const float4*>(crow + g * size + (l % sub) * part);
+      for (int j = 0; j < part / 4; ++j) {
+        const float4 y = from[j];
+        take(y.x);
+        take(y.y);
+        take(y.z);
+        take(y.w);
+      }
+    } else {
+      for (int j = l % sub; j < size; j += sub) take(crow[g * size + j]);
+    }
   }
-  const bool softmax = a.score == 0;
-  const bool raw_order = softmax && !a.bias;
+  for (int d = 1; d < sub; d *= 2) {
+    const float o1 = __shfl_xor(t1, d, LT), o2 = __shfl_xor(t2, d, LT);
+    t2 = fmaxf(fminf(t1, o1), fmaxf(t2, o2));
+    t1 = fmaxf(t1, o1);
+  }
+  // (an expert that cannot be chosen adds nothing)
+  const float score = a.group_top > 1 && t2 > -INFINITY ? t1 + t2 : t1;
+  if (l % sub == 0 && g < a.groups) gscore[g] = score;
+  wave_lds_sync();
+  int before = 0;
+  for (int j = 0; j < a.groups; ++j) {
+    const float o = gscore[j];
+    before += o > score || (o == score && j < g) ? 1 : 0;
+  }
+  wave_lds_sync();
+  *score_out = score;
+  return l % sub == 0 && g < a.groups && before < a.topk_groups;
+}
+// The bit of expert e's group in the ballot of the lanes that speak for the
+// team's groups.
+__device__ __forceinline__ bool group_bit(const RouteArgs& a, uint64_t stay, int e) {
+  const int lane = static_cast<int>((static_cast<uint32_t>(e) * a.group_inv) >> 21) * a.sub;
+  return (stay >> (lane & 63)) & 1ull;
+}
+
+// Waves per SIMD that the registers of a lane's values leave room for.
+constexpr int route_waves(int values) { return values <= 8 ? 6 : (values <= 16 ? 5 : (values <= 32 ? 3 : 2)); }
+}  // namespace
+
+// SIG: sigmoid scores, else softmax.
+template <int DT, int IT, int LT, bool SIG>
+__global__ __launch_bounds__(BT, route_waves(IT * kPer<DT>)) void route_forward_kernel(RouteArgs a) {
+  constexpr int R = BT / LT;   // tokens a workgroup takes at a time
+  constexpr int V = kPer<DT>;
+  using raw = typename Elem<DT>::raw;
+  using mask_t = std::conditional_t<(IT * V > 32), uint64_t, uint32_t>;
+  __shared__ RouteTeam<LT> teams[R];
+  extern __shared__ __align__(16) float dyn[];   // [R][kRow] c, [kRow] bias, [E] counts
+  const int r = threadIdx.x / LT;
+  const int k = a.top_k;
+  RouteTeam<LT>& tm = teams[r];
+  float* crow = dyn + r * kRow<DT, IT, LT>;
+  float* bias = dyn + R * kRow<DT, IT, LT>;
+  int* hist = reinterpret_cast<int*>(bias + kRow<DT, IT, LT>);
+  // (past the row -inf, which masks what is there; NaN forbids as -inf does)
+  for (int e = threadIdx.x; e < IT * LT * V; e += BT)
+    bias[e] = e >= a.experts ? -INFINITY : (a.bias ? fmaxf(a.bias[e], -INFINITY) : 0.0f);
+  if (a.counts)
+    for (int e = threadIdx.x; e < a.experts; e += BT) hist[e] = 0;
+  __syncthreads();
+  const bool raw_order = !SIG && !a.bias;
+  const bool exps = raw_order && a.group_top > 1;   // a group's score is a sum of e^{x - max}
   for (int64_t base = static_cast<int64_t>(blockIdx.x) * R; base < a.tokens;
        base += static_cast<int64_t>(gridDim.x) * R) {
+    // what follows from the lane and E is formed anew for each token: kept over
+    // the loop it would take the registers that the values need
+    int l = threadIdx.x % LT, E = a.experts;
+    asm volatile("" : "+v"(l), "+s"(E));
     const bool on = base + r < a.tokens;
     const int64_t token = on ? base + r : a.tokens - 1;
     const raw* row = static_cast<const raw*>(a.logits) + token * a.stride;
     float c[IT][V];
-    load_row<DT, V, IT, LT>(row, E, l, c);
     float m = 0.0f, sum = 1.0f;
-    if (softmax && (!a.renorm || a.bias || (a.groups > 1 && a.group_top > 1)))
-      softmax_stats<V, IT, LT>(c, &m, &sum);
-    if (!raw_order) {
+    // the exact score of a clean logit, and what the selection compares
+    const auto score_of = [&](float x) -> float {
+      if constexpr (SIG) return sigmoid_f32(x);
+      else return raw_order ? x : expf(x - m) / sum;
+    };
+    const auto value_of = [&](float x, float s, float b) -> float {
+      return x > -INFINITY ? fmaxf(s + b, -INFINITY) : -INFINITY;
+    };
+    load_row<DT, IT, LT>(row, E, l, c);
+    if constexpr (SIG) {
+      float dmax = 0.0f;
+      bool odd = false;
+      each_item<IT, LT>(c, l, [&](float& y, int) {
+        const float d = 1.0f + exp2_fast(y * -static_cast<float>(kLog2e));
+        dmax = fmaxf(dmax, d);
+        y = __builtin_amdgcn_rcpf(d);
+        odd = odd || y != y;
+      });
+      // scores of 0 and NaN may be masked logits: which they are is seen again
+      const bool look = __any(dmax == INFINITY || odd);
+      if (look) {
+        float x[IT][V];
+        load_row<DT, IT, LT>(row, E, l, x);
+#pragma unroll
+        for (int i = 0; i < IT; ++i)
+#pragma unroll
+          for (int v = 0; v < V; ++v) c[i][v] = x[i][v] > -INFINITY ? c[i][v] : -INFINITY;
+      }
 #pragma unroll
       for (int i = 0; i < IT; ++i)
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-          const int e = (i * LT + l) * V + v;
-          const float x = c[i][v];
-          const float s = softmax ? expf(x - m) / sum : sigmoid_f32(x);
-          const float y = a.bias ? s + a.bias[e < E ? e : 0] : s;
-          c[i][v] = x == -INFINITY ? -INFINITY : fmaxf(y, -INFINITY);   // (NaN: -inf)
-        }
+        for (int v = 0; v < V; ++v) c[i][v] += bias[(i * LT + l) * V + v];
+      if (look || a.bias) {   // (-inf + inf)
+#pragma unroll
+        for (int i = 0; i < IT; ++i)
+#pragma unroll
+          for (int v = 0; v < V; ++v) c[i][v] = fmaxf(c[i][v], -INFINITY);
+      }
+    } else {
+      each_item<IT, LT>(c, l, [&](float& y, int e) { y = e < E ? clean(y) : -INFINITY; });
+      if (!a.renorm || a.bias || (a.groups > 1 && exps)) softmax_stats<IT, LT>(c, l, &m, &sum);
+      if (!raw_order) {
+#pragma unroll
+        for (int i = 0; i < IT; ++i)
+#pragma unroll
+          for (int v = 0; v < V; ++v) c[i][v] = value_of(c[i][v], score_of(c[i][v]), bias[(i * LT + l) * V + v]);
+      }
     }
+    bool slow = false;   // of a team of this wave
     if (a.groups > 1) {
-      // the groups' scores: `sub` lanes take a group, a lane every sub-th member
 #pragma unroll
-      for (int i = 0; i < IT; ++i)
+      for (int i = 0; i < IT; ++i) {
+        float y[V];
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-          const int e = (i * LT + l) * V + v;
-          const bool exps = raw_order && a.group_top > 1 && c[i][v] > -INFINITY;
-          if (e < E) crow[e] = exps ? expf(c[i][v] - m) : c[i][v];
-        }
-      wave_lds_sync();
-      const int sub = a.sub, size = a.group_size;
-      const int g = l / sub;
-      float t1 = -INFINITY, t2 = -INFINITY;
-      if (g < a.groups)
-        for (int j = l % sub; j < size; j += sub) {
-          const float y = crow[g * size + j];
-          t2 = fmaxf(t2, fminf(t1, y));
-          t1 = fmaxf(t1, y);
-        }
-      for (int d = 1; d < sub; d *= 2) {
-        const float o1 = __shfl_xor(t1, d, LT), o2 = __shfl_xor(t2, d, LT);
-        t2 = fmaxf(fminf(t1, o1), fmaxf(t2, o2));
-        t1 = fmaxf(t1, o1);
-      }
-      // (an expert that cannot be chosen adds nothing)
-      const float score = a.group_top > 1 && t2 > -INFINITY ? t1 + t2 : t1;
-      if (l % sub == 0 && g < a.groups) tm.gscore[g] = score;
-      wave_lds_sync();
-      int before = 0;
-      for (int j = 0; j < a.groups; ++j) {
-        const float o = tm.gscore[j];
-        before += o > score || (o == score && j < g) ? 1 : 0;
+        for (int v = 0; v < V; ++v)
+          y[v] = !SIG && exps && c[i][v] > -INFINITY ? expf(c[i][v] - m) : c[i][v];
+        __builtin_memcpy(crow + (i * LT + l) * V, y, sizeof(y));
       }
       wave_lds_sync();
-      if (l % sub == 0 && g < a.groups) tm.gscore[g] = before < a.topk_groups ? 1.0f : 0.0f;
-      wave_lds_sync();
-#pragma unroll
-      for (int i = 0; i < IT; ++i)
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-          const int e = (i * LT + l) * V + v;
-          if (e < E && tm.gscore[e / size] == 0.0f) c[i][v] = -INFINITY;
-        }
-      wave_lds_sync();
+      float score;
+      const bool kept = group_kept<LT>(a, crow, tm.gscore, l, &score);
+      const uint64_t all = __ballot(kept);
+      if constexpr (SIG) {
+        // approximate scores settle it where the last group that stays and the
+        // first that does not are clearly apart
+        const bool speaks = l % a.sub == 0 && l / a.sub < a.groups;
+        const float in = team_min<LT>(kept ? score : INFINITY);
+        const float out = team_max<LT>(speaks && !kept ? score : -INFINITY);
+        slow = __any(!(in - out >= 4.0f * near_margin(in)));
+      }
+      const uint64_t stay = LT == 16 ? all >> (threadIdx.x & 48) : all;
+      each_item<IT, LT>(c, l, [&](float& y, int e) { y = group_bit(a, stay, e) ? y : -INFINITY; });
     }
 
     // the candidates: nothing below the k-th largest of the lanes' maxima
     float best = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < IT; ++i)
-#pragma unroll
-      for (int v = 0; v < V; ++v) best = fmaxf(best, c[i][v]);
+    each_item<IT, LT>(c, l, [&](float& y, int) { best = fmaxf(best, y); });
     float bound;
     if constexpr (LT == 16) {
       int above = 0;
@@ -202,98 +315,115 @@ __global__ __launch_bounds__(BT) void route_forward_kernel(RouteArgs a) {
       }
       bound = key_value(K);
     }
+    if (SIG && fabsf(bound) <= FLT_MAX) bound -= near_margin(bound);
     bound = fmaxf(bound, -FLT_MAX);
-    int mine = 0;
+    mask_t mine = 0;   // from the last item, in the highest bit, to the first
 #pragma unroll
-    for (int i = 0; i < IT; ++i)
+    for (int i = IT - 1; i >= 0; --i)
 #pragma unroll
-      for (int v = 0; v < V; ++v) mine += c[i][v] >= bound ? 1 : 0;
-    const int incl = team_incl_add<LT>(mine);
-    const int count = team_max<LT>(incl);
-    tm.sel[l] = -1;
-    if (!__any(count > LT)) {
-      int pos = incl - mine;
-#pragma unroll
-      for (int i = 0; i < IT; ++i)
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-          if (c[i][v] >= bound) {
-            tm.cand[pos] = c[i][v];
-            tm.at[pos] = (i * LT + l) * V + v;
-            ++pos;
-          }
-      wave_lds_sync();
-      const bool is = l < count;
-      const float val = is ? tm.cand[l] : -INFINITY;
-      const int at = is ? tm.at[l] : INT32_MAX;
-      int rank = 0;
-      if constexpr (LT == 16) {
-        each_rotation([&](auto ctl) {
-          const float ov = dpp_move<decltype(ctl)::value>(val, val);
-          const int oa = dpp_move<decltype(ctl)::value>(at, at);
-          rank += ov > val || (ov == val && oa < at) ? 1 : 0;
-        });
-      } else {
-        for (int j = 0; j < count; ++j) {
-          const float ov = readlane_as(val, j);
-          const int oa = readlane_as(at, j);
-          rank += ov > val || (ov == val && oa < at) ? 1 : 0;
+      for (int v = V - 1; v >= 0; --v) mine = mine + mine + (c[i][v] >= bound ? 1 : 0);
+    const int have = IT * V > 32 ? __popcll(mine) : __popc(static_cast<uint32_t>(mine));
+    const int incl = team_incl_add<LT>(have);
+    int count = team_max<LT>(incl);
+    int at = INT32_MAX;
+    slow = slow || __any(count > LT);
+    if (!slow) {
+      int pos = incl - have;
+      while (__any(mine != 0)) {
+        if (mine != 0) {
+          const int q = IT * V > 32 ? __ffsll(static_cast<unsigned long long>(mine)) - 1
+                                    : __ffs(static_cast<uint32_t>(mine)) - 1;
+          mine &= mine - 1;
+          tm.at[pos] = (q / V * LT + l) * V + q % V;
+          ++pos;
         }
       }
-      if (is && rank < k) tm.sel[rank] = at;
+      wave_lds_sync();
+      if (l < count) at = tm.at[l];
     } else {
-      // one maximum at a time
+      // exact values of the whole row in LDS, and one maximum at a time: lane j
+      // gets the j-th
+      wave_lds_sync();
+#pragma unroll 1
+      for (int e = l; e < E; e += LT) {
+        const float x = clean(Elem<DT>::get(row[e]));
+        const float y = value_of(x, score_of(x), bias[e]);
+        crow[e] = exps && y > -INFINITY ? expf(y - m) : y;
+      }
+      wave_lds_sync();
+      uint64_t stay = ~0ull;
+      if (a.groups > 1) {
+        float score;
+        stay = __ballot(group_kept<LT>(a, crow, tm.gscore, l, &score));
+        if constexpr (LT == 16) stay >>= threadIdx.x & 48;
+      }
+#pragma unroll 1
+      for (int e = l; e < E; e += LT) {
+        if (exps) crow[e] = clean(Elem<DT>::get(row[e]));
+        if (a.groups > 1 && !group_bit(a, stay, e)) crow[e] = -INFINITY;
+      }
+      count = 0;
       for (int j = 0; j < k; ++j) {
         float v1 = -INFINITY;
         int a1 = INT32_MAX;
-#pragma unroll
-        for (int i = 0; i < IT; ++i)
-#pragma unroll
-          for (int v = 0; v < V; ++v)
-            if (c[i][v] > v1) {
-              v1 = c[i][v];
-              a1 = (i * LT + l) * V + v;
-            }
+#pragma unroll 1
+        for (int e = l; e < E; e += LT)
+          if (crow[e] > v1) {
+            v1 = crow[e];
+            a1 = e;
+          }
         const float top = team_max<LT>(v1);
-        const int at = team_min<LT>(v1 == top && top > -INFINITY ? a1 : INT32_MAX);
-#pragma unroll
-        for (int i = 0; i < IT; ++i)
-#pragma unroll
-          for (int v = 0; v < V; ++v)
-            if ((i * LT + l) * V + v == at) c[i][v] = -INFINITY;
-        if (l == 0) tm.sel[j] = at == INT32_MAX ? -1 : at;
+        const int got = team_min<LT>(v1 == top && top > -INFINITY ? a1 : INT32_MAX);
+        if (got != INT32_MAX) {
+          if (a1 == got) crow[got] = -INFINITY;   // (its own lane's entry)
+          if (l == j) at = got;
+          ++count;
+        }
       }
     }
-    wave_lds_sync();
 
-    // lane j: the j-th chosen expert and its weight
-    const int at = l < k ? tm.sel[l] : -1;
-    float x = Elem<DT>::get(row[at >= 0 ? at : 0]);
-    x = fminf(x, FLT_MAX);
-    float w = 0.0f;
-    if (!softmax) {
-      w = at >= 0 ? sigmoid_f32(x) : 0.0f;
-    } else if (!a.renorm) {
-      w = at >= 0 ? expf(x - m) / sum : 0.0f;
+    // a candidate to a lane: its exact c, its rank, its weight
+    const bool is = at != INT32_MAX;
+    const float x = clean(Elem<DT>::get(row[is ? at : 0]));
+    const float s = score_of(x);
+    const float val = is ? value_of(x, s, bias[at]) : -INFINITY;
+    const uint64_t key = (static_cast<uint64_t>(asc_key(val)) << 32) | static_cast<uint32_t>(~at);
+    int rank = 0;
+    if constexpr (LT == 16) {
+      each_rotation([&](auto ctl) { rank += dpp_move<decltype(ctl)::value>(key, key) > key ? 1 : 0; });
     } else {
-      const float top = team_max<LT>(at >= 0 ? x : -INFINITY);
-      w = at >= 0 ? expf(x - top) : 0.0f;
+      for (int j = 0; j < count; ++j) rank += readlane_as(key, j) > key ? 1 : 0;
+    }
+    const bool chosen = is && rank < k;
+    float w;
+    if (SIG || !a.renorm) {
+      w = chosen ? (raw_order ? expf(x - m) / sum : s) : 0.0f;
+    } else {
+      const float top = team_max<LT>(chosen ? x : -INFINITY);
+      w = chosen ? expf(x - top) : 0.0f;
     }
     if (a.renorm) {
       const float total = team_sum<LT>(w);
       w = total > 0.0f ? w / total : 0.0f;
     }
-    if (on && l < k) {
-      a.weights[token * k + l] = a.scale * w;
-      a.indices[token * k + l] = at;
-      if (a.counts && at >= 0) atomicAdd(&hist[at], 1);
+    if (on) {
+      const int64_t o = token * k;
+      if (chosen) {
+        a.weights[o + rank] = a.scale * w;
+        a.indices[o + rank] = at;
+        if (a.counts) atomicAdd(&hist[at], 1);
+      }
+      if (l >= count && l < k) {   // places that no expert is left for
+        a.weights[o + l] = 0.0f;
+        a.indices[o + l] = -1;
+      }
     }
-    wave_lds_sync();   // sel has been read
+    wave_lds_sync();   // what the team wrote has been read
   }
   if (a.counts) {
     __syncthreads();
-    for (int e = threadIdx.x; e < E; e += BT)
-      a.counts[static_cast<int64_t>(blockIdx.x) * E + e] = hist[e];
+    for (int e = threadIdx.x; e < a.experts; e += BT)
+      a.counts[static_cast<int64_t>(blockIdx.x) * a.experts + e] = hist[e];
   }
 }
 
@@ -304,8 +434,10 @@ __global__ __launch_bounds__(1024) void route_counts_kernel(const int* __restric
   const int e = blockIdx.x * 32 + threadIdx.x % 32;
   const int part = threadIdx.x / 32;
   int s = 0;
-  if (e < E)
+  if (e < E) {
+#pragma unroll 8
     for (int b = part; b < blocks; b += 32) s += parts[static_cast<int64_t>(b) * E + e];
+  }
   sums[part][threadIdx.x % 32] = s;
   __syncthreads();
   if (part == 0 && e < E) {
@@ -317,15 +449,16 @@ __global__ __launch_bounds__(1024) void route_counts_kernel(const int* __restric
 
 // The gradient of a token's logits, composed in LDS: the chosen experts'
 // entries, zero (or the softmax's common term) elsewhere.
-template <int DT, int V, int IT, int LT>
+template <int DT, int IT, int LT>
 __global__ __launch_bounds__(BT) void route_backward_kernel(RouteGradArgs a) {
   constexpr int R = BT / LT;
+  constexpr int V = kPer<DT>;
   using raw = typename Elem<DT>::raw;
-  extern __shared__ float dyn[];   // [R][E] entries of the chosen
+  extern __shared__ __align__(16) float dyn[];   // [R][kRow] entries of the chosen
   const int l = threadIdx.x % LT;
   const int r = threadIdx.x / LT;
   const int E = a.experts, k = a.top_k;
-  float* grow = dyn + static_cast<int64_t>(r) * (E | 1);
+  float* grow = dyn + r * kRow<DT, IT, LT>;
   const bool softmax = a.score == 0;
   const bool dense = softmax && !a.renorm;
   for (int64_t base = static_cast<int64_t>(blockIdx.x) * R; base < a.tokens;
@@ -333,17 +466,19 @@ __global__ __launch_bounds__(BT) void route_backward_kernel(RouteGradArgs a) {
     const bool on = base + r < a.tokens;
     const int64_t token = on ? base + r : a.tokens - 1;
     const raw* row = static_cast<const raw*>(a.logits) + token * a.stride;
-    for (int e = l; e < E; e += LT) grow[e] = 0.0f;
-    wave_lds_sync();
+    float p[IT][V], m = 0.0f, sum = 1.0f, common = 0.0f, entry;
+    if (dense) load_row<DT, IT, LT>(row, E, l, p);
     int at = l < k ? a.indices[token * k + l] : -1;
     if (at < 0 || at >= E) at = -1;
     const float g = at >= 0 ? a.grad[token * k + l] * a.scale : 0.0f;
-    float x = Elem<DT>::get(row[at >= 0 ? at : 0]);
-    x = x == x ? fminf(x, FLT_MAX) : -INFINITY;
-    float p[IT][V], m = 0.0f, sum = 1.0f, common = 0.0f, entry;
+    const float x = clean(Elem<DT>::get(row[at >= 0 ? at : 0]));
+    const float none[V] = {};
+#pragma unroll
+    for (int i = 0; i < IT; ++i) __builtin_memcpy(grow + (i * LT + l) * V, none, sizeof(none));
+    wave_lds_sync();
     if (dense) {
-      load_row<DT, V, IT, LT>(row, E, l, p);
-      softmax_stats<V, IT, LT>(p, &m, &sum);
+      each_item<IT, LT>(p, l, [&](float& y, int e) { y = e < E ? y : -INFINITY; });
+      softmax_stats<IT, LT>(p, l, &m, &sum);
       const float q = at >= 0 && sum > 0.0f ? expf(x - m) / sum : 0.0f;
       common = team_sum<LT>(g * q);
       entry = g;
@@ -369,22 +504,22 @@ __global__ __launch_bounds__(BT) void route_backward_kernel(RouteGradArgs a) {
     if (at >= 0) grow[at] = entry;
     wave_lds_sync();
     raw* out = static_cast<raw*>(a.grad_logits) + token * E;
+    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
       const int e = (i * LT + l) * V;
-      if (!on || e >= E) continue;
       float y[V];
+      __builtin_memcpy(y, grow + e, sizeof(y));
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        y[v] = grow[e + v];
-        if (dense) y[v] = sum > 0.0f ? expf(p[i][v] - m) / sum * (y[v] - common) : 0.0f;
-      }
+      for (int v = 0; v < V; ++v)
+        if (dense) y[v] = sum > 0.0f ? expf(p[i][v] - m) * inv * (y[v] - common) : 0.0f;
       if constexpr (V == 2) {
         const uint32_t u = static_cast<uint32_t>(Elem<DT>::put(y[0])) |
                            (static_cast<uint32_t>(Elem<DT>::put(y[1])) << 16);
-        __builtin_memcpy(out + e, &u, 4);
+        if (on && e + 1 < E) __builtin_memcpy(out + e, &u, 4);
+        else if (on && e < E) out[e] = static_cast<raw>(u);
       } else {
-        out[e] = Elem<DT>::put(y[0]);
+        if (on && e < E) out[e] = Elem<DT>::put(y[0]);
       }
     }
     wave_lds_sync();   // the row has been read
@@ -393,88 +528,86 @@ __global__ __launch_bounds__(BT) void route_backward_kernel(RouteGradArgs a) {
 
 // ------------------------------------------------------------- launchers ---
 namespace {
-// 16 lanes hold a token of up to 512 experts (32 items each); a team has to
+// 16 lanes hold a token of up to 512 experts (32 values each); a team has to
 // have a lane per chosen expert and per group, and to leave most rows fewer
 // candidates than lanes.
 bool narrow_team(int experts, int top_k, int groups) {
   return experts <= 512 && top_k <= 8 && groups <= 16;
 }
 
-template <int DT, int V, int LT, class F>
-bool by_items(int experts, F&& f) {
-  const int items = (experts / V + LT - 1) / LT;
-  if (items <= 2) f(std::integral_constant<int, 2>{});
-  else if (items <= 4) f(std::integral_constant<int, 4>{});
-  else if (items <= 8) f(std::integral_constant<int, 8>{});
-  else if (items <= 16) f(std::integral_constant<int, 16>{});
-  else if (items <= 32) f(std::integral_constant<int, 32>{});
-  else return false;
-  return true;
+// f(items, lanes of a team) for this many experts.
+template <int DT, class F>
+bool by_team(int experts, bool narrow, F&& f) {
+  const int dwords = (experts + kPer<DT> - 1) / kPer<DT>;
+  const int items = (dwords + (narrow ? 15 : 63)) / (narrow ? 16 : 64);
+  const auto pick = [&](auto lt) {
+    if (items <= 1) f(std::integral_constant<int, 1>{}, lt);
+    else if (items <= 2) f(std::integral_constant<int, 2>{}, lt);
+    else if (items <= 4) f(std::integral_constant<int, 4>{}, lt);
+    else if (items <= 8) f(std::integral_constant<int, 8>{}, lt);
+    else if (items <= 16) f(std::integral_constant<int, 16>{}, lt);
+    else if constexpr (DT == 0) {
+      if (items > 32) return false;
+      f(std::integral_constant<int, 32>{}, lt);
+    } else {
+      return false;
+    }
+    return true;
+  };
+  return narrow ? pick(std::integral_constant<int, 16>{}) : pick(std::integral_constant<int, 64>{});
 }
 
-int64_t route_grid(int64_t tokens, int team) {
-  const int64_t per = BT / team;
+int64_t route_grid(int64_t tokens, bool narrow) {
+  const int64_t per = BT / (narrow ? 16 : 64);
   const int64_t want = (tokens + per - 1) / per;
   return want < kRouteBlocks ? want : kRouteBlocks;
 }
 
-template <int DT, int V, int LT>
-bool forward_team(const RouteArgs& a, int64_t grid, hipStream_t s) {
-  const int rows = BT / LT;
-  const size_t lds = 4 * (static_cast<size_t>(a.groups > 1 ? rows * (a.experts | 1) : 0) +
-                          static_cast<size_t>(a.counts ? a.experts : 0));
-  return by_items<DT, V, LT>(a.experts, [&](auto it) {
-    constexpr int IT = decltype(it)::value;
-    hipLaunchKernelGGL((route_forward_kernel<DT, V, IT, LT>), dim3(static_cast<unsigned>(grid)),
-                       dim3(BT), static_cast<unsigned>(lds), s, a);
+template <int DT>
+bool forward_type(const RouteArgs& a, bool narrow, int64_t grid, hipStream_t s) {
+  return by_team<DT>(a.experts, narrow, [&](auto it, auto lt) {
+    constexpr int IT = decltype(it)::value, LT = decltype(lt)::value;
+    const unsigned lds = 4u * static_cast<unsigned>((BT / LT + 1) * kRow<DT, IT, LT> + (a.counts ? a.experts : 0));
+    if (a.score)
+      hipLaunchKernelGGL((route_forward_kernel<DT, IT, LT, true>), dim3(static_cast<unsigned>(grid)),
+                         dim3(BT), lds, s, a);
+    else
+      hipLaunchKernelGGL((route_forward_kernel<DT, IT, LT, false>), dim3(static_cast<unsigned>(grid)),
+                         dim3(BT), lds, s, a);
   });
 }
-template <int DT, int V, int LT>
-bool backward_team(const RouteGradArgs& a, int64_t grid, hipStream_t s) {
-  const size_t lds = 4 * static_cast<size_t>(BT / LT) * (a.experts | 1);
-  return by_items<DT, V, LT>(a.experts, [&](auto it) {
-    constexpr int IT = decltype(it)::value;
-    hipLaunchKernelGGL((route_backward_kernel<DT, V, IT, LT>), dim3(static_cast<unsigned>(grid)),
-                       dim3(BT), static_cast<unsigned>(lds), s, a);
+template <int DT>
+bool backward_type(const RouteGradArgs& a, bool narrow, int64_t grid, hipStream_t s) {
+  return by_team<DT>(a.experts, narrow, [&](auto it, auto lt) {
+    constexpr int IT = decltype(it)::value, LT = decltype(lt)::value;
+    const unsigned lds = 4u * static_cast<unsigned>(BT / LT * kRow<DT, IT, LT>);
+    hipLaunchKernelGGL((route_backward_kernel<DT, IT, LT>), dim3(static_cast<unsigned>(grid)),
+                       dim3(BT), lds, s, a);
   });
 }
-
-template <int DT>
-bool forward_type(const RouteArgs& a, bool narrow, bool pairs, int64_t grid, hipStream_t s) {
-  if constexpr (DT != 0)
-    if (pairs) return narrow ? forward_team<DT, 2, 16>(a, grid, s) : forward_team<DT, 2, 64>(a, grid, s);
-  return narrow ? forward_team<DT, 1, 16>(a, grid, s) : forward_team<DT, 1, 64>(a, grid, s);
-}
-template <int DT>
-bool backward_type(const RouteGradArgs& a, bool narrow, bool pairs, int64_t grid, hipStream_t s) {
-  if constexpr (DT != 0)
-    if (pairs) return narrow ? backward_team<DT, 2, 16>(a, grid, s) : backward_team<DT, 2, 64>(a, grid, s);
-  return narrow ? backward_team<DT, 1, 16>(a, grid, s) : backward_team<DT, 1, 64>(a, grid, s);
-}
-
 }  // namespace
 
 int64_t route_blocks(int64_t tokens, int experts, int top_k, int groups) {
-  return route_grid(tokens, narrow_team(experts, top_k, groups) ? 16 : 64);
+  return route_grid(tokens, narrow_team(experts, top_k, groups));
 }
 
 hipError_t launch_route_forward(RouteArgs a, int dtype, int* parts, hipStream_t s) {
   const bool narrow = narrow_team(a.experts, a.top_k, a.groups);
-  const int team = narrow ? 16 : 64;
-  const int64_t grid = route_grid(a.tokens, team);
+  const int64_t grid = route_grid(a.tokens, narrow);
   int* const counts = a.counts;
   if (counts && grid > 1) a.counts = parts;
   a.sub = 1;
-  while (a.sub * 2 * a.groups <= team) a.sub *= 2;
+  while (a.sub * 2 * a.groups <= (narrow ? 16 : 64)) a.sub *= 2;
   a.group_size = a.experts / a.groups;
-  // 16-bit logits of an even number of experts are read as pairs (dwords, at
-  // any alignment: a token's result does not depend on where its row lies)
-  const bool pairs = a.experts % 2 == 0;
+  a.wide = a.experts % 4 == 0 && a.group_size % (4 * a.sub) == 0;
+  // e / size by a product: exact where e (size - 1) < 2^21, that is for the
+  // experts of two groups or more and the places past them
+  a.group_inv = static_cast<uint32_t>(((1u << 21) + a.group_size - 1) / a.group_size);
   bool done;
   { ProfScope ps_("route_forward", s);
-  done = dtype == 0 ? forward_type<0>(a, narrow, pairs, grid, s)
-       : dtype == 1 ? forward_type<1>(a, narrow, pairs, grid, s)
-                    : forward_type<2>(a, narrow, pairs, grid, s); }
+  done = dtype == 0 ? forward_type<0>(a, narrow, grid, s)
+       : dtype == 1 ? forward_type<1>(a, narrow, grid, s)
+                    : forward_type<2>(a, narrow, grid, s); }
   if (!done) return hipErrorInvalidValue;
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !counts || grid <= 1) return e;
@@ -486,13 +619,12 @@ hipError_t launch_route_forward(RouteArgs a, int dtype, int* parts, hipStream_t 
 
 hipError_t launch_route_backward(const RouteGradArgs& a, int dtype, hipStream_t s) {
   const bool narrow = narrow_team(a.experts, a.top_k, 1);
-  const int64_t grid = route_grid(a.tokens, narrow ? 16 : 64);
-  const bool pairs = a.experts % 2 == 0;
+  const int64_t grid = route_grid(a.tokens, narrow);
   bool done;
   { ProfScope ps_("route_backward", s);
-  done = dtype == 0 ? backward_type<0>(a, narrow, pairs, grid, s)
-       : dtype == 1 ? backward_type<1>(a, narrow, pairs, grid, s)
-                    : backward_type<2>(a, narrow, pairs, grid, s); }
+  done = dtype == 0 ? backward_type<0>(a, narrow, grid, s)
+       : dtype == 1 ? backward_type<1>(a, narrow, grid, s)
+                    : backward_type<2>(a, narrow, grid, s); }
   if (!done) return hipErrorInvalidValue;
   return hipGetLastError();
 }
