@@ -394,7 +394,7 @@ hipError_t launch_write_m_idx(const int32_t* sorted_idx, int64_t m_len, int64_t 
 constexpr int kRouteMaxExperts = 2048;
 constexpr int kRouteMaxTop = 64;
 constexpr int kRouteMaxGroups = 64;
-constexpr int64_t kRouteBlocks = 2048;   // most workgroups of a call
+constexpr int64_t kRouteBlocks = 1536;   // most workgroups of a call: six per compute unit
 struct RouteArgs {
   const void* logits;
   int64_t tokens, stride;
@@ -404,7 +404,7 @@ struct RouteArgs {
   float* weights;
   int32_t* indices;
   int* counts;               // [experts], or null
-  int sub, group_size, wide; // set by the launcher
+  int sub, lanes, group_size, wide, packed;   // set by the launcher
   uint32_t group_inv;
 };
 struct RouteGradArgs {

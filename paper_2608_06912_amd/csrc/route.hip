@@ -25,8 +25,8 @@
 // the row, so the best experts of a group are spread over the team.  The k-th
 // largest of the lanes' maxima bounds the k-th largest c from below; what is not
 // below it, little more than k values, goes one to a lane and is ranked by
-// counting.  The rare row with more such values than lanes is chosen one
-// maximum at a time.
+// counting.  A row with more such values than lanes gets a higher bound, and
+// where equal values do not allow one it is chosen one maximum at a time.
 //
 // Sigmoid scores are compared in float32, so the choice depends on their
 // rounding: 1/(1 + e^-x) by expf and a correctly rounded division.  Two exact
@@ -131,14 +131,14 @@ struct RouteTeam {
 template <int DT, int IT, int LT>
 constexpr int kRow = IT * LT * kPer<DT> + 4;
 
-// Whether the group that this lane takes part in (l / sub) stays, on the lane
-// that speaks for it (l = g sub), from the row's values in LDS; *score_out: the
+// Whether the group that this lane takes part in (2^sub lanes to a group) stays, on
+// the lane that speaks for it, the first of them, from the row's values in LDS; *score_out: the
 // group's score.
 template <int LT>
 __device__ __forceinline__ bool group_kept(const RouteArgs& a, const float* crow, float* gscore, int l,
                                            float* score_out) {
-  const int sub = a.sub, size = a.group_size;
-  const int g = l / sub;
+  const int sub = 1 << a.sub, size = a.group_size;
+  const int g = l >> a.sub, q = l & (sub - 1);
   float t1 = -INFINITY, t2 = -INFINITY;
   const auto take = [&](float y) {   // (no NaN comes here)
     t2 = __builtin_amdgcn_fmed3f(t1, t2, y);
@@ -146,8 +146,8 @@ __device__ __forceinline__ bool group_kept(const RouteArgs& a, const float* crow
   };
   if (g < a.groups) {
     if (a.wide) {   // whole 16-byte words of a group for each lane
-      const int part = size / sub;
-      const float4* from = reinterpret_cast<const float4*>(crow + g * size + (l % sub) * part);
+      const int part = size >> a.sub;
+      const float4* from = reinterpret_cast<const float4*>(crow + g * size + q * part);
       for (int j = 0; j < part / 4; ++j) {
         const float4 y = from[j];
         take(y.x);
@@ -156,7 +156,7 @@ __device__ __forceinline__ bool group_kept(const RouteArgs& a, const float* crow
         take(y.w);
       }
     } else {
-      for (int j = l % sub; j < size; j += sub) take(crow[g * size + j]);
+      for (int j = q; j < size; j += sub) take(crow[g * size + j]);
     }
   }
   for (int d = 1; d < sub; d *= 2) {
@@ -166,7 +166,7 @@ __device__ __forceinline__ bool group_kept(const RouteArgs& a, const float* crow
   }
   // (an expert that cannot be chosen adds nothing)
   const float score = a.group_top > 1 && t2 > -INFINITY ? t1 + t2 : t1;
-  if (l % sub == 0 && g < a.groups) gscore[g] = score;
+  if (q == 0 && g < a.groups) gscore[g] = score;
   wave_lds_sync();
   int before = 0;
   for (int j = 0; j < a.groups; ++j) {
@@ -175,12 +175,12 @@ __device__ __forceinline__ bool group_kept(const RouteArgs& a, const float* crow
   }
   wave_lds_sync();
   *score_out = score;
-  return l % sub == 0 && g < a.groups && before < a.topk_groups;
+  return q == 0 && g < a.groups && before < a.topk_groups;
 }
 // The bit of expert e's group in the ballot of the lanes that speak for the
 // team's groups.
 __device__ __forceinline__ bool group_bit(const RouteArgs& a, uint64_t stay, int e) {
-  const int lane = static_cast<int>((static_cast<uint32_t>(e) * a.group_inv) >> 21) * a.sub;
+  const int lane = static_cast<int>((static_cast<uint32_t>(e) * a.group_inv) >> 21) << a.sub;
   return (stay >> (lane & 63)) & 1ull;
 }
 
@@ -233,16 +233,13 @@ __global__ __launch_bounds__(BT, route_waves(IT * kPer<DT>)) void route_forward_
     load_row<DT, IT, LT>(row, E, l, c);
     if constexpr (SIG) {
       float dmax = 0.0f;
-      bool odd = false;
       each_item<IT, LT>(c, l, [&](float& y, int) {
         const float d = 1.0f + exp2_fast(y * -static_cast<float>(kLog2e));
         dmax = fmaxf(dmax, d);
         y = __builtin_amdgcn_rcpf(d);
-        odd = odd || y != y;
       });
-      // scores of 0 and NaN may be masked logits: which they are is seen again
-      const bool look = __any(dmax == INFINITY || odd);
-      if (look) {
+      // a score of 0 may be that of a masked logit: which it is is seen again
+      if (__any(dmax == INFINITY)) {
         float x[IT][V];
         load_row<DT, IT, LT>(row, E, l, x);
 #pragma unroll
@@ -253,13 +250,8 @@ __global__ __launch_bounds__(BT, route_waves(IT * kPer<DT>)) void route_forward_
 #pragma unroll
       for (int i = 0; i < IT; ++i)
 #pragma unroll
-        for (int v = 0; v < V; ++v) c[i][v] += bias[(i * LT + l) * V + v];
-      if (look || a.bias) {   // (-inf + inf)
-#pragma unroll
-        for (int i = 0; i < IT; ++i)
-#pragma unroll
-          for (int v = 0; v < V; ++v) c[i][v] = fmaxf(c[i][v], -INFINITY);
-      }
+        for (int v = 0; v < V; ++v)   // (NaN, of a logit or of -inf + inf: -inf)
+          c[i][v] = fmaxf(c[i][v] + bias[(i * LT + l) * V + v], -INFINITY);
     } else {
       each_item<IT, LT>(c, l, [&](float& y, int e) { y = e < E ? clean(y) : -INFINITY; });
       if (!a.renorm || a.bias || (a.groups > 1 && exps)) softmax_stats<IT, LT>(c, l, &m, &sum);
@@ -271,6 +263,9 @@ __global__ __launch_bounds__(BT, route_waves(IT * kPer<DT>)) void route_forward_
       }
     }
     bool slow = false;   // of a team of this wave
+    // the expert of item q, part v: l's dwords, or `first` on
+    bool packed = false;
+    int first = 0;
     if (a.groups > 1) {
 #pragma unroll
       for (int i = 0; i < IT; ++i) {
@@ -287,13 +282,32 @@ __global__ __launch_bounds__(BT, route_waves(IT * kPer<DT>)) void route_forward_
       if constexpr (SIG) {
         // approximate scores settle it where the last group that stays and the
         // first that does not are clearly apart
-        const bool speaks = l % a.sub == 0 && l / a.sub < a.groups;
+        const bool speaks = (l & ((1 << a.sub) - 1)) == 0 && l >> a.sub < a.groups;
         const float in = team_min<LT>(kept ? score : INFINITY);
         const float out = team_max<LT>(speaks && !kept ? score : -INFINITY);
         slow = __any(!(in - out >= 4.0f * near_margin(in)));
       }
-      const uint64_t stay = LT == 16 ? all >> (threadIdx.x & 48) : all;
-      each_item<IT, LT>(c, l, [&](float& y, int e) { y = group_bit(a, stay, e) ? y : -INFINITY; });
+      const uint64_t stay = LT == 16 ? (all >> (threadIdx.x & 48)) & 0xffffull : all;
+      packed = a.packed != 0;
+      if (packed) {
+        // the groups that stay, over all of the team: 2^lanes lanes to a group,
+        // `part` consecutive experts to a lane
+        const int part = a.group_size >> a.lanes;
+        uint64_t rest = stay;   // the speaking lanes, in the order of their groups
+        for (int j = l >> a.lanes; j > 0; --j) rest &= rest - 1;
+        const int g = rest ? (__ffsll(static_cast<unsigned long long>(rest)) - 1) >> a.sub : 0;
+        first = g * a.group_size + (l & ((1 << a.lanes) - 1)) * part;
+#pragma unroll
+        for (int q = 0; q < IT * V; q += 4) {
+          float4 y = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+          if (q < part) y = *reinterpret_cast<const float4*>(crow + first + q);
+          const float w[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+          for (int v = 0; v < 4 && q + v < IT * V; ++v) c[(q + v) / V][(q + v) % V] = w[v];
+        }
+      } else {
+        each_item<IT, LT>(c, l, [&](float& y, int e) { y = group_bit(a, stay, e) ? y : -INFINITY; });
+      }
     }
 
     // the candidates: nothing below the k-th largest of the lanes' maxima
@@ -315,16 +329,32 @@ __global__ __launch_bounds__(BT, route_waves(IT * kPer<DT>)) void route_forward_
       }
       bound = key_value(K);
     }
-    if (SIG && fabsf(bound) <= FLT_MAX) bound -= near_margin(bound);
-    bound = fmaxf(bound, -FLT_MAX);
-    mask_t mine = 0;   // from the last item, in the highest bit, to the first
+    // where that leaves more candidates than lanes, a higher bound that still
+    // leaves k: halving towards the maximum (equal values may not allow one)
+    mask_t mine;
+    int have, incl, count;
+    float top = 0.0f;
+    for (int turn = 0;; ++turn) {
+      float b = bound;
+      if (SIG && fabsf(b) <= FLT_MAX) b -= near_margin(b);
+      b = fmaxf(b, -FLT_MAX);
+      mine = 0;   // from the last item, in the highest bit, to the first
 #pragma unroll
-    for (int i = IT - 1; i >= 0; --i)
+      for (int i = IT - 1; i >= 0; --i)
 #pragma unroll
-      for (int v = V - 1; v >= 0; --v) mine = mine + mine + (c[i][v] >= bound ? 1 : 0);
-    const int have = IT * V > 32 ? __popcll(mine) : __popc(static_cast<uint32_t>(mine));
-    const int incl = team_incl_add<LT>(have);
-    int count = team_max<LT>(incl);
+        for (int v = V - 1; v >= 0; --v) mine = mine + mine + (c[i][v] >= b ? 1 : 0);
+      have = IT * V > 32 ? __popcll(mine) : __popc(static_cast<uint32_t>(mine));
+      incl = team_incl_add<LT>(have);
+      count = team_max<LT>(incl);
+      if (turn == 8 || !__any(count > LT)) break;
+      if (turn == 0) top = fminf(team_max<LT>(best), FLT_MAX);
+      const float mid = 0.5f * fmaxf(bound, -FLT_MAX) + 0.5f * top;
+      int n = 0;
+      each_item<IT, LT>(c, l, [&](float& y, int) { n += y >= mid ? 1 : 0; });
+      n = team_sum<LT>(n);
+      bound = n >= k ? mid : bound;
+      top = n >= k ? top : mid;
+    }
     int at = INT32_MAX;
     slow = slow || __any(count > LT);
     if (!slow) {
@@ -334,7 +364,7 @@ __global__ __launch_bounds__(BT, route_waves(IT * kPer<DT>)) void route_forward_
           const int q = IT * V > 32 ? __ffsll(static_cast<unsigned long long>(mine)) - 1
                                     : __ffs(static_cast<uint32_t>(mine)) - 1;
           mine &= mine - 1;
-          tm.at[pos] = (q / V * LT + l) * V + q % V;
+          tm.at[pos] = packed ? first + q : (q / V * LT + l) * V + q % V;
           ++pos;
         }
       }
@@ -372,8 +402,8 @@ __global__ __launch_bounds__(BT, route_waves(IT * kPer<DT>)) void route_forward_
             v1 = crow[e];
             a1 = e;
           }
-        const float top = team_max<LT>(v1);
-        const int got = team_min<LT>(v1 == top && top > -INFINITY ? a1 : INT32_MAX);
+        const float most = team_max<LT>(v1);
+        const int got = team_min<LT>(v1 == most && most > -INFINITY ? a1 : INT32_MAX);
         if (got != INT32_MAX) {
           if (a1 == got) crow[got] = -INFINITY;   // (its own lane's entry)
           if (l == j) at = got;
@@ -387,20 +417,30 @@ __global__ __launch_bounds__(BT, route_waves(IT * kPer<DT>)) void route_forward_
     const float x = clean(Elem<DT>::get(row[is ? at : 0]));
     const float s = score_of(x);
     const float val = is ? value_of(x, s, bias[at]) : -INFINITY;
-    const uint64_t key = (static_cast<uint64_t>(asc_key(val)) << 32) | static_cast<uint32_t>(~at);
     int rank = 0;
-    if constexpr (LT == 16) {
-      each_rotation([&](auto ctl) { rank += dpp_move<decltype(ctl)::value>(key, key) > key ? 1 : 0; });
-    } else {
-      for (int j = 0; j < count; ++j) rank += readlane_as(key, j) > key ? 1 : 0;
-    }
+    const auto rank_by = [&](auto key) {
+      rank = 0;
+      if constexpr (LT == 16) {
+        each_rotation([&](auto ctl) { rank += dpp_move<decltype(ctl)::value>(key, key) > key ? 1 : 0; });
+      } else {
+        for (int j = 0; j < count; ++j) rank += readlane_as(key, j) > key ? 1 : 0;
+      }
+    };
+    // by value alone; where two are equal (their ranks are then fewer than the
+    // candidates), by value and index
+    rank_by(val);
+    uint32_t lo = is && rank < 32 ? 1u << rank : 0u, hi = is && rank >= 32 ? 1u << (rank - 32) : 0u;
+    lo = team_reduce<LT>(lo, [](uint32_t p, uint32_t q) { return p | q; });
+    if constexpr (LT == 64) hi = team_reduce<LT>(hi, [](uint32_t p, uint32_t q) { return p | q; });
+    if (__any(__popc(lo) + (LT == 64 ? __popc(hi) : 0) != count))
+      rank_by((static_cast<uint64_t>(asc_key(val)) << 32) | static_cast<uint32_t>(~at));
     const bool chosen = is && rank < k;
     float w;
     if (SIG || !a.renorm) {
       w = chosen ? (raw_order ? expf(x - m) / sum : s) : 0.0f;
     } else {
-      const float top = team_max<LT>(chosen ? x : -INFINITY);
-      w = chosen ? expf(x - top) : 0.0f;
+      const float most = team_max<LT>(chosen ? x : -INFINITY);
+      w = chosen ? expf(x - most) : 0.0f;
     }
     if (a.renorm) {
       const float total = team_sum<LT>(w);
@@ -557,10 +597,12 @@ bool by_team(int experts, bool narrow, F&& f) {
   return narrow ? pick(std::integral_constant<int, 16>{}) : pick(std::integral_constant<int, 64>{});
 }
 
+// Workgroups that fit the device together, each with the same number of turns.
 int64_t route_grid(int64_t tokens, bool narrow) {
   const int64_t per = BT / (narrow ? 16 : 64);
   const int64_t want = (tokens + per - 1) / per;
-  return want < kRouteBlocks ? want : kRouteBlocks;
+  const int64_t turns = (want + kRouteBlocks - 1) / kRouteBlocks;
+  return (want + turns - 1) / turns;
 }
 
 template <int DT>
@@ -596,10 +638,17 @@ hipError_t launch_route_forward(RouteArgs a, int dtype, int* parts, hipStream_t 
   const int64_t grid = route_grid(a.tokens, narrow);
   int* const counts = a.counts;
   if (counts && grid > 1) a.counts = parts;
-  a.sub = 1;
-  while (a.sub * 2 * a.groups <= (narrow ? 16 : 64)) a.sub *= 2;
+  const int team = narrow ? 16 : 64;
+  a.sub = 0;
+  while ((2 << a.sub) * a.groups <= team) ++a.sub;
   a.group_size = a.experts / a.groups;
-  a.wide = a.experts % 4 == 0 && a.group_size % (4 * a.sub) == 0;
+  a.wide = a.experts % 4 == 0 && a.group_size % (4 << a.sub) == 0;
+  // the experts of the chosen groups dealt out to the whole team, where that
+  // comes out even and LDS holds what the selection compares
+  a.lanes = 0;
+  while ((2 << a.lanes) * a.topk_groups <= team) ++a.lanes;
+  a.packed = a.groups > 1 && a.experts % 4 == 0 && (a.topk_groups << a.lanes) == team &&
+             a.group_size % (4 << a.lanes) == 0 && !(a.score == 0 && !a.bias && a.group_top > 1);
   // e / size by a product: exact where e (size - 1) < 2^21, that is for the
   // experts of two groups or more and the places past them
   a.group_inv = static_cast<uint32_t>(((1u << 21) + a.group_size - 1) / a.group_size);
