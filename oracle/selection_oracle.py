@@ -130,10 +130,10 @@ def kept_slots(acc, pos, seen, budget, sink, recent):
     """Slots of one (sequence, head) that stay, ascending."""
     live = pos >= 0
     always = live & ((pos < sink) | (pos >= max(0, seen - recent)))
-    order = sorted(np.nonzero(live)[0],
-                   key=lambda i: (not always[i], 0 if always[i] else np.isnan(acc[i]),
-                                  0 if always[i] or np.isnan(acc[i]) else -acc[i], i))
-    return sorted(int(i) for i in order[:budget])
+    none = np.isnan(acc) & ~always
+    value = np.where(always | none, 0.0, acc)
+    order = np.lexsort((np.arange(acc.size), -value, none, ~always, ~live))
+    return sorted(int(i) for i in order[:min(budget, int(live.sum()))])
 
 
 def step_slot(acc, pos, now, sink, recent):

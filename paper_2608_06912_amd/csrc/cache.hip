@@ -126,124 +126,483 @@ __global__ __launch_bounds__(AT) void cache_accumulate_kernel(AccumulateArgs a) 
 }
 
 // ----------------------------------------------------------------- evict ---
-// One workgroup per (sequence, head): the digits of the budget-th largest key
-// (11, 11 and 10 bits) from histograms in LDS, then the kept slots in order.
-constexpr int ET = 1024;
-constexpr int EW = ET / kWave;
+// The slots that stay, one workgroup per (sequence, head): the budget-th
+// largest key, then the kept slots in order.
+//
+// The key is found digit by digit from histograms in LDS, 2048 bins over the
+// range that still holds it (the keys of positive sums are spread like their
+// logarithms, so few share a bin).  Rows of up to 32768 slots keep their keys in
+// registers.  A longer row is read once: 4096 of its entries give a window that
+// holds the last kept value, one pass marks what is above it and what is in it, as
+// bits in LDS, and only the window's entries (a few percent) are looked at again.  What
+// that does not settle (a window that misses, or too many equal values in it)
+// takes a pass over the row per digit.
 constexpr int kEvictBins = 2048;
+constexpr int kEvictSample = 4096;
+constexpr int kEvictList = 8192;             // entries of the window
+constexpr int kEvictWords = 4096;            // 64 slots each
+constexpr double kEvictSigmas = 4.0;
 
 namespace {
+// What the threads of a workgroup of T exchange; the pairs alternate, so that
+// one round's values may still be read while the next are written.
+template <int T>
 struct EvictSmem {
-  uint32_t bins[kEvictBins];
-  uint32_t wsum[EW];
-  uint32_t digit, above, live;
-  uint32_t wg[EW], we[EW];   // kept for sure, and equal to the last key, per wave
+  uint32_t bins[2][kEvictBins];
+  uint32_t wsum[2][T / kWave];
+  uint32_t bin[2], above[2];
+  uint32_t live, stays, lo, hi;
 };
+
+template <int T>
+struct EvictBlock {
+  EvictSmem<T>& sm;
+  int turn = 0;
+
+  // Once, with a barrier before the first histogram.
+  __device__ __forceinline__ void start() {
+    for (int e = threadIdx.x; e < kEvictBins; e += T) sm.bins[0][e] = sm.bins[1][e] = 0u;
+    if (threadIdx.x == 0) {
+      sm.live = sm.stays = sm.hi = 0u;
+      sm.lo = 0xffffffffu;
+    }
+    __syncthreads();
+  }
+  // Inclusive sum over the workgroup, and the total.  One barrier.
+  __device__ __forceinline__ uint32_t incl(uint32_t x, uint32_t* total) {
+    const int wid = threadIdx.x / kWave;
+    uint32_t* wsum = sm.wsum[turn];
+    turn ^= 1;
+    uint32_t s = wave_incl_add<uint32_t>(x);
+    if (lane_id() == kWave - 1) wsum[wid] = s;
+    __syncthreads();
+    uint32_t all = 0u;
+#pragma unroll
+    for (int w = 0; w < T / kWave; ++w) {
+      const uint32_t v = wsum[w];
+      if (w < wid) s += v;
+      all += v;
+    }
+    *total = all;
+    return s;
+  }
+  __device__ __forceinline__ uint32_t sum(uint32_t x) {
+    uint32_t all;
+    incl(x, &all);
+    return all;
+  }
+  // The bin of bins[which] (from the last downwards) where the count reaches
+  // `want`, from 1 to the total, and what is in the bins after it; the bins are
+  // zero again afterwards.  After a barrier; two barriers.
+  __device__ __forceinline__ void find_bin(int which, uint32_t want, uint32_t* bin, uint32_t* above) {
+    constexpr int B = kEvictBins / T;
+    const int hi = kEvictBins - 1 - B * static_cast<int>(threadIdx.x);
+    uint32_t c[B], s = 0u, all;
+#pragma unroll
+    for (int q = 0; q < B; ++q) {
+      c[q] = sm.bins[which][hi - q];
+      sm.bins[which][hi - q] = 0u;
+      s += c[q];
+    }
+    const int slot = turn;
+    uint32_t run = incl(s, &all) - s;
+    if (run < want && want <= run + s) {
+      bool found = false;
+#pragma unroll
+      for (int q = 0; q < B; ++q) {
+        if (!found && want <= run + c[q]) {
+          sm.bin[slot] = static_cast<uint32_t>(hi - q);
+          sm.above[slot] = run;
+          found = true;
+        }
+        run += c[q];
+      }
+    }
+    __syncthreads();
+    *bin = sm.bin[slot];
+    *above = sm.above[slot];
+  }
+  // The live entries, those that always stay, and the range of the others'
+  // keys, of each(f): f(key) for this thread's.  Once; one barrier.
+  template <class F>
+  __device__ __forceinline__ void look(F&& each, uint32_t* live, uint32_t* stays, uint32_t* lo, uint32_t* hi) {
+    uint32_t n = 0u, s = 0u, a = 0xffffffffu, b = 0u;
+    each([&](uint32_t k) {
+      n += k != 0u ? 1u : 0u;
+      s += k == kStays ? 1u : 0u;
+      const bool some = k != 0u && k != kStays;
+      a = some && k < a ? k : a;
+      b = some && k > b ? k : b;
+    });
+    n = wave_sum(n);
+    s = wave_sum(s);
+    a = wave_min_u32(a);
+    b = wave_max_u32(b);
+    if (lane_id() == 0) {
+      atomicAdd(&sm.live, n);
+      atomicAdd(&sm.stays, s);
+      atomicMin(&sm.lo, a);
+      atomicMax(&sm.hi, b);
+    }
+    __syncthreads();
+    *live = sm.live;
+    *stays = sm.stays;
+    *lo = sm.lo;
+    *hi = sm.hi;
+  }
+  static __device__ __forceinline__ int shift_of(uint32_t lo, uint32_t hi) {
+    const int bits = hi > lo ? 32 - __clz(static_cast<int>(hi - lo)) : 0;
+    return bits > 11 ? bits - 11 : 0;
+  }
+  // The `want`-th largest of the keys in [lo, hi] (at least that many), and how
+  // many that equal it are among the first `want`.
+  template <class F>
+  __device__ __forceinline__ void kth(F&& each, uint32_t want, uint32_t lo, uint32_t hi, uint32_t* key,
+                                      uint32_t* equal) {
+    for (int which = 0;; which ^= 1) {
+      const int shift = shift_of(lo, hi);
+      each([&](uint32_t k) {
+        if (k >= lo && k <= hi) atomicAdd(&sm.bins[which][(k - lo) >> shift], 1u);
+      });
+      __syncthreads();
+      uint32_t bin, above;
+      find_bin(which, want, &bin, &above);
+      want -= above;
+      lo += bin << shift;
+      const uint32_t end = lo + ((1u << shift) - 1u);
+      hi = end < hi ? end : hi;
+      if (shift == 0) break;
+    }
+    *key = lo;
+    *equal = want;
+  }
+  // The last key that stays and how many equal ones do, for `budget` of the
+  // entries of each(f); key 0 and none equal where all of them stay.
+  template <class F>
+  __device__ __forceinline__ void last_key(F&& each, uint32_t budget, uint32_t* key, uint32_t* equal) {
+    uint32_t live, stays, lo, hi;
+    look(each, &live, &stays, &lo, &hi);
+    *key = *equal = 0u;
+    if (live <= budget) return;
+    if (stays >= budget) {   // (positions that are not distinct)
+      *key = kStays;
+      *equal = budget;
+      return;
+    }
+    kth(each, budget - stays, lo, hi, key, equal);
+  }
+};
+
+// Which entries of the row are there, and which always stay.
+struct EvictRow {
+  const float* acc;
+  const int32_t* pos;   // null: positions are the slots
+  int64_t n;            // slots to look at
+  int32_t first_old;    // positions from here on are the last `recent`
+  int sink;
+  __device__ __forceinline__ uint32_t key(int64_t i) const {
+    return stay_key(acc[i], pos ? pos[i] : static_cast<int32_t>(i), first_old, sink);
+  }
+};
+__device__ __forceinline__ EvictRow evict_row(const EvictArgs& a, int64_t bh) {
+  const int32_t seen = a.seen[bh / a.kv] < 0 ? 0 : a.seen[bh / a.kv];
+  EvictRow r;
+  r.acc = a.acc + bh * a.room;
+  r.pos = a.pos ? a.pos + bh * a.room : nullptr;
+  r.n = !a.pos && seen < a.room ? seen : a.room;
+  r.first_old = seen - a.recent > 0 ? seen - a.recent : 0;
+  r.sink = a.sink;
+  return r;
+}
 }  // namespace
 
-__global__ __launch_bounds__(ET) void cache_select_kernel(EvictArgs a) {
-  __shared__ EvictSmem sm;
+// Rows of up to T PER slots: slot i T + t is item i of thread t.
+template <int T, int PER>
+__global__ __launch_bounds__(T) void cache_select_kernel(EvictArgs a) {
+  constexpr int W = T / kWave;
+  static_assert(PER * W <= T, "a thread per 64 slots");
+  __shared__ EvictSmem<T> sm;
+  __shared__ uint32_t counts[PER * W];   // kept and equal ones per 64 slots, then before them
+  EvictBlock<T> block{sm};
   const int tid = threadIdx.x, lane = lane_id(), wid = tid / kWave;
   const int64_t bh = blockIdx.x;
-  const int64_t b = bh / a.kv;
-  const float* acc = a.acc + bh * a.room;
-  const int32_t* pos = a.pos ? a.pos + bh * a.room : nullptr;
-  const int32_t seen = a.seen[b] < 0 ? 0 : a.seen[b];
-  const int32_t first_old = seen - a.recent > 0 ? seen - a.recent : 0;
-  // (positions are the slots where none are given)
-  const int64_t n = !pos && seen < a.room ? seen : a.room;
-  auto key_of = [&](int64_t i) -> uint32_t {
-    return stay_key(acc[i], pos ? pos[i] : static_cast<int32_t>(i), first_old, a.sink);
-  };
-  // digits from the top; want: entries still to be found among those that
-  // share the digits so far
-  uint32_t want = static_cast<uint32_t>(a.budget), prefix = 0u;
-  bool all = false;   // no more live entries than the budget
-  for (int p = 0; p < 3 && !all; ++p) {
-    const int shift = p == 0 ? 21 : (p == 1 ? 10 : 0);
-    const int upper = p == 0 ? 32 : (p == 1 ? 21 : 10);
-    const uint32_t mask = p == 2 ? 1023u : 2047u;
-    for (int e = tid; e < kEvictBins; e += ET) sm.bins[e] = 0u;
-    if (tid == 0) sm.live = 0u;
-    __syncthreads();
-    uint32_t mine = 0u;
-    for (int64_t i = tid; i < n; i += ET) {
-      const uint32_t k = key_of(i);
-      if (k != 0u && (p == 0 || (k >> (upper & 31)) == prefix)) {
-        atomicAdd(&sm.bins[(k >> shift) & mask], 1u);
-        ++mine;
-      }
-    }
-    if (p == 0) {
-      mine = wave_sum(mine);
-      if (lane == 0) atomicAdd(&sm.live, mine);
-    }
-    __syncthreads();
-    if (p == 0 && sm.live <= want) {
-      all = true;
-      break;
-    }
-    // the bin where the count from the largest key down reaches `want`
-    const int hi = kEvictBins - 1 - 2 * tid;   // two bins a thread, downwards
-    const uint32_t c0 = sm.bins[hi], c1 = sm.bins[hi - 1];
-    const uint32_t incl = wave_incl_add<uint32_t>(c0 + c1);
-    if (lane == kWave - 1) sm.wsum[wid] = incl;
-    __syncthreads();
-    uint32_t run = incl - c0 - c1;
+  const EvictRow row = evict_row(a, bh);
+  uint32_t k[PER];
 #pragma unroll
-    for (int w = 0; w < EW; ++w)
-      if (w < wid) run += sm.wsum[w];
-    if (run < want && want <= run + c0) {
-      sm.digit = static_cast<uint32_t>(hi);
-      sm.above = run;
-    } else if (run + c0 < want && want <= run + c0 + c1) {
-      sm.digit = static_cast<uint32_t>(hi - 1);
-      sm.above = run + c0;
-    }
-    __syncthreads();
-    want -= sm.above;
-    prefix = (prefix << (p == 2 ? 10 : 11)) | sm.digit;
-    __syncthreads();
+  for (int i = 0; i < PER; ++i) k[i] = i * T + tid < row.n ? row.key(i * T + tid) : 0u;
+  block.start();
+  uint32_t last, want;
+  block.last_key([&](auto&& f) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) f(k[i]);
+  }, static_cast<uint32_t>(a.budget), &last, &want);
+  // above the last key in the low half, equal to it in the high half (at most
+  // 32768 of each)
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const uint64_t gt = __ballot(k[i] > last), eq = __ballot(k[i] == last && k[i] != 0u);
+    if (lane == 0)
+      counts[i * W + wid] = static_cast<uint32_t>(__popcll(gt)) | (static_cast<uint32_t>(__popcll(eq)) << 16);
   }
-  // kept: above the last key, and the first `want` that equal it
-  const uint32_t last = all ? 1u : prefix;
-  if (all) want = 0xffffffffu;
+  __syncthreads();
+  const uint32_t c = tid < PER * W ? counts[tid] : 0u;
+  uint32_t all;
+  const uint32_t before = block.incl(c, &all) - c;
+  if (tid < PER * W) counts[tid] = before;
+  __syncthreads();
   int32_t* slots = a.slots + bh * a.budget;
-  uint32_t out = 0u, equal = 0u;   // kept, and equal ones seen, before this round
-  const int64_t rounds = (n + ET - 1) / ET;
-  for (int64_t q = 0; q < rounds; ++q) {
-    const int64_t i = q * ET + tid;
-    const uint32_t k = i < n ? key_of(i) : 0u;
-    const uint64_t gt = __ballot(k > last), eq = __ballot(k == last && k != 0u);
-    if (lane == 0) {
-      sm.wg[wid] = static_cast<uint32_t>(__popcll(gt));
-      sm.we[wid] = static_cast<uint32_t>(__popcll(eq));
-    }
-    __syncthreads();
-    const uint64_t before = (1ull << lane) - 1ull;
-    uint32_t g = static_cast<uint32_t>(__popcll(gt & before)), e = static_cast<uint32_t>(__popcll(eq & before));
-    uint32_t tg = 0u, te = 0u;
+  const uint64_t below = (1ull << lane) - 1ull;
 #pragma unroll
-    for (int w = 0; w < EW; ++w) {
-      if (w < wid) {
-        g += sm.wg[w];
-        e += sm.we[w];
-      }
-      tg += sm.wg[w];
-      te += sm.we[w];
-    }
-    // equal ones kept before this lane: at most `want` in all
-    const uint32_t eb = equal + e < want ? equal + e : want;
-    const uint32_t e0 = equal < want ? equal : want;
-    const bool keep = k > last || (k == last && k != 0u && equal + e < want);
-    const uint32_t at = out + g + (eb - e0);
-    if (keep && at < static_cast<uint32_t>(a.budget)) slots[at] = static_cast<int32_t>(i);
-    const uint32_t e1 = equal + te < want ? equal + te : want;
-    out += tg + (e1 - e0);
-    equal += te;
-    __syncthreads();
+  for (int i = 0; i < PER; ++i) {
+    const uint64_t gt = __ballot(k[i] > last), eq = __ballot(k[i] == last && k[i] != 0u);
+    const uint32_t b = counts[i * W + wid];
+    const uint32_t e = (b >> 16) + static_cast<uint32_t>(__popcll(eq & below));
+    const uint32_t at = (b & 0xffffu) + static_cast<uint32_t>(__popcll(gt & below)) + (e < want ? e : want);
+    if (k[i] > last || (k[i] == last && k[i] != 0u && e < want)) slots[at] = i * T + tid;
   }
-  for (int64_t j = out + tid; j < a.budget; j += ET) slots[j] = -1;
+  const uint32_t eq_all = all >> 16;
+  const int64_t kept = (all & 0xffffu) + (eq_all < want ? eq_all : want);
+  for (int64_t j = kept + tid; j < a.budget; j += T) slots[j] = -1;
+}
+
+// Longer rows.
+constexpr int ET = 1024;
+constexpr int EW = ET / kWave;
+
+__global__ __launch_bounds__(ET) void cache_select_long_kernel(EvictArgs a) {
+  __shared__ EvictSmem<ET> sm;
+  __shared__ uint64_t keep[kEvictWords], window[kEvictWords];
+  __shared__ uint32_t list[kEvictList];
+  __shared__ int32_t list_at[kEvictList];
+  EvictBlock<ET> block{sm};
+  const int tid = threadIdx.x, lane = lane_id(), wid = tid / kWave;
+  const int64_t bh = blockIdx.x;
+  const EvictRow row = evict_row(a, bh);
+  const int64_t n = row.n;
+  const uint32_t budget = static_cast<uint32_t>(a.budget);
+  int32_t* slots = a.slots + bh * a.budget;
+  const int words = static_cast<int>((n + 63) / 64);
+  bool done = words <= kEvictWords;
+  if (done) {
+    // 1. a window from the sample
+    constexpr int PER = kEvictSample / ET;
+    uint32_t k[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      k[i] = n > 0 ? row.key((static_cast<int64_t>(i) * ET + tid) * n / kEvictSample) : 0u;
+      if (k[i] == kStays) k[i] = 0u;
+    }
+    block.start();
+    uint32_t got, none, lo, hi;
+    const auto sample = [&](auto&& f) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) f(k[i]);
+    };
+    block.look(sample, &got, &none, &lo, &hi);
+    // ranks of its ends in the sample, from the largest: kEvictSigmas standard
+    // deviations of a binomial around the share that stays (of the entries
+    // that do not always stay)
+    const double always = static_cast<double>(a.sink) + static_cast<double>(a.recent);
+    const double total = row.pos ? static_cast<double>(n) * got / kEvictSample : n - always;
+    const double share = total > a.budget - always ? (a.budget - always) / total : 1.0;
+    const double mid = share * got, dev = kEvictSigmas * sqrt(got * (share * (1.0 - share))) + 2.0;
+    uint32_t wlo = 0u, whi = kStays - 1u;   // window of keys, both ends in it
+    if (got > 0u) {
+      const int shift = block.shift_of(lo, hi);
+      sample([&](uint32_t v) {
+        if (v != 0u) atomicAdd(&sm.bins[0][(v - lo) >> shift], 1u);
+        if (v != 0u) atomicAdd(&sm.bins[1][(v - lo) >> shift], 1u);
+      });
+      __syncthreads();
+      const bool top = mid - dev >= 1.0, bottom = mid + dev <= got;
+      const uint32_t r1 = top ? static_cast<uint32_t>(mid - dev) : 1u;
+      const uint32_t r2 = bottom ? static_cast<uint32_t>(mid + dev) : got;
+      uint32_t b1, b2, above1, above2, f1, f2, unused;
+      block.find_bin(0, r1, &b1, &above1);
+      block.find_bin(1, r2, &b2, &above2);
+      // the same once more inside the two bins
+      const uint32_t lo1 = lo + (b1 << shift), lo2 = lo + (b2 << shift);
+      const int fine = shift > 11 ? shift - 11 : 0;
+      sample([&](uint32_t v) {
+        if (v != 0u && (v - lo) >> shift == b1) atomicAdd(&sm.bins[0][(v - lo1) >> fine], 1u);
+        if (v != 0u && (v - lo) >> shift == b2) atomicAdd(&sm.bins[1][(v - lo2) >> fine], 1u);
+      });
+      __syncthreads();
+      block.find_bin(0, r1 - above1, &f1, &unused);
+      block.find_bin(1, r2 - above2, &f2, &unused);
+      if (top) whi = lo1 + (f1 << fine) + ((1u << fine) - 1u);
+      if (bottom) wlo = lo2 + (f2 << fine);
+    }
+    // 2. one pass: what is above the window stays, what is in it is marked.
+    // As floats; NaN (key 1) is below every window but an open one.
+    const bool open = wlo <= 1u;
+    const float vlo = open ? -INFINITY : key_value(wlo);
+    const float vhi = whi >= kStays - 1u ? INFINITY : key_value(whi);
+    constexpr int U = 16;
+    for (int w0 = wid; w0 < words; w0 += EW * U) {
+      float x[U];
+      int32_t ps[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t i = static_cast<int64_t>(w0 + u * EW) * 64 + lane;
+        const int64_t at = i < n ? i : 0;
+        x[u] = row.acc[at];
+        ps[u] = row.pos ? row.pos[at] : static_cast<int32_t>(i);
+        if (i >= n) ps[u] = -1;
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int w = w0 + u * EW;
+        const bool live = ps[u] >= 0;
+        const bool sure = live && (x[u] > vhi || ps[u] < row.sink || ps[u] >= row.first_old);
+        const bool in = live && !sure && (open || x[u] >= vlo);
+        const uint64_t ks = __ballot(sure), ws = __ballot(in);
+        if (lane == 0 && w < words) {
+          keep[w] = ks;
+          window[w] = ws;
+        }
+      }
+    }
+    __syncthreads();
+    // 3. the window's entries, in order
+    constexpr int WPT = kEvictWords / ET;
+    const int per = (words + ET - 1) / ET;   // words a thread takes, consecutive ones
+    uint32_t nk = 0u, nw = 0u;
+#pragma unroll
+    for (int q = 0; q < WPT; ++q) {
+      const int w = tid * per + q;
+      if (q < per && w < words) {
+        nk += static_cast<uint32_t>(__popcll(keep[w]));
+        nw += static_cast<uint32_t>(__popcll(window[w]));
+      }
+    }
+    const uint32_t sure = block.sum(nk);
+    uint32_t found;
+    uint32_t at = block.incl(nw, &found) - nw;
+    const uint32_t want = budget - sure;
+    done = sure <= budget && want <= found && found <= kEvictList;
+    if (done && want > 0u) {
+#pragma unroll
+      for (int q = 0; q < WPT; ++q) {
+        const int w = tid * per + q;
+        if (q < per && w < words) {
+          uint64_t bits = window[w];
+          while (bits) {
+            list_at[at++] = w * 64 + __ffsll(static_cast<unsigned long long>(bits)) - 1;
+            bits &= bits - 1;
+          }
+        }
+      }
+      __syncthreads();
+      constexpr int LPT = kEvictList / ET;
+      uint32_t key[LPT];
+#pragma unroll
+      for (int i = 0; i < LPT; ++i) {
+        const uint32_t j = i * ET + tid;
+        key[i] = j < found ? row.key(list_at[j]) : 0u;
+      }
+      const auto each = [&](auto&& f) {
+#pragma unroll
+        for (int i = 0; i < LPT; ++i) f(key[i]);
+      };
+      // (the window as it was asked for; a lower end at 1 leaves out no entry)
+      uint32_t last, equal;
+      block.kth(each, want, wlo > 1u ? wlo : 1u, whi, &last, &equal);
+      uint32_t eq = 0u;
+      each([&](uint32_t v) { eq += v == last ? 1u : 0u; });
+      if (block.sum(eq) == equal) {
+#pragma unroll
+        for (int i = 0; i < LPT; ++i)
+          if (key[i] >= last) {
+            const int32_t s = list_at[i * ET + tid];
+            atomicOr(reinterpret_cast<uint32_t*>(keep) + s / 32, 1u << (s % 32));
+          }
+      } else {   // the first of the equal ones
+        uint32_t before = 0u;
+#pragma unroll
+        for (int i = 0; i < LPT; ++i) {
+          const bool is = key[i] == last;
+          uint32_t all;
+          const uint32_t rank = before + block.incl(is ? 1u : 0u, &all) - (is ? 1u : 0u);
+          before += all;
+          if (key[i] > last || (is && rank < equal)) {
+            const int32_t s = list_at[i * ET + tid];
+            atomicOr(reinterpret_cast<uint32_t*>(keep) + s / 32, 1u << (s % 32));
+          }
+        }
+      }
+    }
+    __syncthreads();
+    if (done) {
+      // 4. the slots
+      uint32_t c = 0u, all;
+#pragma unroll
+      for (int q = 0; q < WPT; ++q) {
+        const int w = tid * per + q;
+        if (q < per && w < words) c += static_cast<uint32_t>(__popcll(keep[w]));
+      }
+      uint32_t out = block.incl(c, &all) - c;
+#pragma unroll
+      for (int q = 0; q < WPT; ++q) {
+        const int w = tid * per + q;
+        if (q < per && w < words) {
+          uint64_t bits = keep[w];
+          while (bits) {
+            slots[out++] = w * 64 + __ffsll(static_cast<unsigned long long>(bits)) - 1;
+            bits &= bits - 1;
+          }
+        }
+      }
+      for (int64_t j = static_cast<int64_t>(all) + tid; j < a.budget; j += ET) slots[j] = -1;
+      return;
+    }
+  }
+  // every digit by a pass over the row, and one more for the slots, a wave's
+  // part of the row consecutive
+  __syncthreads();
+  block.start();
+  uint32_t last, want;
+  block.last_key([&](auto&& f) {
+    for (int64_t i = tid; i < n; i += ET) f(row.key(i));
+  }, budget, &last, &want);
+  const int64_t part = (n + 64 * EW - 1) / (64 * EW) * 64;
+  const int64_t i0 = wid * part, i1 = i0 + part < n ? i0 + part : n;
+  uint32_t gt = 0u, eq = 0u;
+  for (int64_t i = i0 + lane; i < i1; i += kWave) {
+    const uint32_t k = row.key(i);
+    gt += k > last ? 1u : 0u;
+    eq += k == last && k != 0u ? 1u : 0u;
+  }
+  gt = wave_sum(gt);
+  eq = wave_sum(eq);
+  __shared__ uint32_t wgt[EW], weq[EW];
+  if (lane == 0) {
+    wgt[wid] = gt;
+    weq[wid] = eq;
+  }
+  __syncthreads();
+  uint32_t g = 0u, e = 0u, all_g = 0u, all_e = 0u;
+  for (int w = 0; w < EW; ++w) {
+    if (w < wid) {
+      g += wgt[w];
+      e += weq[w];
+    }
+    all_g += wgt[w];
+    all_e += weq[w];
+  }
+  const uint64_t below = (1ull << lane) - 1ull;
+  for (int64_t j = i0; j < i1; j += kWave) {
+    const int64_t i = j + lane;
+    const uint32_t k = i < i1 ? row.key(i) : 0u;
+    const uint64_t mg = __ballot(k > last), me = __ballot(k == last && k != 0u);
+    const uint32_t er = e + static_cast<uint32_t>(__popcll(me & below));
+    const uint32_t at = g + static_cast<uint32_t>(__popcll(mg & below)) + (er < want ? er : want);
+    if (k > last || (k == last && k != 0u && er < want)) slots[at] = static_cast<int32_t>(i);
+    g += static_cast<uint32_t>(__popcll(mg));
+    e += static_cast<uint32_t>(__popcll(me));
+  }
+  const int64_t kept = static_cast<int64_t>(all_g) + (all_e < want ? all_e : want);
+  for (int64_t j = kept + tid; j < a.budget; j += ET) slots[j] = -1;
 }
 
 // Rows of K and V, acc and positions of the kept slots: a team of `team`
@@ -383,8 +742,13 @@ hipError_t launch_cache_accumulate(AccumulateArgs a, int dtype, hipStream_t s) {
 
 // Sizes and strides of K and V in vectors of `width` bytes.
 hipError_t launch_cache_evict(EvictArgs a, int width, hipStream_t s) {
+  const dim3 rows(static_cast<unsigned>(a.batch * a.kv));
   { ProfScope ps_("cache_select", s);
-  hipLaunchKernelGGL(cache_select_kernel, dim3(static_cast<unsigned>(a.batch * a.kv)), dim3(ET), 0, s, a); }
+  if (a.room <= 1024) hipLaunchKernelGGL((cache_select_kernel<256, 4>), rows, dim3(256), 0, s, a);
+  else if (a.room <= 4096) hipLaunchKernelGGL((cache_select_kernel<512, 8>), rows, dim3(512), 0, s, a);
+  else if (a.room <= 8192) hipLaunchKernelGGL((cache_select_kernel<1024, 8>), rows, dim3(1024), 0, s, a);
+  else if (a.room <= 32768) hipLaunchKernelGGL((cache_select_kernel<1024, 32>), rows, dim3(1024), 0, s, a);
+  else hipLaunchKernelGGL(cache_select_long_kernel, rows, dim3(ET), 0, s, a); }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   a.team = 1;

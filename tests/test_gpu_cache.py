@@ -141,6 +141,28 @@ def test_evict_ties_and_values_that_are_none(lib, slots):
         _check_evict(lib, k, v, acc, seen, budget, sink, recent)
 
 
+@pytest.mark.parametrize("slots", [32_769, 100_000, 262_144, 300_007])
+def test_evict_long_rows_that_a_sample_misleads(lib, slots):
+    """Values that the sample's stride meets or misses, sorted rows, rows of few
+    values and of one, and budgets from nearly none to nearly all."""
+    import torch
+    k, v, _ = _cache(7, 1, 8, slots, 2)
+    gen = torch.Generator(device="cuda").manual_seed(slots)
+    acc = torch.rand(1, 8, slots, generator=gen, device="cuda")
+    acc[0, 1] = acc[0, 1].sort()[0]
+    acc[0, 2] = acc[0, 2].sort(descending=True)[0]
+    acc[0, 3, :] = 0.5
+    acc[0, 4] = (acc[0, 4] * 3).floor()
+    acc[0, 5, ::slots // 4096] = 10.0 + acc[0, 5, ::slots // 4096]
+    acc[0, 6] = acc[0, 6].pow(40)
+    acc[0, 7] = -acc[0, 7]
+    acc[0, 7, ::5] = float("nan")
+    seen = torch.tensor([slots], dtype=torch.int32, device="cuda")
+    for budget, sink, recent in ((1, 0, 0), (100, 4, 64), (slots // 30, 4, 64), (slots // 2, 0, 1),
+                                 (slots - 7, 3, 4), (slots // 2, slots // 4, slots // 4)):
+        _check_evict(lib, k, v, acc, seen, budget, sink, recent)
+
+
 @pytest.mark.parametrize("slots", [40, 2000, 36_000])
 def test_evict_by_positions(lib, slots):
     """Slots that earlier steps left in any order, with empty ones between."""
