@@ -141,6 +141,7 @@ constexpr int kEvictBins = 2048;
 constexpr int kEvictSample = 4096;
 constexpr int kEvictList = 8192;             // entries of the window
 constexpr int kEvictWords = 4096;            // 64 slots each
+constexpr int kEvictRound = 16;              // loads in flight per lane
 constexpr double kEvictSigmas = 4.0;
 
 namespace {
@@ -438,42 +439,92 @@ __global__ __launch_bounds__(ET) void cache_select_long_kernel(EvictArgs a) {
     const bool open = wlo <= 1u;
     const float vlo = open ? -INFINITY : key_value(wlo);
     const float vhi = whi >= kStays - 1u ? INFINITY : key_value(whi);
-    constexpr int U = 16;
-    for (int w0 = wid; w0 < words; w0 += EW * U) {
-      float x[U];
-      int32_t ps[U];
+    // One compute unit's instructions bound the pass, so a wave takes 64 words in
+    // a row: loads at fixed offsets, two comparisons, and the masks into the
+    // lanes of a register.  (Words past the last may be marked.)
+    const int w1 = __builtin_amdgcn_readfirstlane(wid);
+    const uint32_t end = static_cast<uint32_t>(n - 1);
+    for (int s = w1; s * 64 < words; s += EW) {
+      uint32_t k0 = 0u, k1 = 0u, i0 = 0u, i1 = 0u;
+      const auto mark = [&](const float (&x)[kEvictRound], int b) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int64_t i = static_cast<int64_t>(w0 + u * EW) * 64 + lane;
-        const int64_t at = i < n ? i : 0;
-        x[u] = row.acc[at];
-        ps[u] = row.pos ? row.pos[at] : static_cast<int32_t>(i);
-        if (i >= n) ps[u] = -1;
-      }
+        for (int u = 0; u < kEvictRound; ++u) {
+          const uint64_t ks = __ballot(x[u] > vhi), ws = __ballot(x[u] >= vlo);
+          const int to = b * kEvictRound + u;
+          k0 = lane == to ? static_cast<uint32_t>(ks) : k0;
+          k1 = lane == to ? static_cast<uint32_t>(ks >> 32) : k1;
+          i0 = lane == to ? static_cast<uint32_t>(ws) : i0;
+          i1 = lane == to ? static_cast<uint32_t>(ws >> 32) : i1;
+        }
+      };
+      constexpr int rounds = 64 / kEvictRound;
+      float x[2][kEvictRound];
+      if (static_cast<int64_t>(s + 1) * 4096 <= n) {
+        const float* from = row.acc + static_cast<int64_t>(s) * 4096 + lane;
+        const auto fetch = [&](float (&y)[kEvictRound], int b) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int w = w0 + u * EW;
-        const bool live = ps[u] >= 0;
-        const bool sure = live && (x[u] > vhi || ps[u] < row.sink || ps[u] >= row.first_old);
-        const bool in = live && !sure && (open || x[u] >= vlo);
-        const uint64_t ks = __ballot(sure), ws = __ballot(in);
-        if (lane == 0 && w < words) {
-          keep[w] = ks;
-          window[w] = ws;
+          for (int u = 0; u < kEvictRound; ++u) y[u] = from[(b * kEvictRound + u) * 64];
+        };
+        fetch(x[0], 0);
+#pragma unroll
+        for (int b = 0; b < rounds; ++b) {
+          if (b + 1 < rounds) fetch(x[(b + 1) % 2], b + 1);
+          mark(x[b % 2], b);
+        }
+      } else {
+#pragma unroll 1
+        for (int b = 0; b < rounds; ++b) {
+#pragma unroll
+          for (int u = 0; u < kEvictRound; ++u) {
+            const uint32_t i = static_cast<uint32_t>(s * 64 + b * kEvictRound + u) * 64u + static_cast<uint32_t>(lane);
+            x[0][u] = row.acc[i < end ? i : end];
+          }
+          mark(x[0], b);
         }
       }
+      keep[s * 64 + lane] = (static_cast<uint64_t>(k1) << 32) | k0;
+      window[s * 64 + lane] = open ? ~0ull : (static_cast<uint64_t>(i1) << 32) | i0;
     }
+    if (row.pos) __syncthreads();   // (other waves' words)
+    if (row.pos)   // by their positions: what always stays, and what is there
+      for (int w0 = w1; w0 < words; w0 += EW * kEvictRound) {
+        int32_t ps[kEvictRound];
+#pragma unroll
+        for (int u = 0; u < kEvictRound; ++u) {
+          const uint32_t i = static_cast<uint32_t>(w0 + u * EW) * 64u + static_cast<uint32_t>(lane);
+          ps[u] = row.pos[i < end ? i : end];
+        }
+#pragma unroll
+        for (int u = 0; u < kEvictRound; ++u) {
+          const uint64_t there = __ballot(ps[u] >= 0);
+          const uint64_t stays = __ballot(ps[u] < row.sink || ps[u] >= row.first_old);
+          if (lane == 0 && w0 + u * EW < words) {
+            keep[w0 + u * EW] = (keep[w0 + u * EW] | stays) & there;
+            window[w0 + u * EW] &= there;
+          }
+        }
+      }
     __syncthreads();
     // 3. the window's entries, in order
     constexpr int WPT = kEvictWords / ET;
     const int per = (words + ET - 1) / ET;   // words a thread takes, consecutive ones
+    const auto from = [](int64_t first) -> uint64_t {   // bits `first` on
+      return first <= 0 ? ~0ull : (first >= 64 ? 0ull : ~0ull << first);
+    };
     uint32_t nk = 0u, nw = 0u;
 #pragma unroll
     for (int q = 0; q < WPT; ++q) {
       const int w = tid * per + q;
       if (q < per && w < words) {
-        nk += static_cast<uint32_t>(__popcll(keep[w]));
-        nw += static_cast<uint32_t>(__popcll(window[w]));
+        const int64_t s0 = static_cast<int64_t>(w) * 64;
+        uint64_t ks = keep[w];
+        if (!row.pos) ks |= ~from(row.sink - s0) | from(row.first_old - s0);
+        ks &= ~from(n - s0);
+        const uint64_t ws = window[w] & ~from(n - s0) & ~ks;
+        keep[w] = ks;
+        window[w] = ws;
+        nk += static_cast<uint32_t>(__popcll(ks));
+        nw += static_cast<uint32_t>(__popcll(ws));
       }
     }
     const uint32_t sure = block.sum(nk);
