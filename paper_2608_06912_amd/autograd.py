@@ -213,6 +213,16 @@ def _load_node():
 _PLAIN = (torch.Tensor, torch.nn.Parameter)
 
 
+def _eager():
+    """Nothing looks at the calls or transforms them: no torch function or
+    dispatch mode, functorch transform, forward-mode AD, tracing or compilation."""
+    return not (torch.compiler.is_compiling()
+                or torch._C._len_torch_function_stack() or torch._C._len_torch_dispatch_stack()
+                or torch._C._are_functorch_transforms_active()
+                or torch.autograd.forward_ad._current_level >= 0
+                or torch._C._get_tracing_state() is not None)
+
+
 def _native_full(scores, k, alpha, ste=False):
     """p of the full path (ste: the hard mask with p's gradient) through the
     native node, or None where the Python node has to run: a tensor subclass,
@@ -224,12 +234,7 @@ def _native_full(scores, k, alpha, ste=False):
             or (at and type(alpha) not in _PLAIN) or not scores.is_cuda
             or scores.layout is not torch.strided or scores.numel() == 0
             or scores.is_complex() or scores.is_quantized
-            or (kt and k.numel() != 1) or (at and alpha.numel() != 1)
-            or torch.compiler.is_compiling()
-            or torch._C._len_torch_function_stack() or torch._C._len_torch_dispatch_stack()
-            or torch._C._are_functorch_transforms_active()
-            or torch.autograd.forward_ad._current_level >= 0
-            or torch._C._get_tracing_state() is not None):
+            or (kt and k.numel() != 1) or (at and alpha.numel() != 1) or not _eager()):
         return None
     node = _node or _load_node()
     if not node:
@@ -294,6 +299,9 @@ def soft_topk(scores, k, alpha, *, path: str = "auto", sample: str = "n23", z: f
     return straight_through(p, hard_topk_mask(scores.detach(), int(float(k)))) if ste else p
 
 
+_ROUTE_SCORES = {"softmax": 0, "sigmoid": 1}
+
+
 class RouteFunction(torch.autograd.Function):
     """The weights of lapsum_route_forward as an autograd node: the gradient
     with respect to the logits, the chosen experts held fixed."""
@@ -303,12 +311,15 @@ class RouteFunction(torch.autograd.Function):
         out = lapsum_route_forward(logits.detach(), top_k, counts=counts, **options)
         ctx.options = {name: options[name] for name in ("score", "renormalise", "scale")}
         ctx.save_for_backward(logits, out[1])
+        ctx.set_materialize_grads(False)
         ctx.mark_non_differentiable(*out[1:])
         return out
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, grad_weights, *unused):
+        if grad_weights is None:
+            return None, None, None, None
         logits, indices = ctx.saved_tensors
         g = grad_weights
         if g.dtype != torch.float32:
@@ -326,5 +337,16 @@ def route_topk(logits, top_k: int, *, score: str = "softmax", bias=None, groups:
     options = {"score": score, "bias": bias, "groups": groups, "topk_groups": topk_groups,
                "group_top": group_top, "renormalise": renormalise, "scale": scale}
     if torch.is_grad_enabled() and isinstance(logits, torch.Tensor) and logits.requires_grad:
+        node = _node or _load_node()
+        if (node and type(logits) in _PLAIN and (bias is None or type(bias) in _PLAIN)
+                and score in _ROUTE_SCORES and _eager()):
+            try:
+                out = node.route(logits, top_k, _ROUTE_SCORES[score], bias, groups,
+                                 groups if topk_groups is None else topk_groups, group_top,
+                                 renormalise, scale, counts, True)
+            except TypeError:
+                out = None
+            if out is not None:
+                return tuple(out)
         return RouteFunction.apply(logits, top_k, options, counts)
     return lapsum_route_forward(logits, top_k, counts=counts, **options)

@@ -32,6 +32,7 @@ HIP_SOURCES = ["row_kernels.hip", "stream_kernels.hip", "sort_kernels.hip",
                "route.hip", "beam.hip", "cache.hip"]
 HOST_SOURCES = ["lapsum_api.cpp", "selection_api.cpp"]
 NODE_SOURCE = "autograd_node.cpp"
+NODE_SOURCES = [NODE_SOURCE, "selection_node.cpp"]
 
 ARCH = "gfx950"
 COMMON = ["-O3", "-std=c++17", "-fPIC", f"-I{INCLUDE}", f"-I{CSRC}"]
@@ -55,7 +56,7 @@ def _compile(args):
     return src
 
 
-def _node_compile(hipcc: str, rocm_inc: str, obj: str) -> list:
+def _node_compile(hipcc: str, rocm_inc: str, src: str, obj: str) -> list:
     import sysconfig
 
     import torch
@@ -65,7 +66,7 @@ def _node_compile(hipcc: str, rocm_inc: str, obj: str) -> list:
     return [hipcc, "-O2", "-std=c++17", "-fPIC", "-x", "c++", "-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM",
             "-DTORCH_EXTENSION_NAME=_node", "-DTORCH_API_INCLUDE_EXTENSION_H",
             f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", *incs, "-c",
-            os.path.join(CSRC, NODE_SOURCE), "-o", obj]
+            os.path.join(CSRC, src), "-o", obj]
 
 
 def build(verbose: bool = False, jobs: int | None = None) -> str:
@@ -90,8 +91,9 @@ def build(verbose: bool = False, jobs: int | None = None) -> str:
         # torch the library alone is built
         node = None
         if importlib.util.find_spec("torch") is not None:
-            node_obj = os.path.join(BUILD, NODE_SOURCE + ".o")
-            node = ex.submit(lambda: _compile((_node_compile(hipcc, rocm_inc, node_obj), NODE_SOURCE)))
+            node_objs = [os.path.join(BUILD, src + ".o") for src in NODE_SOURCES]
+            node = [ex.submit(lambda s=src, o=obj: _compile((_node_compile(hipcc, rocm_inc, s, o), s)))
+                    for src, obj in zip(NODE_SOURCES, node_objs)]
         for src in ex.map(_compile, work):
             if verbose:
                 print(f"compiled {src}", flush=True)
@@ -101,10 +103,13 @@ def build(verbose: bool = False, jobs: int | None = None) -> str:
         if node is None:
             print("torch not found: the native autograd node is not built", flush=True)
             return LIB
-        node.result()
-    _link_node(hipcc, node_obj)
+        for unit in node:
+            src = unit.result()
+            if verbose:
+                print(f"compiled {src}", flush=True)
+    _link_node(hipcc, node_objs)
     if verbose:
-        print(f"compiled {NODE_SOURCE}\nbuilt {NODE}", flush=True)
+        print(f"built {NODE}", flush=True)
     return LIB
 
 
@@ -120,11 +125,11 @@ def _link_library(hipcc: str, objs: list) -> None:
     os.replace(tmp, LIB)
 
 
-def _link_node(hipcc: str, node_obj: str) -> None:
+def _link_node(hipcc: str, node_objs: list) -> None:
     import torch
     tlib = os.path.join(os.path.dirname(torch.__file__), "lib")
     tmp = NODE + ".tmp"
-    _run([hipcc, "-shared", "-o", tmp, node_obj, LIB, f"-L{tlib}", "-lc10", "-lc10_hip",
+    _run([hipcc, "-shared", "-o", tmp, *node_objs, LIB, f"-L{tlib}", "-lc10", "-lc10_hip",
           "-ltorch_cpu", "-ltorch_python", "-ltorch", "-Wl,-rpath,$ORIGIN"])
     os.replace(tmp, NODE)
 

@@ -8,49 +8,17 @@
 // What the two share: the forward saves p, the backward returns dL/dscores
 // and, for k and alpha given as tensors that require grad, dL/dk and
 // dL/dalpha summed over the rows.
-#include <torch/extension.h>
-
-#include <ATen/hip/impl/HIPStreamMasqueradingAsCUDA.h>
-#include <c10/core/DeviceGuard.h>
-
-#include <torch/csrc/Exceptions.h>
-
-#include <stdexcept>
-
-#include "../../include/lapsum.h"
+#include "node.hpp"
 
 namespace {
 
+using lapsum_node::bytes;
+using lapsum_node::check;
+using lapsum_node::ptr;
+using lapsum_node::stream_of;
 using torch::Tensor;
 using torch::autograd::AutogradContext;
 using torch::autograd::variable_list;
-
-// A library call that failed, as the binding's own exception: LapsumError with
-// the status and the entry point's name.
-struct Failed : std::runtime_error {
-  Failed(int status, const char* where) : std::runtime_error(where), status(status) {}
-  int status;
-};
-
-void check(int status, const char* where) {
-  if (status != LAPSUM_OK) throw Failed(status, where);
-}
-
-// Sets it as the current Python error (with the GIL held).
-void set_error(const Failed& f) {
-  const py::object type = py::module_::import("paper_2608_06912_amd").attr("LapsumError");
-  PyErr_SetObject(type.ptr(), type(f.status, f.what()).ptr());
-}
-
-hipStream_t stream_of(const Tensor& x) {
-  return c10::hip::getCurrentHIPStreamMasqueradingAsCUDA(x.device().index()).stream();
-}
-
-Tensor bytes(size_t n, const Tensor& like) {
-  return n ? at::empty({static_cast<int64_t>(n)}, like.options().dtype(at::kByte)) : Tensor();
-}
-
-void* ptr(const Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
 
 struct FullNode : public torch::autograd::Function<FullNode> {
   static Tensor forward(AutogradContext* ctx, const Tensor& scores,
@@ -89,15 +57,7 @@ struct FullNode : public torch::autograd::Function<FullNode> {
   }
 
   static variable_list backward(AutogradContext* ctx, variable_list grads) {
-    try {
-      return vjp(ctx, grads);
-    } catch (const Failed& f) {   // on the engine's thread
-      const py::gil_scoped_acquire gil;
-      set_error(f);
-      python_error e;
-      e.persist();
-      throw e;
-    }
+    return lapsum_node::in_engine([&] { return vjp(ctx, grads); });
   }
 
   static variable_list vjp(AutogradContext* ctx, const variable_list& grads) {
@@ -159,17 +119,14 @@ struct FullNode : public torch::autograd::Function<FullNode> {
 
 }  // namespace
 
+namespace {
+Tensor full(const Tensor& scores, const std::optional<Tensor>& k_like,
+            const std::optional<Tensor>& alpha_like, double k, double alpha, bool ste) {
+  return FullNode::apply(scores, k_like, alpha_like, k, alpha, ste);
+}
+}  // namespace
+
 PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
-  m.def("full", [](const Tensor& scores, const std::optional<Tensor>& k_like,
-                   const std::optional<Tensor>& alpha_like, double k, double alpha, bool ste) {
-    try {
-      // without the GIL, as a ctypes call runs: an allocation or a launch can
-      // wait for the device
-      const py::gil_scoped_release nogil;
-      return FullNode::apply(scores, k_like, alpha_like, k, alpha, ste);
-    } catch (const Failed& f) {
-      set_error(f);
-      throw py::error_already_set();
-    }
-  });
+  m.def("full", lapsum_node::entry(full));
+  bind_selection(m);
 }

@@ -75,6 +75,21 @@ def _load():
     return lib
 
 
+_native = None
+
+
+def _node():
+    """The calls in native code (csrc/selection_node.cpp), or False where only
+    the library is built.  They take the common case and return None (or
+    raise TypeError, for arguments of another type) for everything else, which
+    then comes to the checks here."""
+    global _native
+    if _native is None:
+        from .autograd import _load_node
+        _native = _load_node()
+    return _native
+
+
 def _dtype(x, name):
     global _dtypes
     if _dtypes is None:
@@ -141,6 +156,16 @@ def lapsum_route_forward(logits, top_k: int, *, score: str = "softmax", bias=Non
     with counts=True the tokens per expert, int32.  score "softmax" or
     "sigmoid"; bias: float32 [experts], added to the scores for the choice
     only.  A place without an expert has index -1 and weight 0."""
+    node = _native or _node()
+    if node and workspace is None and score in _SCORES:
+        try:
+            out = node.route(logits, top_k, _SCORES[score], bias, groups,
+                             groups if topk_groups is None else topk_groups, group_top, renormalise,
+                             scale, counts, False)
+        except TypeError:
+            out = None
+        if out is not None:
+            return tuple(out)
     torch = _torch()
     lib = _lib or _load()
     _device_tensor(logits, "logits")
@@ -206,6 +231,14 @@ def lapsum_beam_select(logits, beam_scores, num: int, *, workspace=None):
     vocab] or [batch, beams, vocab], beam_scores float32 [batch, beams].
     Returns (scores, tokens, parents), each [batch, num]; score -inf, token -1
     and parent -1 where no continuation is left."""
+    node = _native or _node()
+    if node and workspace is None:
+        try:
+            out = node.beam_select(logits, beam_scores, num)
+        except TypeError:
+            out = None
+        if out is not None:
+            return out
     torch = _torch()
     lib = _lib or _load()
     _device_tensor(logits, "logits")
@@ -237,14 +270,21 @@ def lapsum_beam_reorder(states, parents, *, length: int | None = None, out=None)
     [batch * beams, heads, room, dim] (any dimensions before room), move only
     the first `length` of room.  In place, or with `out` (as many tensors of
     the same shapes) into those.  Returns the tensors written."""
+    states = list(states)
+    outs = states if out is None else list(out)
+    node = _native or _node()
+    if node:
+        try:
+            if node.beam_reorder(states, parents, length, outs):
+                return outs
+        except TypeError:
+            pass
     torch = _torch()
     lib = _lib or _load()
-    states = list(states)
     _device_tensor(parents, "parents", torch.int32)
     if parents.dim() != 2 or parents.stride(1) != 1 and parents.shape[1] > 1:
         raise ValueError("parents must be [batch, beams] with dense rows")
     batch, beams = parents.shape
-    outs = states if out is None else list(out)
     if len(outs) != len(states):
         raise ValueError("out must have one tensor for each state")
     dev = parents.device
@@ -295,6 +335,14 @@ def lapsum_cache_accumulate(weights, kv_heads: int, *, seen=None, acc=None):
     summed over the query heads that share a key head and over the queries, to
     float32 [batch, kv_heads, keys].  seen (int32 [batch]): only the first
     seen[b] columns of a sequence count.  acc: added to, in place."""
+    node = _native or _node()
+    if node:
+        try:
+            out = node.cache_accumulate(weights, kv_heads, seen, acc)
+        except TypeError:
+            out = None
+        if out is not None:
+            return out if acc is None else acc
     torch = _torch()
     lib = _lib or _load()
     _device_tensor(weights, "weights")
@@ -330,6 +378,14 @@ def lapsum_cache_evict(k, v, acc, seen, budget: int, *, sink: int = 0, recent: i
     float32 [batch, kv_heads, slots], seen int32 [batch], and pos int32 like
     acc where slots do not hold their own positions.  Returns (k, v, acc, pos)
     with `budget` slots; where fewer stay, zeros and position -1 follow."""
+    node = _native or _node()
+    if node and workspace is None:
+        try:
+            out = node.cache_evict(k, v, acc, seen, budget, sink, recent, pos)
+        except TypeError:
+            out = None
+        if out is not None:
+            return out
     torch = _torch()
     lib = _lib or _load()
     _device_tensor(k, "k")
@@ -367,6 +423,14 @@ def lapsum_cache_step(weights, k_new, v_new, seen, k, v, acc, pos, *, sink: int 
     take the first empty slot (pos -1) or that of the smallest acc outside the
     first `sink` and last `recent` positions, at position seen[b].  Returns the slots, int32
     [batch, kv_heads].  The caller advances seen."""
+    node = _native or _node()
+    if node:
+        try:
+            out = node.cache_step(weights, k_new, v_new, seen, k, v, acc, pos, sink, recent)
+        except TypeError:
+            out = None
+        if out is not None:
+            return out
     torch = _torch()
     lib = _lib or _load()
     _device_tensor(weights, "weights")
