@@ -97,6 +97,25 @@ struct BestList {
   }
 };
 
+// A value that at least `num` lanes' reach: the largest but for its low bits,
+// which are not looked for once few more lanes do.
+__device__ __forceinline__ float nth_bound(float mx, int num) {
+  const uint32_t key = asc_key(mx);
+  const uint32_t differ = wave_max_u32(key) ^ wave_min_u32(key);
+  const int bits = differ ? 32 - __clz(static_cast<int>(differ)) : 0;   // that are not common
+  uint32_t K = bits < 32 ? (wave_max_u32(key) >> bits) << bits : 0u;
+  int count = kWave;
+  for (int bit = bits - 1; bit >= 0 && count > num + 4; --bit) {
+    const uint32_t cand = K | (1u << bit);
+    const int c = __popcll(__ballot(key >= cand));
+    if (c >= num) {
+      K = cand;
+      count = c;
+    }
+  }
+  return key_value(K);
+}
+
 // The VE elements of a row from `first` on; past the row -inf.  (A row starts at
 // any element: the loads are as wide as they are at any alignment, and a
 // row's parts do not depend on its address, so equal rows get equal sums.)
@@ -106,23 +125,27 @@ struct RowVec {
 };
 template <int DT>
 __device__ __forceinline__ void load_vec(const typename Elem<DT>::raw* __restrict__ row, int64_t first,
-                                         int64_t V, float* x) {
+                                         int64_t V, uint32_t (&w)[4]) {
   constexpr int VE = RowVec<DT>::VE;
   if (first + VE <= V) {
-    uint32_t w[4];
     __builtin_memcpy(w, row + first, 16);
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      if constexpr (DT == 0) {
-        x[q] = Elem<0>::get(w[q]);
-      } else {
-        x[2 * q] = Elem<DT>::get(w[q] & 0xffffu);
-        x[2 * q + 1] = Elem<DT>::get(w[q] >> 16);
-      }
-    }
   } else {
+    typename Elem<DT>::raw r[VE];
 #pragma unroll
-    for (int j = 0; j < VE; ++j) x[j] = first + j < V ? Elem<DT>::get(row[first + j]) : -INFINITY;
+    for (int j = 0; j < VE; ++j) r[j] = first + j < V ? row[first + j] : Elem<DT>::put(-INFINITY);
+    __builtin_memcpy(w, r, 16);
+  }
+}
+template <int DT>
+__device__ __forceinline__ void get_vec(const uint32_t (&w)[4], float* x) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    if constexpr (DT == 0) {
+      x[q] = Elem<0>::get(w[q]);
+    } else {
+      x[2 * q] = Elem<DT>::get(w[q] & 0xffffu);
+      x[2 * q + 1] = Elem<DT>::get(w[q] >> 16);
+    }
   }
 }
 
@@ -154,11 +177,19 @@ __global__ __launch_bounds__(BT) void beam_scan_kernel(BeamArgs a) {
   bool first = true;
   // (a wave's steps are consecutive: later ones hold higher indices)
   const int64_t s0 = (static_cast<int64_t>(blockIdx.x) * BW + wid) * a.steps;
-  for (int64_t st = s0; st < s0 + a.steps && st < a.row_steps; ++st) {
-    float x[U][VE];
+  const int64_t s1 = s0 + a.steps < a.row_steps ? s0 + a.steps : a.row_steps;
+  uint32_t next[U][4];   // the next step's logits, under way while one is worked on
+  const auto fetch = [&](int64_t st) {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      load_vec<DT>(row, ((st * U + u) * kWave + lane) * VE, a.vocab, x[u]);
+    for (int u = 0; u < U; ++u) load_vec<DT>(row, ((st * U + u) * kWave + lane) * VE, a.vocab, next[u]);
+  };
+  if (s0 < s1) fetch(s0);
+  for (int64_t st = s0; st < s1; ++st) {
+    float x[U][VE];
+    const int64_t at = (st * U * kWave + lane) * VE;   // of u = 0
+#pragma unroll
+    for (int u = 0; u < U; ++u) get_vec<DT>(next[u], x[u]);
+    if (st + 1 < s1) fetch(st + 1);
     float mx = -INFINITY;
 #pragma unroll
     for (int u = 0; u < U; ++u)
@@ -180,24 +211,24 @@ __global__ __launch_bounds__(BT) void beam_scan_kernel(BeamArgs a) {
       sum += static_cast<double>(t);
     }
     if (first) {
-      // the num-th largest of the lanes' maxima: at least num logits reach it
-      const uint32_t key = asc_key(mx);
-      uint32_t K = 0u;
-      for (int bit = 31; bit >= 0; --bit) {
-        const uint32_t cand = K | (1u << bit);
-        if (__popcll(__ballot(key >= cand)) >= a.num) K = cand;
-      }
-      const float at = key_value(K);
-      best.base = best.admit = at >= -FLT_MAX ? at : -FLT_MAX;
+      best.base = best.admit = fmaxf(nth_bound(mx, a.num), -FLT_MAX);
       first = false;
     }
     if (__ballot(mx >= best.admit)) {
+      // each lane's wanted logits as bits, then one of each lane at a time (its
+      // value read again: registers have no index)
+      uint32_t bits = 0u;
 #pragma unroll
-      for (int u = 0; u < U; ++u)
+      for (int u = U - 1; u >= 0; --u)
 #pragma unroll
-        for (int j = 0; j < VE; ++j)
-          best.push(x[u][j] >= best.admit, x[u][j],
-                    static_cast<uint32_t>(((st * U + u) * kWave + lane) * VE + j));
+        for (int j = VE - 1; j >= 0; --j) bits = bits + bits + (x[u][j] >= best.admit ? 1u : 0u);
+      while (__ballot(bits != 0u)) {
+        const int q = bits ? __ffs(bits) - 1 : 0;
+        const int64_t v = at + static_cast<int64_t>(q / VE) * (kWave * VE) + q % VE;
+        const float y = bits ? Elem<DT>::get(row[v]) : -INFINITY;
+        best.push(y >= best.admit, y, static_cast<uint32_t>(v));
+        bits &= bits - 1u;
+      }
     }
     best.all_later();
   }
@@ -237,7 +268,7 @@ __global__ __launch_bounds__(BT) void beam_scan_kernel(BeamArgs a) {
 template <int DT>
 __global__ __launch_bounds__(BT) void beam_finish_kernel(BeamArgs a) {
   using raw = typename Elem<DT>::raw;
-  __shared__ uint64_t lists[BW][kList];
+  __shared__ uint64_t list[kList];
   __shared__ float lse[kBeamMaxBeams];
   __shared__ int again;
   __shared__ int wcount[BW];
@@ -263,32 +294,48 @@ __global__ __launch_bounds__(BT) void beam_finish_kernel(BeamArgs a) {
   if (threadIdx.x == 0) again = 0;
   __syncthreads();
 
-  BestList best;
-  best.start(lists[wid], num);
+  // one wave chooses: a lane holds 16 kept entries at a time, the first bound
+  // from the lanes' largest
   const uint64_t* kept = a.lists + req * W * P * num;
   const int total = W * P * num;
-  for (int c0 = wid * kWave; c0 < total; c0 += BT) {
-    const int c = c0 + lane;
-    const uint64_t e = c < total ? kept[c] : 0ull;
-    const int w = c < total ? c / (P * num) : 0;
-    const float s = e ? cum[w] + (entry_value(e) - lse[w]) : -INFINITY;
-    best.push(s >= best.admit, s, static_cast<uint32_t>(w) * static_cast<uint32_t>(a.vocab) + entry_index(e));
-  }
-  best.cut();
-  for (int j = best.count + lane; j < kBeamMaxNum; j += kWave) lists[wid][j] = 0ull;
-  __syncthreads();
   if (wid == 0) {
-    uint64_t e[BW];
+    constexpr int H = 16;
+    BestList best;
+    best.start(list, num);
+    const float per = 1.0f / static_cast<float>(P * num);
+    const auto score = [&](int c, uint32_t* at) -> float {
+      const uint64_t e = c < total ? kept[c] : 0ull;
+      // c / (P num): the product may be off by one either way
+      int w = static_cast<int>(static_cast<float>(c) * per);
+      w += (w + 1) * P * num <= c ? 1 : 0;
+      w -= w * P * num > c ? 1 : 0;
+      w = w < W ? w : W - 1;
+      *at = static_cast<uint32_t>(w) * static_cast<uint32_t>(a.vocab) + entry_index(e);
+      return e ? cum[w] + (entry_value(e) - lse[w]) : -INFINITY;
+    };
+    for (int c0 = 0; c0 < total; c0 += H * kWave) {
+      float s[H], mx = -INFINITY;
+      uint32_t at;
 #pragma unroll
-    for (int w = 0; w < BW; ++w) e[w] = lane < kBeamMaxNum ? lists[w][lane] : 0ull;
+      for (int h = 0; h < H; ++h) s[h] = score(c0 + h * kWave + lane, &at);
 #pragma unroll
-    for (int w = 1; w < BW; ++w)
-      best.push(e[w] && entry_value(e[w]) >= best.admit, entry_value(e[w]), entry_index(e[w]));
+      for (int h = 0; h < H; ++h) mx = fmaxf(mx, s[h]);
+      if (c0 == 0) best.base = best.admit = fmaxf(nth_bound(mx, num), -FLT_MAX);
+      uint32_t bits = 0u;
+#pragma unroll
+      for (int h = H - 1; h >= 0; --h) bits = bits + bits + (s[h] >= best.admit ? 1u : 0u);
+      while (__ballot(bits != 0u)) {
+        const int h = bits ? __ffs(bits) - 1 : 0;
+        const float y = score(bits ? c0 + h * kWave + lane : total, &at);
+        best.push(y >= best.admit, y, at);
+        bits &= bits - 1u;
+      }
+    }
     best.cut();
-    for (int j = best.count + lane; j < kBeamMaxNum; j += kWave) lists[0][j] = 0ull;
+    for (int j = best.count + lane; j < kBeamMaxNum; j += kWave) list[j] = 0ull;
   }
   __syncthreads();
-  uint64_t* out = lists[0];
+  uint64_t* out = list;
 
   // A full list whose last entry has the last s taken may have left out
   // equal ones of a lower index.
@@ -359,21 +406,25 @@ __global__ __launch_bounds__(BT) void beam_reorder_kernel(ReorderArgs a) {
   Vec* out = static_cast<Vec*>(st.out) + req * W * st.row + at;
   const bool same = st.in == st.out;
   const int32_t* parents = a.parents + req * a.parent_stride;
-  Vec v[WMAX] = {};
+  // (A row that is not needed, because it stays or there is no such beam, is
+  // replaced by one that is: no branch stands between the loads.)
+  int from[WMAX];
+  int some = 0;
+#pragma unroll
+  for (int i = 0; i < WMAX; ++i) {
+    const int32_t p = parents[i < W ? i : 0];
+    from[i] = i < W ? (p >= 0 && p < W ? p : i) : -1;
+    if (i < W && from[i] != i) some = from[i];
+  }
+  Vec v[WMAX];
+#pragma unroll
+  for (int i = 0; i < WMAX; ++i) {
+    const bool wanted = from[i] >= 0 && !(same && from[i] == i);
+    v[i] = in[(wanted ? from[i] : some) * st.row];
+  }
 #pragma unroll
   for (int i = 0; i < WMAX; ++i)
-    if (i < W) {
-      const int32_t p = parents[i];
-      const int from = p >= 0 && p < W ? p : i;
-      if (!same || from != i) v[i] = in[from * st.row];
-    }
-#pragma unroll
-  for (int i = 0; i < WMAX; ++i)
-    if (i < W) {
-      const int32_t p = parents[i];
-      const int from = p >= 0 && p < W ? p : i;
-      if (!same || from != i) out[i * st.row] = v[i];
-    }
+    if (from[i] >= 0 && !(same && from[i] == i)) out[i * st.row] = v[i];
 }
 
 // ------------------------------------------------------------- launchers ---
