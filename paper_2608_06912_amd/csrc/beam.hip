@@ -6,19 +6,20 @@
 // in float32 at each step; larger s first, equal s by the lowest w V + v.  A
 // continuation whose s is NaN or -inf is none.
 //
-// The logits are read once.  A wave takes a contiguous part of a row, holds
-// its 2048 logits of a step in registers, adds e^{x - R} to its lanes' sums (R the
-// wave's first maximum, moved only when a logit exceeds it by 60, so the sum
-// is hardly ever scaled) and keeps the best `num` logits: what reaches the
-// current num-th best goes to a list of 64 in LDS, which is cut to the best
-// num, by counting, when it is full.  The first threshold is the num-th largest of the
-// lanes' maxima.  The finish has one workgroup per request: lse from the
-// parts, s of the kept, the best num of them.  s is a monotone function of x, but
-// rounding can make it equal for different x (a beam at the lowest float, say), and
-// then the index decides among logits that were not kept; the finish
-// sees that (a full list ends at the last s taken) and looks for them in the logits.
+// beam_scan reads the logits once, as a stream: a wave takes consecutive steps
+// of 2048 logits, adds their exponentials to its lanes' sums and keeps each
+// step's largest logit, no more.  beam_finish, one workgroup per request, has
+// lse from the waves' sums and s of every step's largest.  The num-th largest of
+// those bounds the num-th best continuation from below, so only the steps that reach
+// the bound, little more than num, are read again (they are in the caches), and
+// their continuations that reach it go to lists of 64, cut to the best num by counting.  Nothing that
+// could be chosen is left out before its s is known: where rounding makes s
+// equal for different logits (a beam at the lowest float, say) the index decides.
 //
-// The sums are held in float64: eight terms in float32, then added.
+// e^x is formed as 2^(x log2 e - N), N an integer power that moves only when a logit
+// exceeds it by far, with log2 e in two parts; sums are float64, of eight
+// terms in float32 each.  A row's parts do not depend on its address, so equal
+// rows get equal sums.
 #include "select_common.hpp"
 
 namespace lapsum {
@@ -26,8 +27,10 @@ namespace lapsum {
 namespace {
 constexpr int BT = 256;
 constexpr int BW = BT / kWave;
+constexpr int FT = 1024;            // threads of the finish
+constexpr int FW = FT / kWave;
+constexpr int kFinishSteps = 2048;  // steps the finish looks at together
 constexpr int kList = 64;           // entries of a wave's list
-constexpr float kMove = 60.0f;      // e^60 times 2^31 terms stays below the largest float
 static_assert(kBeamMaxNum * 2 <= kList, "a cut list leaves room");
 
 // Entry: larger value first, then the lower index; 0 is none.
@@ -116,9 +119,8 @@ __device__ __forceinline__ float nth_bound(float mx, int num) {
   return key_value(K);
 }
 
-// The VE elements of a row from `first` on; past the row -inf.  (A row starts at
-// any element: the loads are as wide as they are at any alignment, and a
-// row's parts do not depend on its address, so equal rows get equal sums.)
+// The VE elements of a row from `first` on; past the row -inf.  (A row may start
+// at any element: the loads are as wide at any alignment.)
 template <int DT>
 struct RowVec {
   static constexpr int VE = DT == 0 ? 4 : 8;
@@ -149,235 +151,223 @@ __device__ __forceinline__ void get_vec(const uint32_t (&w)[4], float* x) {
   }
 }
 
-// e^d for d <= kMove to about a float's rounding of d log2(e).
-__device__ __forceinline__ float exp_term(float d) {
-  constexpr float hi = 1.44269502162933349609375f;
-  constexpr float lo = 1.925963033500011e-8f;
-  return exp2_fast(__builtin_fmaf(d, hi, d * lo));
+// A wave's step: 32 logits a lane.
+template <int DT>
+struct Step {
+  static constexpr int VE = RowVec<DT>::VE;
+  static constexpr int U = 32 / VE;   // vectors
+  uint32_t w[U][4];
+  // The first logit of vector u, which lane 0 .. 63 continue.
+  static __device__ __forceinline__ int64_t first(int64_t st, int u) {
+    return ((st * U + u) * kWave + lane_id()) * VE;
+  }
+  __device__ __forceinline__ void fetch(const typename Elem<DT>::raw* row, int64_t st, int64_t V) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) load_vec<DT>(row, first(st, u), V, w[u]);
+  }
+  __device__ __forceinline__ void get(float (&x)[U][VE]) const {
+#pragma unroll
+    for (int u = 0; u < U; ++u) get_vec<DT>(w[u], x[u]);
+  }
+};
+
+// sum of f(x) over the step, eight float32 terms at a time.
+template <int U, int VE, class F>
+__device__ __forceinline__ double step_sum(const float (&x)[U][VE], F&& f) {
+  double sum = 0.0;
+#pragma unroll
+  for (int u = 0; u < U; u += 8 / VE) {
+    float t = 0.0f;
+#pragma unroll
+    for (int q = 0; q < 8 / VE; ++q)
+#pragma unroll
+      for (int j = 0; j < VE; ++j) t += f(x[u + q][j]);
+    sum += static_cast<double>(t);
+  }
+  return sum;
 }
+
+constexpr float kLog2eHi = 1.44269502162933349609375f;
+constexpr float kLog2eLo = 1.925963033500011e-8f;
+constexpr double kLn2 = 0.69314718055994530942;
+constexpr float kMove = 80.0f;          // 2^80 times 2^31 terms stays below the largest float
+constexpr float kFar = 1048576.0f;      // logits past it are referred to the largest itself
 }  // namespace
 
-// grid (parts, rows).  part p of a row: its steps [p per, (p+1) per).
+// grid (parts, rows), a wave a part of `steps` steps.  refs and sums: sum of
+// e^{x - ref} over the part.
 template <int DT>
 __global__ __launch_bounds__(BT) void beam_scan_kernel(BeamArgs a) {
-  using raw = typename Elem<DT>::raw;
-  constexpr int VE = RowVec<DT>::VE;
-  constexpr int U = 32 / VE;   // vectors of a lane and step
-  __shared__ uint64_t lists[BW][kList];
-  __shared__ float refs[BW];
-  __shared__ double sums[BW];
+  using S = Step<DT>;
   const int lane = lane_id();
-  const int wid = threadIdx.x / kWave;
   const int64_t r = blockIdx.y;
-  const raw* row = static_cast<const raw*>(a.logits) + r * a.stride;
-  BestList best;
-  best.start(lists[wid], a.num);
-  float R = -INFINITY;
-  double sum = 0.0;
-  bool first = true;
-  // (a wave's steps are consecutive: later ones hold higher indices)
-  const int64_t s0 = (static_cast<int64_t>(blockIdx.x) * BW + wid) * a.steps;
+  const auto* row = static_cast<const typename Elem<DT>::raw*>(a.logits) + r * a.stride;
+  const int64_t part = static_cast<int64_t>(blockIdx.x) * BW + threadIdx.x / kWave;
+  if (part >= a.parts) return;   // (whole waves; no barrier below)
+  const int64_t s0 = part * a.steps;
   const int64_t s1 = s0 + a.steps < a.row_steps ? s0 + a.steps : a.row_steps;
-  uint32_t next[U][4];   // the next step's logits, under way while one is worked on
-  const auto fetch = [&](int64_t st) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) load_vec<DT>(row, ((st * U + u) * kWave + lane) * VE, a.vocab, next[u]);
-  };
-  if (s0 < s1) fetch(s0);
+  float N = 0.0f, R = 0.0f, kept = -INFINITY;
+  bool have = false, far = false;   // the reference is R where it is far, else N ln 2
+  double ref = 0.0, sum = 0.0;
+  S next;
+  next.fetch(row, s0, a.vocab);
   for (int64_t st = s0; st < s1; ++st) {
-    float x[U][VE];
-    const int64_t at = (st * U * kWave + lane) * VE;   // of u = 0
-#pragma unroll
-    for (int u = 0; u < U; ++u) get_vec<DT>(next[u], x[u]);
-    if (st + 1 < s1) fetch(st + 1);
+    float x[S::U][S::VE];
+    next.get(x);
+    if (st + 1 < s1) next.fetch(row, st + 1, a.vocab);   // under way while this one is worked on
     float mx = -INFINITY;
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int u = 0; u < S::U; ++u)
 #pragma unroll
-      for (int j = 0; j < VE; ++j) mx = fmaxf(mx, x[u][j]);
+      for (int j = 0; j < S::VE; ++j) mx = fmaxf(mx, x[u][j]);
     const float top = wave_max(mx, -INFINITY);
-    if (top > R + kMove) {
-      sum = R == -INFINITY ? 0.0 : sum * exp(static_cast<double>(R) - static_cast<double>(top));
+    const int at = static_cast<int>(st - s0);
+    kept = lane == (at & 63) ? top : kept;
+    if ((at & 63) == 63 || st + 1 == s1) {
+      if (lane <= (at & 63)) a.tops[r * a.row_steps + s0 + (at & ~63) + lane] = kept;
+    }
+    // the reference: the first largest that is no mask, moved where one is far
+    // above it
+    if (!have ? top > -INFINITY : (far ? top > R : top * kLog2eHi > N + kMove)) {
+      const double old = ref;
+      have = true;
+      far = fabsf(top) > kFar;
+      N = rintf(top * kLog2eHi);
       R = top;
+      ref = far ? static_cast<double>(R) : static_cast<double>(N) * kLn2;
+      if (sum != 0.0) sum *= exp(old - ref);
     }
-    const float ref = R == -INFINITY ? 0.0f : R;
-#pragma unroll
-    for (int u = 0; u < U; u += 8 / VE) {
-      float t = 0.0f;
-#pragma unroll
-      for (int q = 0; q < 8 / VE; ++q)
-#pragma unroll
-        for (int j = 0; j < VE; ++j) t += exp_term(x[u + q][j] - ref);
-      sum += static_cast<double>(t);
+    if (!far) {
+      sum += step_sum(x, [&](float y) {
+        return exp2_fast(__builtin_fmaf(y, kLog2eLo, __builtin_fmaf(y, kLog2eHi, -N)));
+      });
+    } else {
+      sum += step_sum(x, [&](float y) { return exp2_fast((y - R) * kLog2eHi); });
     }
-    if (first) {
-      best.base = best.admit = fmaxf(nth_bound(mx, a.num), -FLT_MAX);
-      first = false;
-    }
-    if (__ballot(mx >= best.admit)) {
-      // each lane's wanted logits as bits, then one of each lane at a time (its
-      // value read again: registers have no index)
-      uint32_t bits = 0u;
-#pragma unroll
-      for (int u = U - 1; u >= 0; --u)
-#pragma unroll
-        for (int j = VE - 1; j >= 0; --j) bits = bits + bits + (x[u][j] >= best.admit ? 1u : 0u);
-      while (__ballot(bits != 0u)) {
-        const int q = bits ? __ffs(bits) - 1 : 0;
-        const int64_t v = at + static_cast<int64_t>(q / VE) * (kWave * VE) + q % VE;
-        const float y = bits ? Elem<DT>::get(row[v]) : -INFINITY;
-        best.push(y >= best.admit, y, static_cast<uint32_t>(v));
-        bits &= bits - 1u;
-      }
-    }
-    best.all_later();
   }
-  best.cut();
   sum = wave_sum(sum);
   if (lane == 0) {
-    refs[wid] = R;
-    sums[wid] = sum;
-  }
-  for (int j = best.count + lane; j < kBeamMaxNum; j += kWave) lists[wid][j] = 0ull;
-  __syncthreads();
-  if (wid != 0) return;
-  // one list and one sum for the workgroup
-  uint64_t e[BW];
-#pragma unroll
-  for (int w = 0; w < BW; ++w) e[w] = lane < kBeamMaxNum ? lists[w][lane] : 0ull;
-#pragma unroll
-  for (int w = 1; w < BW; ++w)
-    best.push(e[w] && entry_value(e[w]) >= best.admit, entry_value(e[w]), entry_index(e[w]));
-  best.cut();
-  const int64_t part = r * gridDim.x + blockIdx.x;
-  if (lane < a.num)
-    a.lists[part * a.num + lane] = lane < best.count ? best.buf[lane] : 0ull;
-  if (lane == 0) {
-    float m = refs[0];
-    for (int w = 1; w < BW; ++w) m = fmaxf(m, refs[w]);
-    double t = 0.0;
-    for (int w = 0; w < BW; ++w)
-      if (sums[w] != 0.0)   // (NaN too)
-        t += sums[w] * exp(static_cast<double>(refs[w]) - static_cast<double>(m));
-    a.refs[part] = m;
-    a.sums[part] = t;
+    a.refs[r * a.parts + part] = ref;
+    a.sums[r * a.parts + part] = sum;
   }
 }
 
 // One workgroup per request.
 template <int DT>
-__global__ __launch_bounds__(BT) void beam_finish_kernel(BeamArgs a) {
+__global__ __launch_bounds__(FT) void beam_finish_kernel(BeamArgs a) {
+  using S = Step<DT>;
   using raw = typename Elem<DT>::raw;
-  __shared__ uint64_t list[kList];
+  __shared__ uint64_t lists[FW][kList];
   __shared__ float lse[kBeamMaxBeams];
-  __shared__ int again;
-  __shared__ int wcount[BW];
+  __shared__ uint32_t wanted[kFinishSteps];
+  __shared__ int count;
+  __shared__ float bound;
   const int lane = lane_id();
-  const int wid = threadIdx.x / kWave;
+  const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int64_t req = blockIdx.x;
   const int W = a.beams, P = a.parts, num = a.num;
+  const int steps = static_cast<int>(a.row_steps);
   const float* cum = a.cum + req * W;
-  for (int w = wid; w < W; w += BW) {
+  for (int w = wid; w < W; w += FW) {
     const int64_t o = (req * W + w) * P;
-    float m = -INFINITY;
-    for (int p = lane; p < P; p += kWave) m = fmaxf(m, a.refs[o + p]);
-    m = wave_max(m, -INFINITY);
+    double m = -INFINITY;
+    for (int p = lane; p < P; p += kWave) m = a.sums[o + p] != 0.0 ? fmax(m, a.refs[o + p]) : m;
+    m = wave_max(m, -static_cast<double>(INFINITY));
     double t = 0.0;
     for (int p = lane; p < P; p += kWave) {
       const double s = a.sums[o + p];
-      if (s != 0.0) t += s * exp(static_cast<double>(a.refs[o + p]) - static_cast<double>(m));
+      if (s != 0.0) t += s * exp(a.refs[o + p] - m);   // (NaN too)
     }
     t = wave_sum(t);
-    // (no finite logit: -inf + log 0, and every s is NaN)
-    if (lane == 0) lse[w] = static_cast<float>(static_cast<double>(m) + log(t));
+    // (nothing but masked logits: -inf, and every s is NaN)
+    if (lane == 0) lse[w] = t == 0.0 ? -INFINITY : static_cast<float>(m + log(t));
   }
-  if (threadIdx.x == 0) again = 0;
   __syncthreads();
 
-  // one wave chooses: a lane holds 16 kept entries at a time, the first bound
-  // from the lanes' largest
-  const uint64_t* kept = a.lists + req * W * P * num;
-  const int total = W * P * num;
-  if (wid == 0) {
-    constexpr int H = 16;
-    BestList best;
-    best.start(list, num);
-    const float per = 1.0f / static_cast<float>(P * num);
-    const auto score = [&](int c, uint32_t* at) -> float {
-      const uint64_t e = c < total ? kept[c] : 0ull;
-      // c / (P num): the product may be off by one either way
-      int w = static_cast<int>(static_cast<float>(c) * per);
-      w += (w + 1) * P * num <= c ? 1 : 0;
-      w -= w * P * num > c ? 1 : 0;
-      w = w < W ? w : W - 1;
-      *at = static_cast<uint32_t>(w) * static_cast<uint32_t>(a.vocab) + entry_index(e);
-      return e ? cum[w] + (entry_value(e) - lse[w]) : -INFINITY;
-    };
-    for (int c0 = 0; c0 < total; c0 += H * kWave) {
-      float s[H], mx = -INFINITY;
-      uint32_t at;
-#pragma unroll
-      for (int h = 0; h < H; ++h) s[h] = score(c0 + h * kWave + lane, &at);
-#pragma unroll
-      for (int h = 0; h < H; ++h) mx = fmaxf(mx, s[h]);
-      if (c0 == 0) best.base = best.admit = fmaxf(nth_bound(mx, num), -FLT_MAX);
-      uint32_t bits = 0u;
-#pragma unroll
-      for (int h = H - 1; h >= 0; --h) bits = bits + bits + (s[h] >= best.admit ? 1u : 0u);
-      while (__ballot(bits != 0u)) {
-        const int h = bits ? __ffs(bits) - 1 : 0;
-        const float y = score(bits ? c0 + h * kWave + lane : total, &at);
-        best.push(y >= best.admit, y, at);
-        bits &= bits - 1u;
+  // s of step q's largest logit: steps of one beam after another
+  const float* tops = a.tops + req * W * static_cast<int64_t>(steps);
+  const int total = W * steps;
+  const float inv = 1.0f / static_cast<float>(steps);
+  const auto beam_of = [&](int q) {   // q / steps: the product may be off by one either way
+    int w = static_cast<int>(static_cast<float>(q) * inv);
+    w += w + 1 < W && (w + 1) * steps <= q ? 1 : 0;
+    w -= w * steps > q ? 1 : 0;
+    return w < W ? w : W - 1;
+  };
+  const auto top_score = [&](int q) {
+    const int w = beam_of(q);
+    return cum[w] + (tops[q] - lse[w]);
+  };
+  BestList best;
+  best.start(lists[wid], num);
+  for (int q0 = 0; q0 < total; q0 += kFinishSteps) {
+    const int q1 = total - q0 < kFinishSteps ? total : q0 + kFinishSteps;
+    if (wid == 0) {
+      if (q0 == 0) {
+        float mx = -INFINITY;
+#pragma unroll 8
+        for (int q = q0 + lane; q < q1; q += kWave) mx = fmaxf(mx, top_score(q));
+        const float b = fmaxf(nth_bound(mx, num), -FLT_MAX);
+        if (lane == 0) bound = b;
+        best.base = best.admit = b;
       }
-    }
-    best.cut();
-    for (int j = best.count + lane; j < kBeamMaxNum; j += kWave) list[j] = 0ull;
-  }
-  __syncthreads();
-  uint64_t* out = list;
-
-  // A full list whose last entry has the last s taken may have left out
-  // equal ones of a lower index.
-  const uint64_t last = out[num - 1];
-  if (last) {
-    const float least = entry_value(last);
-    for (int q = threadIdx.x; q < W * P; q += BT) {
-      const uint64_t e = kept[static_cast<int64_t>(q) * num + num - 1];
-      const int w = q / P;
-      if (e && cum[w] + (entry_value(e) - lse[w]) == least) again = 1;
+      int n = 0;   // the steps that reach the bound, in order
+      const float b = best.base;
+#pragma unroll 8
+      for (int q = q0 + lane; q - lane < q1; q += kWave) {
+        const bool is = q < q1 && top_score(q) >= b;
+        const uint64_t mask = __ballot(is);
+        if (is) wanted[n + __popcll(mask & ((1ull << lane) - 1ull))] = static_cast<uint32_t>(q);
+        n += __popcll(mask);
+      }
+      if (lane == 0) count = n;
     }
     __syncthreads();
-    if (again) {
-      // what is above `least` stays; then the lowest indices that equal it
-      int have = 0;
-      while (have < num && entry_value(out[have]) > least) ++have;
-      __syncthreads();
-      for (int w = 0; w < W && have < num; ++w) {
-        const raw* row = static_cast<const raw*>(a.logits) + (req * W + w) * a.stride;
-        for (int64_t v0 = 0; v0 < a.vocab && have < num; v0 += BT) {
-          const int64_t v = v0 + threadIdx.x;
-          const float x = v < a.vocab ? Elem<DT>::get(row[v]) : -INFINITY;
-          const bool is = x > -INFINITY && cum[w] + (x - lse[w]) == least;
-          const uint64_t mask = __ballot(is);
-          if (lane == 0) wcount[wid] = __popcll(mask);
-          __syncthreads();
-          int pos = have + __popcll(mask & ((1ull << lane) - 1ull));
+    if (q0 == 0) best.base = best.admit = bound;
+    const int n = count;
+    for (int i = wid; i < n; i += FW) {
+      const int q = static_cast<int>(wanted[i]);
+      const int w = beam_of(q);
+      const int64_t st = q - w * steps;
+      const raw* row = static_cast<const raw*>(a.logits) + (req * W + w) * a.stride;
+      const float c = cum[w], l = lse[w];
+      const uint32_t base = static_cast<uint32_t>(w) * static_cast<uint32_t>(a.vocab);
+      S step;
+      step.fetch(row, st, a.vocab);
+      float x[S::U][S::VE];
+      step.get(x);
+      // each lane's wanted ones as bits, then one of each lane at a time (its
+      // value read again: registers have no index)
+      uint32_t bits = 0u;
 #pragma unroll
-          for (int q = 0; q < BW; ++q) {
-            if (q < wid) pos += wcount[q];
-            have += wcount[q];
-          }
-          if (is && pos < num)
-            out[pos] = entry(least, static_cast<uint32_t>(w) * static_cast<uint32_t>(a.vocab) + static_cast<uint32_t>(v));
-          __syncthreads();
-        }
+      for (int u = S::U - 1; u >= 0; --u)
+#pragma unroll
+        for (int j = S::VE - 1; j >= 0; --j) bits = bits + bits + (c + (x[u][j] - l) >= best.admit ? 1u : 0u);
+      while (__ballot(bits != 0u)) {
+        const int k = bits ? __ffs(bits) - 1 : 0;
+        const int64_t v = S::first(st, k / S::VE) + k % S::VE;
+        const float s = bits ? c + (Elem<DT>::get(row[v]) - l) : -INFINITY;
+        best.push(s >= best.admit, s, base + static_cast<uint32_t>(v));
+        bits &= bits - 1u;
       }
+      best.all_later();
     }
+    __syncthreads();   // wanted and count have been read
   }
-  if (threadIdx.x < num) {
-    const uint64_t e = out[threadIdx.x];
-    const int64_t o = req * num + threadIdx.x;
+  best.cut();
+  for (int j = best.count + lane; j < kBeamMaxNum; j += kWave) lists[wid][j] = 0ull;
+  __syncthreads();
+  if (wid != 0) return;
+  // the waves' lists, two at a time
+#pragma unroll 1
+  for (int f = 0; f < FW; f += 2) {
+    const uint64_t e = f + lane / 32 == 0 ? 0ull : lists[f + lane / 32][lane % 32];
+    best.push(e && entry_value(e) >= best.admit, entry_value(e), entry_index(e));
+  }
+  best.cut();
+  if (lane < num) {
+    const uint64_t e = lane < best.count ? best.buf[lane] : 0ull;
+    const int64_t o = req * num + lane;
     const uint32_t at = entry_index(e);
     const uint32_t w = at / static_cast<uint32_t>(a.vocab);
     a.scores[o] = e ? entry_value(e) : -INFINITY;
@@ -434,15 +424,15 @@ void beam_plan(int64_t rows, int64_t vocab, int* steps, int64_t* row_steps, int*
   // about 16 waves per compute unit, and at least one step each
   int64_t waves = (256 * 16 + rows - 1) / rows;
   if (waves > n) waves = n;
-  if (waves > kBeamMaxParts * BW) waves = kBeamMaxParts * BW;
+  if (waves > kBeamMaxParts) waves = kBeamMaxParts;
   const int64_t per = (n + waves - 1) / waves;
   *steps = static_cast<int>(per);
   *row_steps = n;
-  *parts = static_cast<int>((n + per * BW - 1) / (per * BW));
+  *parts = static_cast<int>((n + per - 1) / per);
 }
 
 hipError_t launch_beam_select(BeamArgs a, int dtype, hipStream_t s) {
-  const dim3 grid(static_cast<unsigned>(a.parts), static_cast<unsigned>(a.batch * a.beams));
+  const dim3 grid(static_cast<unsigned>((a.parts + BW - 1) / BW), static_cast<unsigned>(a.batch * a.beams));
   { ProfScope ps_("beam_scan", s);
   if (dtype == 0) hipLaunchKernelGGL((beam_scan_kernel<0>), grid, dim3(BT), 0, s, a);
   else if (dtype == 1) hipLaunchKernelGGL((beam_scan_kernel<1>), grid, dim3(BT), 0, s, a);
@@ -451,9 +441,9 @@ hipError_t launch_beam_select(BeamArgs a, int dtype, hipStream_t s) {
   if (e != hipSuccess) return e;
   const dim3 one(static_cast<unsigned>(a.batch));
   { ProfScope ps_("beam_finish", s);
-  if (dtype == 0) hipLaunchKernelGGL((beam_finish_kernel<0>), one, dim3(BT), 0, s, a);
-  else if (dtype == 1) hipLaunchKernelGGL((beam_finish_kernel<1>), one, dim3(BT), 0, s, a);
-  else hipLaunchKernelGGL((beam_finish_kernel<2>), one, dim3(BT), 0, s, a); }
+  if (dtype == 0) hipLaunchKernelGGL((beam_finish_kernel<0>), one, dim3(FT), 0, s, a);
+  else if (dtype == 1) hipLaunchKernelGGL((beam_finish_kernel<1>), one, dim3(FT), 0, s, a);
+  else hipLaunchKernelGGL((beam_finish_kernel<2>), one, dim3(FT), 0, s, a); }
   return hipGetLastError();
 }
 

@@ -424,7 +424,7 @@ hipError_t launch_route_backward(const RouteGradArgs& a, int dtype, hipStream_t 
 // Beam search.
 constexpr int kBeamMaxNum = 32;
 constexpr int kBeamMaxBeams = 32;
-constexpr int kBeamMaxParts = 64;
+constexpr int kBeamMaxParts = 256;   // waves of a row
 struct BeamArgs {
   const void* logits;        // [batch beams] rows of vocab, `stride` apart
   int64_t stride, vocab, batch;
@@ -434,9 +434,8 @@ struct BeamArgs {
   int32_t *tokens, *parents;
   int steps, parts;          // beam_plan
   int64_t row_steps;
-  uint64_t* lists;           // [batch beams][parts][num]
-  float* refs;               // [batch beams][parts]
-  double* sums;
+  float* tops;               // [batch beams][row_steps]
+  double *refs, *sums;       // [batch beams][parts]
 };
 void beam_plan(int64_t rows, int64_t vocab, int* steps, int64_t* row_steps, int* parts);
 hipError_t launch_beam_select(BeamArgs a, int dtype, hipStream_t s);

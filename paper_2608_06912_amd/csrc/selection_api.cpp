@@ -34,14 +34,13 @@ bool valid_route(int dtype, int64_t tokens, int64_t experts, int64_t row_stride,
 }
 
 struct BeamWs {
-  uint64_t* lists;
-  float* refs;
-  double* sums;
+  float* tops;
+  double *refs, *sums;
 };
-BeamWs carve_beam(Carve& c, int64_t rows, int64_t parts, int64_t num) {
+BeamWs carve_beam(Carve& c, int64_t rows, int64_t row_steps, int64_t parts) {
   BeamWs w{};
-  w.lists = c.take<uint64_t>(static_cast<size_t>(rows * parts * num));
-  w.refs = c.take<float>(static_cast<size_t>(rows * parts));
+  w.tops = c.take<float>(static_cast<size_t>(rows * row_steps));
+  w.refs = c.take<double>(static_cast<size_t>(rows * parts));
   w.sums = c.take<double>(static_cast<size_t>(rows * parts));
   return w;
 }
@@ -147,7 +146,7 @@ size_t lapsum_beam_select_workspace_size(int64_t batch, int64_t beams, int64_t v
   int64_t row_steps = 0;
   beam_plan(batch * beams, vocab, &steps, &row_steps, &parts);
   Carve c(nullptr);
-  carve_beam(c, batch * beams, parts, num);
+  carve_beam(c, batch * beams, row_steps, parts);
   return c.size();
 }
 
@@ -178,8 +177,8 @@ int lapsum_beam_select(const void* logits, int dtype, int64_t batch, int64_t bea
   a.parents = parents;
   beam_plan(batch * beams, vocab, &a.steps, &a.row_steps, &a.parts);
   Carve c(workspace);
-  const BeamWs w = carve_beam(c, batch * beams, a.parts, num);
-  a.lists = w.lists;
+  const BeamWs w = carve_beam(c, batch * beams, a.row_steps, a.parts);
+  a.tops = w.tops;
   a.refs = w.refs;
   a.sums = w.sums;
   LAPSUM_TRY(launch_beam_select(a, dtype, stream));

@@ -165,6 +165,47 @@ def test_beam_select_rising_and_extreme_logits(lib):
     assert out[1][0].tolist() == list(range(v - 1, v - 11, -1))
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_beam_select_references_that_move(lib, dtype):
+    """Parts of a row that are masked, far below or far above the rest, at the
+    types' ends, in every order."""
+    import torch
+    v = 12_000
+    big = 6e4 if dtype == "float16" else 3e38
+    x = _logits(9, 12, v, dtype, 1.0)
+    x[0, :5000] = -float("inf")
+    x[0, 5000:] -= 500.0
+    x[1, 4096:] -= 300.0
+    x[2, :4096] -= 300.0
+    x[3, :6000] = -big
+    x[4, 6000:] = -big
+    x[5, 7000] = 300.0
+    x[6, :] = -big
+    x[6, 9000] = -big / 2
+    x[7, 2047:2049] = 200.0
+    x[8, :] = -float("inf")
+    x[8, 11_999] = -700.0
+    x[9, ::2048] += 90.0
+    x[10] *= 1000.0
+    x[11, 100] = big
+    cum = -torch.rand(12, 1, device="cuda")
+    for num in (1, 7, 32):
+        _check(x, cum, num, lib.lapsum_beam_select(x, cum, num))
+
+
+def test_beam_select_of_a_long_row(lib):
+    """Steps of more than one turn of the finish, in several beams."""
+    import torch
+    v = 3_000_001
+    x = _logits(4, 2, v, "bfloat16")
+    cum = torch.tensor([[-1.0, -1.5]], device="cuda")
+    _check(x, cum, 16, lib.lapsum_beam_select(x, cum, 16))
+    flat = torch.zeros(2, v, dtype=torch.bfloat16, device="cuda")
+    flat[1, 2_999_000] = 1.0
+    s, t, p = lib.lapsum_beam_select(flat, torch.zeros(1, 2, device="cuda"), 20)
+    assert t[0].tolist() == [2_999_000, *range(19)] and p[0].tolist() == [1] + [0] * 19
+
+
 def test_beam_select_under_graph_capture(lib):
     import torch
     x = _logits(3, 8, 10_001, "float16")
