@@ -259,8 +259,10 @@ __global__ __launch_bounds__(FT) void beam_finish_kernel(BeamArgs a) {
   using raw = typename Elem<DT>::raw;
   __shared__ uint64_t lists[FW][kList];
   __shared__ float lse[kBeamMaxBeams];
+  __shared__ uint64_t merged[FW * kBeamMaxNum];
+  __shared__ float score[kFinishSteps];
   __shared__ uint32_t wanted[kFinishSteps];
-  __shared__ int count;
+  __shared__ int count, counts[FW];
   __shared__ float bound;
   const int lane = lane_id();
   const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -294,30 +296,30 @@ __global__ __launch_bounds__(FT) void beam_finish_kernel(BeamArgs a) {
     w -= w * steps > q ? 1 : 0;
     return w < W ? w : W - 1;
   };
-  const auto top_score = [&](int q) {
-    const int w = beam_of(q);
-    return cum[w] + (tops[q] - lse[w]);
-  };
   BestList best;
   best.start(lists[wid], num);
   for (int q0 = 0; q0 < total; q0 += kFinishSteps) {
     const int q1 = total - q0 < kFinishSteps ? total : q0 + kFinishSteps;
+    for (int q = q0 + threadIdx.x; q < q1; q += FT) {
+      const int w = beam_of(q);
+      score[q - q0] = cum[w] + (tops[q] - lse[w]);
+    }
+    __syncthreads();
     if (wid == 0) {
+      const int size = q1 - q0;
       if (q0 == 0) {
         float mx = -INFINITY;
-#pragma unroll 8
-        for (int q = q0 + lane; q < q1; q += kWave) mx = fmaxf(mx, top_score(q));
+        for (int q = lane; q < size; q += kWave) mx = fmaxf(mx, score[q]);
         const float b = fmaxf(nth_bound(mx, num), -FLT_MAX);
         if (lane == 0) bound = b;
         best.base = best.admit = b;
       }
       int n = 0;   // the steps that reach the bound, in order
       const float b = best.base;
-#pragma unroll 8
-      for (int q = q0 + lane; q - lane < q1; q += kWave) {
-        const bool is = q < q1 && top_score(q) >= b;
+      for (int q = lane; q - lane < size; q += kWave) {
+        const bool is = q < size && score[q] >= b;
         const uint64_t mask = __ballot(is);
-        if (is) wanted[n + __popcll(mask & ((1ull << lane) - 1ull))] = static_cast<uint32_t>(q);
+        if (is) wanted[n + __popcll(mask & ((1ull << lane) - 1ull))] = static_cast<uint32_t>(q0 + q);
         n += __popcll(mask);
       }
       if (lane == 0) count = n;
@@ -354,14 +356,23 @@ __global__ __launch_bounds__(FT) void beam_finish_kernel(BeamArgs a) {
     }
     __syncthreads();   // wanted and count have been read
   }
-  best.cut();
-  for (int j = best.count + lane; j < kBeamMaxNum; j += kWave) lists[wid][j] = 0ull;
+  // the waves' lists together, and the best of them
+  if (best.count > num) best.cut();
+  if (lane == 0) counts[wid] = best.count;
+  __syncthreads();
+  int before = 0, all = 0;
+#pragma unroll
+  for (int f = 0; f < FW; ++f) {
+    before += f < wid ? counts[f] : 0;
+    all += counts[f];
+  }
+  wave_lds_sync();   // (this wave's list)
+  if (lane < best.count) merged[before + lane] = best.buf[lane];
   __syncthreads();
   if (wid != 0) return;
-  // the waves' lists, two at a time
-#pragma unroll 1
-  for (int f = 0; f < FW; f += 2) {
-    const uint64_t e = f + lane / 32 == 0 ? 0ull : lists[f + lane / 32][lane % 32];
+  best.start(lists[0], num);
+  for (int j = 0; j < all; j += kWave) {
+    const uint64_t e = j + lane < all ? merged[j + lane] : 0ull;
     best.push(e && entry_value(e) >= best.admit, entry_value(e), entry_index(e));
   }
   best.cut();
