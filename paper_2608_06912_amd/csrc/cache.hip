@@ -19,6 +19,7 @@ namespace lapsum {
 
 namespace {
 constexpr uint32_t kStays = 0xffffffffu;
+constexpr uint32_t kTopKey = 0xff800000u;   // of +inf, the largest of a number
 
 __device__ __forceinline__ uint32_t stay_key(float acc, int32_t pos, int32_t first_old, int sink) {
   if (pos < 0) return 0u;
@@ -32,42 +33,30 @@ struct Wide {
   static constexpr int VE = DT == 0 ? 4 : 8;
 };
 
-// VE weights at p (their own alignment only), those from `live` on as 0.
 template <int DT>
-__device__ __forceinline__ void load_weights(const typename Elem<DT>::raw* __restrict__ p, int live,
-                                             float* x) {
-  constexpr int VE = Wide<DT>::VE;
-  if (live >= VE) {
-    uint32_t w[4];
-    __builtin_memcpy(w, p, 16);
+__device__ __forceinline__ void get_words(const uint32_t (&w)[4], float* x) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      if constexpr (DT == 0) {
-        x[q] = Elem<0>::get(w[q]);
-      } else {
-        x[2 * q] = Elem<DT>::get(w[q] & 0xffffu);
-        x[2 * q + 1] = Elem<DT>::get(w[q] >> 16);
-      }
+  for (int q = 0; q < 4; ++q) {
+    if constexpr (DT == 0) {
+      x[q] = Elem<0>::get(w[q]);
+    } else {
+      x[2 * q] = Elem<DT>::get(w[q] & 0xffffu);
+      x[2 * q + 1] = Elem<DT>::get(w[q] >> 16);
     }
-  } else {
-#pragma unroll
-    for (int j = 0; j < VE; ++j) x[j] = j < live ? Elem<DT>::get(p[j]) : 0.0f;
   }
 }
 }  // namespace
 
 // ------------------------------------------------------------ accumulate ---
 // A workgroup takes 64 VE columns of one (sequence, head); its waves take the
-// rows of weights (query heads x queries) in turn.
-constexpr int AT = 256;
-constexpr int AW = AT / kWave;
-
-template <int DT>
-__global__ __launch_bounds__(AT) void cache_accumulate_kernel(AccumulateArgs a) {
+// rows of weights (query heads x queries) in turn, eight in flight each.
+template <int DT, int T>
+__global__ __launch_bounds__(T) void cache_accumulate_kernel(AccumulateArgs a) {
   using raw = typename Elem<DT>::raw;
   constexpr int VE = Wide<DT>::VE;
-  constexpr int U = 4;   // rows in flight per lane
-  __shared__ double part[AW - 1][kWave][VE + 1];
+  constexpr int W = T / kWave;
+  constexpr int U = 8;
+  __shared__ double part[W - 1][kWave][VE + 1];
   const int lane = lane_id();
   const int wid = threadIdx.x / kWave;
   const int64_t bh = blockIdx.x / a.tiles;
@@ -81,25 +70,39 @@ __global__ __launch_bounds__(AT) void cache_accumulate_kernel(AccumulateArgs a) 
 #pragma unroll
   for (int j = 0; j < VE; ++j) sum[j] = 0.0;
   const raw* base = static_cast<const raw*>(a.weights) + b * a.stride_b + h * a.group * a.stride_h + s;
-  const int64_t rows = a.group * a.queries;
-  if (live > 0) {
-    for (int64_t r0 = wid; r0 < rows; r0 += AW * U) {
-      float x[U][VE];
+  const int rows = static_cast<int>(a.group * a.queries), queries = static_cast<int>(a.queries);
+  // the wave's next row: query q of head g, counted on without a division
+  int g = 0, q = __builtin_amdgcn_readfirstlane(wid);
+  const auto row = [&]() -> const raw* {
+    while (q >= queries && g + 1 < a.group) {
+      q -= queries;
+      ++g;
+    }
+    const raw* p = base + g * a.stride_h + (q < queries ? q : queries - 1) * a.stride_q;
+    q += W;
+    return p;
+  };
+  if (live == VE) {
+    for (int r0 = wid; r0 < rows; r0 += W * U) {
+      uint32_t x[U][4];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int64_t r = r0 + u * AW;
-        if (r < rows) {
-          const int64_t g = r / a.queries, q = r - g * a.queries;
-          load_weights<DT>(base + g * a.stride_h + q * a.stride_q, live, x[u]);
-        } else {
-#pragma unroll
-          for (int j = 0; j < VE; ++j) x[u][j] = 0.0f;
-        }
-      }
+      for (int u = 0; u < U; ++u)   // (past the last row that one again, left out below)
+        __builtin_memcpy(x[u], row(), 16);
 #pragma unroll
       for (int u = 0; u < U; ++u)
+        if (r0 + u * W < rows) {
+          float y[VE];
+          get_words<DT>(x[u], y);
 #pragma unroll
-        for (int j = 0; j < VE; ++j) sum[j] += static_cast<double>(x[u][j]);
+          for (int j = 0; j < VE; ++j) sum[j] += static_cast<double>(y[j]);
+        }
+    }
+  } else if (live > 0) {
+    for (int r = wid; r < rows; r += W) {
+      const raw* p = row();
+#pragma unroll
+      for (int j = 0; j < VE; ++j)
+        if (j < live) sum[j] += static_cast<double>(Elem<DT>::get(p[j]));
     }
   }
   if (wid > 0) {
@@ -115,7 +118,7 @@ __global__ __launch_bounds__(AT) void cache_accumulate_kernel(AccumulateArgs a) 
     if (s + j >= a.keys) continue;
     double t = sum[j];
 #pragma unroll
-    for (int w = 0; w < AW - 1; ++w) t += part[w][lane][j];
+    for (int w = 0; w < W - 1; ++w) t += part[w][lane][j];
     if (old) {
       const float o = old[j];
       acc[j] = j < live ? static_cast<float>(static_cast<double>(o) + t) : o;
@@ -407,84 +410,85 @@ __global__ __launch_bounds__(ET) void cache_select_long_kernel(EvictArgs a) {
     const double total = row.pos ? static_cast<double>(n) * got / kEvictSample : n - always;
     const double share = total > a.budget - always ? (a.budget - always) / total : 1.0;
     const double mid = share * got, dev = kEvictSigmas * sqrt(got * (share * (1.0 - share))) + 2.0;
-    uint32_t wlo = 0u, whi = kStays - 1u;   // window of keys, both ends in it
+    uint32_t wlo = 0u, whi = kTopKey;   // window of keys, both ends in it
+    // (a list that holds all that stays as well needs no upper end)
+    const bool top = mid - dev >= 1.0 && (mid + dev) * (static_cast<double>(n) / kEvictSample) > 0.9 * kEvictList;
+    const bool bottom = mid + dev <= got;
     if (got > 0u) {
+      // ends rounded outwards to a bin: about two entries of the sample
       const int shift = block.shift_of(lo, hi);
       sample([&](uint32_t v) {
         if (v != 0u) atomicAdd(&sm.bins[0][(v - lo) >> shift], 1u);
-        if (v != 0u) atomicAdd(&sm.bins[1][(v - lo) >> shift], 1u);
+        if (v != 0u && top) atomicAdd(&sm.bins[1][(v - lo) >> shift], 1u);
       });
       __syncthreads();
-      const bool top = mid - dev >= 1.0, bottom = mid + dev <= got;
-      const uint32_t r1 = top ? static_cast<uint32_t>(mid - dev) : 1u;
-      const uint32_t r2 = bottom ? static_cast<uint32_t>(mid + dev) : got;
-      uint32_t b1, b2, above1, above2, f1, f2, unused;
-      block.find_bin(0, r1, &b1, &above1);
-      block.find_bin(1, r2, &b2, &above2);
-      // the same once more inside the two bins
-      const uint32_t lo1 = lo + (b1 << shift), lo2 = lo + (b2 << shift);
-      const int fine = shift > 11 ? shift - 11 : 0;
-      sample([&](uint32_t v) {
-        if (v != 0u && (v - lo) >> shift == b1) atomicAdd(&sm.bins[0][(v - lo1) >> fine], 1u);
-        if (v != 0u && (v - lo) >> shift == b2) atomicAdd(&sm.bins[1][(v - lo2) >> fine], 1u);
-      });
-      __syncthreads();
-      block.find_bin(0, r1 - above1, &f1, &unused);
-      block.find_bin(1, r2 - above2, &f2, &unused);
-      if (top) whi = lo1 + (f1 << fine) + ((1u << fine) - 1u);
-      if (bottom) wlo = lo2 + (f2 << fine);
+      uint32_t bin, unused;
+      block.find_bin(0, bottom ? static_cast<uint32_t>(mid + dev) : got, &bin, &unused);
+      if (bottom) wlo = lo + (bin << shift);
+      if (top) {
+        block.find_bin(1, static_cast<uint32_t>(mid - dev), &bin, &unused);
+        whi = lo + (bin << shift) + ((1u << shift) - 1u);
+        whi = whi < kTopKey ? whi : kTopKey;
+      }
     }
     // 2. one pass: what is above the window stays, what is in it is marked.
     // As floats; NaN (key 1) is below every window but an open one.
     const bool open = wlo <= 1u;
     const float vlo = open ? -INFINITY : key_value(wlo);
-    const float vhi = whi >= kStays - 1u ? INFINITY : key_value(whi);
+    const float vhi = key_value(whi);
     // One compute unit's instructions bound the pass, so a wave takes 64 words in
     // a row: loads at fixed offsets, two comparisons, and the masks into the
     // lanes of a register.  (Words past the last may be marked.)
     const int w1 = __builtin_amdgcn_readfirstlane(wid);
     const uint32_t end = static_cast<uint32_t>(n - 1);
-    for (int s = w1; s * 64 < words; s += EW) {
-      uint32_t k0 = 0u, k1 = 0u, i0 = 0u, i1 = 0u;
-      const auto mark = [&](const float (&x)[kEvictRound], int b) {
-#pragma unroll
-        for (int u = 0; u < kEvictRound; ++u) {
-          const uint64_t ks = __ballot(x[u] > vhi), ws = __ballot(x[u] >= vlo);
-          const int to = b * kEvictRound + u;
-          k0 = lane == to ? static_cast<uint32_t>(ks) : k0;
-          k1 = lane == to ? static_cast<uint32_t>(ks >> 32) : k1;
-          i0 = lane == to ? static_cast<uint32_t>(ws) : i0;
-          i1 = lane == to ? static_cast<uint32_t>(ws >> 32) : i1;
-        }
-      };
-      constexpr int rounds = 64 / kEvictRound;
-      float x[2][kEvictRound];
-      if (static_cast<int64_t>(s + 1) * 4096 <= n) {
-        const float* from = row.acc + static_cast<int64_t>(s) * 4096 + lane;
-        const auto fetch = [&](float (&y)[kEvictRound], int b) {
-#pragma unroll
-          for (int u = 0; u < kEvictRound; ++u) y[u] = from[(b * kEvictRound + u) * 64];
-        };
-        fetch(x[0], 0);
-#pragma unroll
-        for (int b = 0; b < rounds; ++b) {
-          if (b + 1 < rounds) fetch(x[(b + 1) % 2], b + 1);
-          mark(x[b % 2], b);
-        }
-      } else {
-#pragma unroll 1
-        for (int b = 0; b < rounds; ++b) {
+    const auto pass = [&](auto both) {   // both ends of the window, or the lower alone
+      for (int s = w1; s * 64 < words; s += EW) {
+        uint32_t k0 = 0u, k1 = 0u, i0 = 0u, i1 = 0u;
+        const auto mark = [&](const float (&x)[kEvictRound], int b) {
 #pragma unroll
           for (int u = 0; u < kEvictRound; ++u) {
-            const uint32_t i = static_cast<uint32_t>(s * 64 + b * kEvictRound + u) * 64u + static_cast<uint32_t>(lane);
-            x[0][u] = row.acc[i < end ? i : end];
+            const uint64_t ws = __ballot(x[u] >= vlo);
+            const int to = b * kEvictRound + u;
+            i0 = lane == to ? static_cast<uint32_t>(ws) : i0;
+            i1 = lane == to ? static_cast<uint32_t>(ws >> 32) : i1;
+            if constexpr (decltype(both)::value) {
+              const uint64_t ks = __ballot(x[u] > vhi);
+              k0 = lane == to ? static_cast<uint32_t>(ks) : k0;
+              k1 = lane == to ? static_cast<uint32_t>(ks >> 32) : k1;
+            }
           }
-          mark(x[0], b);
+        };
+        constexpr int rounds = 64 / kEvictRound;
+        float x[2][kEvictRound];
+        if (static_cast<int64_t>(s + 1) * 4096 <= n) {
+          const float* from = row.acc + static_cast<int64_t>(s) * 4096 + lane;
+          const auto fetch = [&](float (&y)[kEvictRound], int b) {
+#pragma unroll
+            for (int u = 0; u < kEvictRound; ++u) y[u] = from[(b * kEvictRound + u) * 64];
+          };
+          fetch(x[0], 0);
+#pragma unroll
+          for (int b = 0; b < rounds; ++b) {
+            if (b + 1 < rounds) fetch(x[(b + 1) % 2], b + 1);
+            mark(x[b % 2], b);
+          }
+        } else {
+#pragma unroll 1
+          for (int b = 0; b < rounds; ++b) {
+#pragma unroll
+            for (int u = 0; u < kEvictRound; ++u) {
+              const uint32_t i = static_cast<uint32_t>(s * 64 + b * kEvictRound + u) * 64u + static_cast<uint32_t>(lane);
+              x[0][u] = row.acc[i < end ? i : end];
+            }
+            mark(x[0], b);
+          }
         }
+        keep[s * 64 + lane] = (static_cast<uint64_t>(k1) << 32) | k0;
+        window[s * 64 + lane] = open ? ~0ull : (static_cast<uint64_t>(i1) << 32) | i0;
       }
-      keep[s * 64 + lane] = (static_cast<uint64_t>(k1) << 32) | k0;
-      window[s * 64 + lane] = open ? ~0ull : (static_cast<uint64_t>(i1) << 32) | i0;
-    }
+    };
+    if (top) pass(std::true_type{});
+    else pass(std::false_type{});
     if (row.pos) __syncthreads();   // (other waves' words)
     if (row.pos)   // by their positions: what always stays, and what is there
       for (int w0 = w1; w0 < words; w0 += EW * kEvictRound) {
@@ -697,6 +701,7 @@ __global__ __launch_bounds__(T) void cache_step_kernel(StepArgs a) {
   using raw = typename Elem<DT>::raw;
   constexpr int NW = T / kWave;
   constexpr int VE = 4;
+  constexpr int U = 8;   // rows of weights in flight
   __shared__ uint64_t least[NW];
   const int tid = threadIdx.x;
   const int64_t bh = blockIdx.x;
@@ -712,8 +717,8 @@ __global__ __launch_bounds__(T) void cache_step_kernel(StepArgs a) {
     float o[VE];
     int32_t p[VE];
     if (live == VE) {
-      __builtin_memcpy(o, acc + s, 16);
-      __builtin_memcpy(p, pos + s, 16);
+      __builtin_memcpy(o, acc + s, sizeof(o));
+      __builtin_memcpy(p, pos + s, sizeof(p));
     } else {
 #pragma unroll
       for (int j = 0; j < VE; ++j) {
@@ -721,19 +726,27 @@ __global__ __launch_bounds__(T) void cache_step_kernel(StepArgs a) {
         p[j] = j < live ? pos[s + j] : -1;
       }
     }
-    double t[VE] = {0.0, 0.0, 0.0, 0.0};
-    for (int64_t g = 0; g < a.group; ++g) {
-      const raw* wp = w + g * a.stride_h + s;
-      if (live == VE) {
-        raw x[VE];
-        __builtin_memcpy(x, wp, sizeof(x));
+    double t[VE] = {};
+    for (int g0 = 0; g0 < a.group; g0 += U) {
+      raw x[U][VE];
 #pragma unroll
-        for (int j = 0; j < VE; ++j) t[j] += static_cast<double>(Elem<DT>::get(x[j]));
-      } else {
+      for (int u = 0; u < U; ++u) {
+        // (past the last head its row again, left out below)
+        const int g = g0 + u < a.group ? g0 + u : static_cast<int>(a.group) - 1;
+        const raw* wp = w + g * a.stride_h + s;
+        if (live == VE) {
+          __builtin_memcpy(x[u], wp, sizeof(x[u]));
+        } else {
 #pragma unroll
-        for (int j = 0; j < VE; ++j)
-          if (j < live) t[j] += static_cast<double>(Elem<DT>::get(wp[j]));
+          for (int j = 0; j < VE; ++j) x[u][j] = j < live ? wp[j] : raw(0);
+        }
       }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (g0 + u < a.group) {
+#pragma unroll
+          for (int j = 0; j < VE; ++j) t[j] += static_cast<double>(Elem<DT>::get(x[u][j]));
+        }
     }
 #pragma unroll
     for (int j = 0; j < VE; ++j) {
@@ -743,7 +756,7 @@ __global__ __launch_bounds__(T) void cache_step_kernel(StepArgs a) {
       if (j < live && k < best) best = k;
     }
     if (live == VE) {
-      __builtin_memcpy(acc + s, o, 16);
+      __builtin_memcpy(acc + s, o, sizeof(o));
     } else {
 #pragma unroll
       for (int j = 0; j < VE; ++j)
@@ -784,10 +797,18 @@ hipError_t launch_cache_accumulate(AccumulateArgs a, int dtype, hipStream_t s) {
   const int64_t cols = kWave * (dtype == 0 ? 4 : 8);
   a.tiles = (a.keys + cols - 1) / cols;
   const dim3 grid(static_cast<unsigned>(a.tiles * a.batch * a.kv));
+  // with fewer workgroups than compute units a workgroup's waves are the only
+  // ones that share the rows: sixteen of them
+  const bool few = a.tiles * a.batch * a.kv < 256 && a.group * a.queries > 32;
   ProfScope ps_("cache_accumulate", s);
-  if (dtype == 0) hipLaunchKernelGGL((cache_accumulate_kernel<0>), grid, dim3(AT), 0, s, a);
-  else if (dtype == 1) hipLaunchKernelGGL((cache_accumulate_kernel<1>), grid, dim3(AT), 0, s, a);
-  else hipLaunchKernelGGL((cache_accumulate_kernel<2>), grid, dim3(AT), 0, s, a);
+  const auto launch = [&](auto dt) {
+    constexpr int DT = decltype(dt)::value;
+    if (few) hipLaunchKernelGGL((cache_accumulate_kernel<DT, 1024>), grid, dim3(1024), 0, s, a);
+    else hipLaunchKernelGGL((cache_accumulate_kernel<DT, 256>), grid, dim3(256), 0, s, a);
+  };
+  if (dtype == 0) launch(std::integral_constant<int, 0>{});
+  else if (dtype == 1) launch(std::integral_constant<int, 1>{});
+  else launch(std::integral_constant<int, 2>{});
   return hipGetLastError();
 }
 
@@ -819,15 +840,16 @@ hipError_t launch_cache_evict(EvictArgs a, int width, hipStream_t s) {
 hipError_t launch_cache_step(const StepArgs& a, int dtype, hipStream_t s) {
   const dim3 grid(static_cast<unsigned>(a.batch * a.kv));
   ProfScope ps_("cache_step", s);
-  if (a.room <= 1024) {
-    if (dtype == 0) hipLaunchKernelGGL((cache_step_kernel<0, 256>), grid, dim3(256), 0, s, a);
-    else if (dtype == 1) hipLaunchKernelGGL((cache_step_kernel<1, 256>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((cache_step_kernel<2, 256>), grid, dim3(256), 0, s, a);
-  } else {
-    if (dtype == 0) hipLaunchKernelGGL((cache_step_kernel<0, 512>), grid, dim3(512), 0, s, a);
-    else if (dtype == 1) hipLaunchKernelGGL((cache_step_kernel<1, 512>), grid, dim3(512), 0, s, a);
-    else hipLaunchKernelGGL((cache_step_kernel<2, 512>), grid, dim3(512), 0, s, a);
-  }
+  const auto launch = [&](auto dt) {
+    constexpr int DT = decltype(dt)::value;
+    // 512 rows of 4096 slots, 8 heads each: 512 threads with eight rows of weights
+    // in flight 11.9 us, 256 threads 14.9, 1024 14.4; eight slots a thread 15.2
+    if (a.room <= 1024) hipLaunchKernelGGL((cache_step_kernel<DT, 256>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((cache_step_kernel<DT, 512>), grid, dim3(512), 0, s, a);
+  };
+  if (dtype == 0) launch(std::integral_constant<int, 0>{});
+  else if (dtype == 1) launch(std::integral_constant<int, 1>{});
+  else launch(std::integral_constant<int, 2>{});
   return hipGetLastError();
 }
 
