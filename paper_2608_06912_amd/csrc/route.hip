@@ -124,7 +124,7 @@ __device__ __forceinline__ void softmax_stats(float (&x)[IT][V], int l, float* m
 template <int LT>
 struct RouteTeam {
   int at[LT];
-  float gscore[64];
+  float gscore[LT];   // (no more groups than lanes)
 };
 
 // Floats from one token's c in LDS to the next (whole 16-byte words).
