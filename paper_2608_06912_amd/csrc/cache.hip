@@ -135,14 +135,14 @@ __global__ __launch_bounds__(T) void cache_accumulate_kernel(AccumulateArgs a) {
 // The key is found digit by digit from histograms in LDS, 2048 bins over the
 // range that still holds it (the keys of positive sums are spread like their
 // logarithms, so few share a bin).  Rows of up to 32768 slots keep their keys in
-// registers.  A longer row is read once: 4096 of its entries give a window that
+// registers.  A longer row is read once: 8192 of its entries give a window that
 // holds the last kept value, one pass marks what is above it and what is in it, as
 // bits in LDS, and only the window's entries (a few percent) are looked at again.  What
 // that does not settle (a window that misses, or too many equal values in it)
 // takes a pass over the row per digit.
 constexpr int kEvictBins = 2048;
-constexpr int kEvictSample = 4096;
-constexpr int kEvictList = 8192;             // entries of the window
+constexpr int kEvictSample = 8192;
+constexpr int kEvictList = 12288;            // entries of the window
 constexpr int kEvictWords = 4096;            // 64 slots each
 constexpr int kEvictRound = 16;              // loads in flight per lane
 constexpr double kEvictSigmas = 4.0;
@@ -376,7 +376,6 @@ constexpr int EW = ET / kWave;
 __global__ __launch_bounds__(ET) void cache_select_long_kernel(EvictArgs a) {
   __shared__ EvictSmem<ET> sm;
   __shared__ uint64_t keep[kEvictWords], window[kEvictWords];
-  __shared__ uint32_t list[kEvictList];
   __shared__ int32_t list_at[kEvictList];
   EvictBlock<ET> block{sm};
   const int tid = threadIdx.x, lane = lane_id(), wid = tid / kWave;
