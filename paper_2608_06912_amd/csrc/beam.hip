@@ -340,6 +340,15 @@ __global__ __launch_bounds__(FT) void beam_finish_kernel(BeamArgs a) {
       step.get(x);
       // each lane's wanted ones as bits, then one of each lane at a time (its
       // value read again: registers have no index)
+      if (total < 2 * num && best.count < num) {
+        // so few steps bound little: the num-th largest of this one's lanes
+        float mx = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < S::U; ++u)
+#pragma unroll
+          for (int j = 0; j < S::VE; ++j) mx = fmaxf(mx, c + (x[u][j] - l));
+        best.base = best.admit = fmaxf(best.base, nth_bound(mx, num));
+      }
       uint32_t bits = 0u;
 #pragma unroll
       for (int u = S::U - 1; u >= 0; --u)
