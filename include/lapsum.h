@@ -534,7 +534,7 @@ int lapsum_beam_reorder(const lapsum_beam_state* states, int64_t count,
  * lapsum_cache_accumulate: acc[b, h, s] = (acc_in[b, h, s], or 0) + the sum of
  * the weights w[b, h G + g, q, s] over the G = heads / kv_heads query heads that share
  * h and all queries q, for s < seen[b]; formed in float64 and rounded once.
- * Columns from seen[b] on are not read: they keep acc_in, or get 0.
+ * Columns from seen[b] on take no part: they keep acc_in, or get 0.
  *   weights   [batch, heads, queries] rows of `keys` elements by three strides
  *   seen      [batch] int32, or NULL (all of the columns)
  *   acc_in    [batch, kv_heads, keys] float32, or NULL; may be acc

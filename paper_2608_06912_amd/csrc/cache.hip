@@ -49,13 +49,13 @@ __device__ __forceinline__ void get_words(const uint32_t (&w)[4], float* x) {
 
 // ------------------------------------------------------------ accumulate ---
 // A workgroup takes 64 VE columns of one (sequence, head); its waves take the
-// rows of weights (query heads x queries) in turn, eight in flight each.
+// rows of weights (query heads x queries) in turn.
 template <int DT, int T>
 __global__ __launch_bounds__(T) void cache_accumulate_kernel(AccumulateArgs a) {
   using raw = typename Elem<DT>::raw;
   constexpr int VE = Wide<DT>::VE;
   constexpr int W = T / kWave;
-  constexpr int U = 8;
+  constexpr int U = T == 1024 ? 4 : 8;   // rows in flight
   __shared__ double part[W - 1][kWave][VE + 1];
   const int lane = lane_id();
   const int wid = threadIdx.x / kWave;
@@ -82,21 +82,34 @@ __global__ __launch_bounds__(T) void cache_accumulate_kernel(AccumulateArgs a) {
     q += W;
     return p;
   };
-  if (live == VE) {
-    for (int r0 = wid; r0 < rows; r0 += W * U) {
-      uint32_t x[U][4];
+  if (a.keys >= VE) {
+    // A lane at the row's end adds up the row's last VE columns and moves its
+    // sums into place afterwards, and columns that are not seen are added up with the others
+    // and left out: every lane's loads are whole, and none waits for a branch.
+    const int64_t over = s + VE > a.keys ? s + VE - a.keys : 0;
+    if (tile * kWave * VE < seen) {   // (columns of this workgroup are seen)
+      for (int r0 = wid; r0 < rows; r0 += W * U) {
+        uint32_t x[U][4];
 #pragma unroll
-      for (int u = 0; u < U; ++u)   // (past the last row that one again, left out below)
-        __builtin_memcpy(x[u], row(), 16);
+        for (int u = 0; u < U; ++u)   // (past the last row that one again)
+          __builtin_memcpy(x[u], row() - over, 16);
+        const int in = (rows - r0 + W - 1) / W;   // of the U, rows there are
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (r0 + u * W < rows) {
+        for (int u = 0; u < U; ++u) {
           float y[VE];
           get_words<DT>(x[u], y);
+          const bool is = u < in;
 #pragma unroll
-          for (int j = 0; j < VE; ++j) sum[j] += static_cast<double>(y[j]);
+          for (int j = 0; j < VE; ++j) sum[j] += static_cast<double>(is ? y[j] : 0.0f);
         }
+      }
     }
+    const int back = over < VE ? static_cast<int>(over) : 0;
+#pragma unroll
+    for (int d = 1; d < VE; d *= 2)   // sum[j] <- sum[j + back]
+#pragma unroll
+      for (int j = 0; j < VE; ++j)
+        if (back & d) sum[j] = sum[j + d < VE ? j + d : j];
   } else if (live > 0) {
     for (int r = wid; r < rows; r += W) {
       const raw* p = row();
