@@ -9,17 +9,25 @@
 // beam_scan reads the logits once, as a stream: a wave takes consecutive steps
 // of 2048 logits, adds their exponentials to its lanes' sums and keeps each
 // step's largest logit, no more.  beam_finish, one workgroup per request, has
-// lse from the waves' sums and s of every step's largest.  The num-th largest of
-// those bounds the num-th best continuation from below, so only the steps that reach
-// the bound, little more than num, are read again (they are in the caches), and
-// their continuations that reach it go to lists of 64, cut to the best num by counting.  Nothing that
-// could be chosen is left out before its s is known: where rounding makes s
-// equal for different logits (a beam at the lowest float, say) the index decides.
+// lse from the waves' sums and s of every step's largest.  The num-th largest
+// of those bounds the num-th best continuation from below, so only the steps
+// that reach the bound, little more than num, are read again (they are in the
+// caches), and their continuations that reach it go to lists of 64, cut to the
+// best num by counting.  Nothing that could be chosen is left out before its s
+// is known: where rounding makes s equal for different logits (a beam at the
+// lowest float, say) the index decides.
 //
-// e^x is formed as 2^(x log2 e - N), N an integer power that moves only when a logit
-// exceeds it by far, with log2 e in two parts; sums are float64, of eight
+// e^x is formed as 2^(x log2 e - N), N an integer power that moves only when a
+// logit exceeds it by far, with log2 e in two parts; sums are float64, of eight
 // terms in float32 each.  A row's parts do not depend on its address, so equal
 // rows get equal sums.
+//
+// Bound: the scan by the read of the logits and the vector issue beside it,
+// about even (256 rows of 128000 bfloat16: 21.6 us, 3.0 TB/s; 16.7 on its own,
+// where part of the logits is in the caches).  Lists of the best logits kept in
+// the scan, as a first form had them, took 43: the candidates' steps wait on
+// each other.  The finish is such a chain (lse, bound, the steps' second read,
+// the lists): 12.7 us for 32 requests of 8 beams, 6.5 for one of 4.
 #include "select_common.hpp"
 
 namespace lapsum {
@@ -93,8 +101,8 @@ struct BestList {
       pred = pred && v >= admit;
     }
   }
-  // All that follows has a higher index: what equals the num-th best is not
-  // wanted any more.
+  // All that follows has a higher index: what equals the num-th best is not wanted
+  // any more.
   __device__ __forceinline__ void all_later() {
     if (count >= num) admit = next_up(base);
   }
@@ -119,8 +127,8 @@ __device__ __forceinline__ float nth_bound(float mx, int num) {
   return key_value(K);
 }
 
-// The VE elements of a row from `first` on; past the row -inf.  (A row may start
-// at any element: the loads are as wide at any alignment.)
+// The VE elements of a row from `first` on; past the row -inf.  (A row may
+// start at any element: the loads are as wide at any alignment.)
 template <int DT>
 struct RowVec {
   static constexpr int VE = DT == 0 ? 4 : 8;
@@ -338,8 +346,8 @@ __global__ __launch_bounds__(FT) void beam_finish_kernel(BeamArgs a) {
       step.fetch(row, st, a.vocab);
       float x[S::U][S::VE];
       step.get(x);
-      // each lane's wanted ones as bits, then one of each lane at a time (its
-      // value read again: registers have no index)
+      // each lane's wanted ones as bits, then one of each lane at a time (its value
+      // read again: registers have no index)
       if (total < 2 * num && best.count < num) {
         // so few steps bound little: the num-th largest of this one's lanes
         float mx = -INFINITY;
@@ -397,10 +405,13 @@ __global__ __launch_bounds__(FT) void beam_finish_kernel(BeamArgs a) {
 }
 
 // --------------------------------------------------------------- reorder ---
-// A thread owns a column of 16 bytes (or what the alignment allows) of all of a request's beams:
-// it reads every beam's parent before it writes a beam, so the states may be
-// reordered in place, and a parent of several beams comes from the caches after its
-// first read.
+// A thread owns a column of 16 bytes (or what the alignment allows) of all of a
+// request's beams: it reads every beam's parent before it writes a beam, so the
+// states may be reordered in place, and a parent of several beams comes from
+// the caches after its first read.  Bound: memory.  32 x 8 rows of 258 KiB in
+// two states 37 us (135 MB written, up to as much read), 16 x 4 rows of 517 KiB
+// in eight 77 us (271 MB). A branch around each load took the first from 37 to
+// 73: its registers.
 template <typename Vec, int WMAX>
 __global__ __launch_bounds__(BT) void beam_reorder_kernel(ReorderArgs a) {
   int t = 0;

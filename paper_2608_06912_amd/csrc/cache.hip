@@ -11,8 +11,8 @@
 // A selection compares acc, so it is formed in float64 and rounded once: its
 // value does not depend on the order of the sum.
 //
-// Selection key of an entry (uint32, larger stays longer): empty 0, NaN 1,
-// then the float's order, and the largest for what always stays.
+// Selection key of an entry (uint32, larger stays longer): empty 0, NaN 1, then
+// the float's order, and the largest for what always stays.
 #include "select_common.hpp"
 
 namespace lapsum {
@@ -49,7 +49,11 @@ __device__ __forceinline__ void get_words(const uint32_t (&w)[4], float* x) {
 
 // ------------------------------------------------------------ accumulate ---
 // A workgroup takes 64 VE columns of one (sequence, head); its waves take the
-// rows of weights (query heads x queries) in turn.
+// rows of weights (query heads x queries) in turn.  Bound: the read of the
+// weights (32 heads x 32 queries over 131072 bfloat16: 50 us, 5.4 TB/s; 12 x 53
+// rows of 130789, which start at any element, 29 us); with few columns the
+// latency of the rows in flight (1000 columns, 512 rows: 7 us with sixteen
+// waves, 9 with four).
 template <int DT, int T>
 __global__ __launch_bounds__(T) void cache_accumulate_kernel(AccumulateArgs a) {
   using raw = typename Elem<DT>::raw;
@@ -83,9 +87,10 @@ __global__ __launch_bounds__(T) void cache_accumulate_kernel(AccumulateArgs a) {
     return p;
   };
   if (a.keys >= VE) {
-    // A lane at the row's end adds up the row's last VE columns and moves its
-    // sums into place afterwards, and columns that are not seen are added up with the others
-    // and left out: every lane's loads are whole, and none waits for a branch.
+    // A lane at the row's end adds up the row's last VE columns and moves its sums
+    // into place afterwards, and columns that are not seen are added up with the
+    // others and left out: every lane's loads are whole, and none waits for a
+    // branch.
     const int64_t over = s + VE > a.keys ? s + VE - a.keys : 0;
     if (tile * kWave * VE < seen) {   // (columns of this workgroup are seen)
       for (int r0 = wid; r0 < rows; r0 += W * U) {
@@ -147,12 +152,19 @@ __global__ __launch_bounds__(T) void cache_accumulate_kernel(AccumulateArgs a) {
 //
 // The key is found digit by digit from histograms in LDS, 2048 bins over the
 // range that still holds it (the keys of positive sums are spread like their
-// logarithms, so few share a bin).  Rows of up to 32768 slots keep their keys in
-// registers.  A longer row is read once: 8192 of its entries give a window that
-// holds the last kept value, one pass marks what is above it and what is in it, as
-// bits in LDS, and only the window's entries (a few percent) are looked at again.  What
-// that does not settle (a window that misses, or too many equal values in it)
-// takes a pass over the row per digit.
+// logarithms, so few share a bin).  Rows of up to 32768 slots keep their keys
+// in registers.  A longer row is read once: 8192 of its entries give a window
+// that holds the last kept value, one pass marks what is above it and what is
+// in it, as bits in LDS, and only the window's entries (a few percent) are
+// looked at again.  What that does not settle (a window that misses, or too
+// many equal values in it), and a row past 262144 slots, takes a pass over the
+// row per digit.
+//
+// Bound: one compute unit per row, its barriers and its instructions.  8 rows
+// of 131072, 4096 kept: 34 us (sample and window 5, marking 7.4, list 3, its
+// digits 6, slots 3, the rest loads and launch), 255 where every digit took a
+// pass and the bins were the floats' top bits; half of that row kept 57.  96
+// rows of 6007: 11.4 us; 8 of 1000: 8.4.
 constexpr int kEvictBins = 2048;
 constexpr int kEvictSample = 8192;
 constexpr int kEvictList = 12288;            // entries of the window
@@ -239,8 +251,8 @@ struct EvictBlock {
     *bin = sm.bin[slot];
     *above = sm.above[slot];
   }
-  // The live entries, those that always stay, and the range of the others'
-  // keys, of each(f): f(key) for this thread's.  Once; one barrier.
+  // The live entries, those that always stay, and the range of the others' keys, of
+  // each(f): f(key) for this thread's.  Once; one barrier.
   template <class F>
   __device__ __forceinline__ void look(F&& each, uint32_t* live, uint32_t* stays, uint32_t* lo, uint32_t* hi) {
     uint32_t n = 0u, s = 0u, a = 0xffffffffu, b = 0u;
@@ -293,8 +305,8 @@ struct EvictBlock {
     *key = lo;
     *equal = want;
   }
-  // The last key that stays and how many equal ones do, for `budget` of the
-  // entries of each(f); key 0 and none equal where all of them stay.
+  // The last key that stays and how many equal ones do, for `budget` of the entries
+  // of each(f); key 0 and none equal where all of them stay.
   template <class F>
   __device__ __forceinline__ void last_key(F&& each, uint32_t budget, uint32_t* key, uint32_t* equal) {
     uint32_t live, stays, lo, hi;
@@ -353,8 +365,8 @@ __global__ __launch_bounds__(T) void cache_select_kernel(EvictArgs a) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) f(k[i]);
   }, static_cast<uint32_t>(a.budget), &last, &want);
-  // above the last key in the low half, equal to it in the high half (at most
-  // 32768 of each)
+  // above the last key in the low half, equal to it in the high half (at most 32768
+  // of each)
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const uint64_t gt = __ballot(k[i] > last), eq = __ballot(k[i] == last && k[i] != 0u);
@@ -416,8 +428,8 @@ __global__ __launch_bounds__(ET) void cache_select_long_kernel(EvictArgs a) {
     };
     block.look(sample, &got, &none, &lo, &hi);
     // ranks of its ends in the sample, from the largest: kEvictSigmas standard
-    // deviations of a binomial around the share that stays (of the entries
-    // that do not always stay)
+    // deviations of a binomial around the share that stays (of the entries that do
+    // not always stay)
     const double always = static_cast<double>(a.sink) + static_cast<double>(a.recent);
     const double total = row.pos ? static_cast<double>(n) * got / kEvictSample : n - always;
     const double share = total > a.budget - always ? (a.budget - always) / total : 1.0;
@@ -443,14 +455,14 @@ __global__ __launch_bounds__(ET) void cache_select_long_kernel(EvictArgs a) {
         whi = whi < kTopKey ? whi : kTopKey;
       }
     }
-    // 2. one pass: what is above the window stays, what is in it is marked.
-    // As floats; NaN (key 1) is below every window but an open one.
+    // 2. one pass: what is above the window stays, what is in it is marked. As
+    // floats; NaN (key 1) is below every window but an open one.
     const bool open = wlo <= 1u;
     const float vlo = open ? -INFINITY : key_value(wlo);
     const float vhi = key_value(whi);
-    // One compute unit's instructions bound the pass, so a wave takes 64 words in
-    // a row: loads at fixed offsets, two comparisons, and the masks into the
-    // lanes of a register.  (Words past the last may be marked.)
+    // One compute unit's instructions bound the pass, so a wave takes 64 words in a
+    // row: loads at fixed offsets, two comparisons, and the masks into the lanes of
+    // a register.  (Words past the last may be marked.)
     const int w1 = __builtin_amdgcn_readfirstlane(wid);
     const uint32_t end = static_cast<uint32_t>(n - 1);
     const auto pass = [&](auto both) {   // both ends of the window, or the lower alone
@@ -624,8 +636,8 @@ __global__ __launch_bounds__(ET) void cache_select_long_kernel(EvictArgs a) {
       return;
     }
   }
-  // every digit by a pass over the row, and one more for the slots, a wave's
-  // part of the row consecutive
+  // every digit by a pass over the row, and one more for the slots, a wave's part
+  // of the row consecutive
   __syncthreads();
   block.start();
   uint32_t last, want;
@@ -672,8 +684,9 @@ __global__ __launch_bounds__(ET) void cache_select_long_kernel(EvictArgs a) {
   for (int64_t j = kept + tid; j < a.budget; j += ET) slots[j] = -1;
 }
 
-// Rows of K and V, acc and positions of the kept slots: a team of `team`
-// lanes copies a row of each, in vectors.
+// Rows of K and V, acc and positions of the kept slots: a team of `team` lanes
+// copies a row of each, in vectors.  Bound: memory (96 x 1024 rows of 192
+// bytes, twice: 75 MB in 17 us, 4.4 TB/s; 8 x 4096 of 256 bytes 9.4 us).
 template <typename Vec>
 __global__ __launch_bounds__(256) void cache_gather_kernel(EvictArgs a) {
   const int team = a.team;
@@ -707,7 +720,11 @@ __global__ __launch_bounds__(256) void cache_gather_kernel(EvictArgs a) {
 }
 
 // ------------------------------------------------------------------ step ---
-// One workgroup per (sequence, head).
+// One workgroup per (sequence, head): its row of sums stays in registers
+// between the addition and the choice, so one launch and one pass do both.
+// Bound: the read of the weights where there are many rows (512 of 4096 slots,
+// 8 heads each: 59 MB in 12 to 13 us, 4.7 TB/s), else the launch (8 rows of
+// 2048: 4.8 us).
 template <int DT, int T>
 __global__ __launch_bounds__(T) void cache_step_kernel(StepArgs a) {
   using raw = typename Elem<DT>::raw;
@@ -809,8 +826,8 @@ hipError_t launch_cache_accumulate(AccumulateArgs a, int dtype, hipStream_t s) {
   const int64_t cols = kWave * (dtype == 0 ? 4 : 8);
   a.tiles = (a.keys + cols - 1) / cols;
   const dim3 grid(static_cast<unsigned>(a.tiles * a.batch * a.kv));
-  // with fewer workgroups than compute units a workgroup's waves are the only
-  // ones that share the rows: sixteen of them
+  // with fewer workgroups than compute units a workgroup's waves are the only ones
+  // that share the rows: sixteen of them
   const bool few = a.tiles * a.batch * a.kv < 256 && a.group * a.queries > 32;
   ProfScope ps_("cache_accumulate", s);
   const auto launch = [&](auto dt) {

@@ -49,7 +49,8 @@ auto in_engine(F&& f) -> decltype(f()) {
 }
 
 // A function called from Python: without the GIL, as a ctypes call runs (an
-// allocation or a launch can wait for the device), a failure as the Python error.
+// allocation or a launch can wait for the device), a failure as the Python
+// error.
 template <class R, class... A>
 auto entry(R (*f)(A...)) {
   return [f](A... args) -> R {

@@ -1,6 +1,6 @@
 // Device helpers of the hard selections (routing, beams, cache entries):
-// elements of three types, an order on floats, and lanes that work on one
-// row together.
+// elements of three types, an order on floats, and lanes that work on one row
+// together.
 #pragma once
 
 #include <float.h>

@@ -1,9 +1,9 @@
 // The hard selections' calls in native code: the common case of each (plain
 // tensors of the right type, shape and device) straight to the C ABI, and the
 // autograd node of the routing's weights.  The binding in selection.py does the
-// same through ctypes with 5 to 10 us more host time per call, which is more than
-// the kernels of a single-token step take; whatever a function here does not
-// take (it returns None) goes there, where it is checked and refused.
+// same through ctypes with 5 to 10 us more host time per call, which is more
+// than the kernels of a single-token step take; whatever a function here does
+// not take (it returns None) goes there, where it is checked and refused.
 #include "node.hpp"
 
 #include <torch/csrc/autograd/functions/basic_ops.h>
