@@ -394,7 +394,8 @@ hipError_t launch_write_m_idx(const int32_t* sorted_idx, int64_t m_len, int64_t 
 constexpr int kRouteMaxExperts = 2048;
 constexpr int kRouteMaxTop = 64;
 constexpr int kRouteMaxGroups = 64;
-constexpr int64_t kRouteBlocks = 1536;   // most workgroups of a call: six per compute unit
+constexpr int64_t kRouteBlocks = 1536;    // most workgroups with counts: six per compute unit
+constexpr int64_t kRouteMost = 1 << 20;   // most workgroups else
 struct RouteArgs {
   const void* logits;
   int64_t tokens, stride;

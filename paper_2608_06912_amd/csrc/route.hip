@@ -35,12 +35,14 @@
 // settles what cannot be chosen; the candidates, and rows whose groups are
 // closer than that, get the exact one.
 //
-// Bound: vector issue.  65536 tokens of 256 bfloat16 logits in eight groups, 8
-// chosen: 37 us, and 4.7 for the counts (their bytes take 7.4 at the rate of a
-// copy); about 785 vector instructions for four tokens, 20 us without groups.
-// With the exact score of every logit, and ranks that compare indices too, it
-// took 72.  16 tokens: 4.6 us, one wave's chain of steps. Backward: 32768
-// tokens of 128 float32 logits, dense, 11.4 us (bytes 6.6).
+// Bound: vector issue and the latency between its steps.  65536 tokens of 256
+// bfloat16 logits in eight groups, 8 chosen: 34 us, and 4.7 for the counts
+// (their bytes take 7.4 at the rate of a copy); 675 vector instructions for four
+// tokens, 17 us without groups.  With comparisons counted as such, not as the
+// sign of a difference, and the groups' scores passed through LDS, it took 37
+// (785 instructions); with the exact score of every logit as well 72.  16
+// tokens: 4.4 us, one wave's chain of steps.  Backward: 32768 tokens of 128
+// float32 logits, dense, 10.8 us (bytes 6.6).
 #include "select_common.hpp"
 
 namespace lapsum {
@@ -167,14 +169,30 @@ __device__ __forceinline__ bool group_kept(const RouteArgs& a, const float* crow
       for (int j = q; j < size; j += sub) take(crow[g * size + j]);
     }
   }
-  for (int d = 1; d < sub; d *= 2) {
-    const float o1 = __shfl_xor(t1, d, LT), o2 = __shfl_xor(t2, d, LT);
-    t2 = fmaxf(fminf(t1, o1), fmaxf(t2, o2));
-    t1 = fmaxf(t1, o1);
+  const auto join = [&](float o1, float o2) {
+    t2 = __builtin_amdgcn_fmed3f(t1, o1, max_f32(t2, o2));
+    t1 = max_f32(t1, o1);
+  };
+  if constexpr (LT == 16) {   // pairs, fours, and mirrors of eight and sixteen
+    if (sub > 1) join(row_move<0xb1>(t1), row_move<0xb1>(t2));
+    if (sub > 2) join(row_move<0x4e>(t1), row_move<0x4e>(t2));
+    if (sub > 4) join(row_move<0x141>(t1), row_move<0x141>(t2));
+    if (sub > 8) join(row_move<0x140>(t1), row_move<0x140>(t2));
+  } else {
+    for (int d = 1; d < sub; d *= 2) join(__shfl_xor(t1, d, LT), __shfl_xor(t2, d, LT));
   }
   // (an expert that cannot be chosen adds nothing)
   const float score = a.group_top > 1 && t2 > -INFINITY ? t1 + t2 : t1;
-  if (q == 0 && g < a.groups) gscore[g] = score;
+  const bool speaks = q == 0 && g < a.groups;
+  *score_out = score;
+  if constexpr (LT == 16) {
+    // by score alone; where equal ones do not leave topk_groups, by index too
+    const float s = speaks ? __builtin_amdgcn_fmed3f(score, -FLT_MAX, FLT_MAX) : -FLT_MAX;
+    const bool stays = speaks && row_count_above(s) < a.topk_groups;
+    const uint32_t row = static_cast<uint32_t>(__ballot(stays) >> (threadIdx.x & 48)) & 0xffffu;
+    if (!__any(__popc(row) != a.topk_groups)) return stays;
+  }
+  if (speaks) gscore[g] = score;
   wave_lds_sync();
   int before = 0;
   for (int j = 0; j < a.groups; ++j) {
@@ -182,14 +200,16 @@ __device__ __forceinline__ bool group_kept(const RouteArgs& a, const float* crow
     before += o > score || (o == score && j < g) ? 1 : 0;
   }
   wave_lds_sync();
-  *score_out = score;
-  return q == 0 && g < a.groups && before < a.topk_groups;
+  return speaks && before < a.topk_groups;
 }
 // The bit of expert e's group in the ballot of the lanes that speak for the
 // team's groups.
-__device__ __forceinline__ bool group_bit(const RouteArgs& a, uint64_t stay, int e) {
+template <int LT>
+using lanes_t = std::conditional_t<LT == 16, uint32_t, uint64_t>;
+template <int LT>
+__device__ __forceinline__ bool group_bit(const RouteArgs& a, lanes_t<LT> stay, int e) {
   const int lane = static_cast<int>((static_cast<uint32_t>(e) * a.group_inv) >> 21) << a.sub;
-  return (stay >> (lane & 63)) & 1ull;
+  return (stay >> (lane & (sizeof(stay) * 8 - 1))) & 1u;
 }
 
 // Waves per SIMD that the registers of a lane's values leave room for.
@@ -295,15 +315,18 @@ __global__ __launch_bounds__(BT, route_waves(IT * kPer<DT>)) void route_forward_
         const float out = team_max<LT>(speaks && !kept ? score : -INFINITY);
         slow = __any(!(in - out >= 4.0f * near_margin(in)));
       }
-      const uint64_t stay = LT == 16 ? (all >> (threadIdx.x & 48)) & 0xffffull : all;
+      const lanes_t<LT> stay =
+          static_cast<lanes_t<LT>>(LT == 16 ? (all >> (threadIdx.x & 48)) & 0xffffull : all);
       packed = a.packed != 0;
       if (packed) {
         // the groups that stay, over all of the team: 2^lanes lanes to a group,
         // `part` consecutive experts to a lane
         const int part = a.group_size >> a.lanes;
-        uint64_t rest = stay;   // the speaking lanes, in the order of their groups
+        lanes_t<LT> rest = stay;   // the speaking lanes, in the order of their groups
         for (int j = l >> a.lanes; j > 0; --j) rest &= rest - 1;
-        const int g = rest ? (__ffsll(static_cast<unsigned long long>(rest)) - 1) >> a.sub : 0;
+        const int lane = LT == 16 ? __ffs(static_cast<uint32_t>(rest))
+                                  : __ffsll(static_cast<unsigned long long>(rest));
+        const int g = rest ? (lane - 1) >> a.sub : 0;
         first = g * a.group_size + (l & ((1 << a.lanes) - 1)) * part;
 #pragma unroll
         for (int q = 0; q < IT * V; q += 4) {
@@ -314,7 +337,7 @@ __global__ __launch_bounds__(BT, route_waves(IT * kPer<DT>)) void route_forward_
           for (int v = 0; v < 4 && q + v < IT * V; ++v) c[(q + v) / V][(q + v) % V] = w[v];
         }
       } else {
-        each_item<IT, LT>(c, l, [&](float& y, int e) { y = group_bit(a, stay, e) ? y : -INFINITY; });
+        each_item<IT, LT>(c, l, [&](float& y, int e) { y = group_bit<LT>(a, stay, e) ? y : -INFINITY; });
       }
     }
 
@@ -323,11 +346,8 @@ __global__ __launch_bounds__(BT, route_waves(IT * kPer<DT>)) void route_forward_
     each_item<IT, LT>(c, l, [&](float& y, int) { best = fmaxf(best, y); });
     float bound;
     if constexpr (LT == 16) {
-      int above = 0;
-      each_rotation([&](auto ctl) {
-        above += dpp_move<decltype(ctl)::value>(best, best) > best ? 1 : 0;
-      });
-      bound = team_min<LT>(above < k ? best : INFINITY);
+      const float b = __builtin_amdgcn_fmed3f(best, -FLT_MAX, FLT_MAX);
+      bound = team_min<LT>(row_count_above(b) < k ? b : INFINITY);
     } else {
       const uint32_t key = asc_key(best);
       uint32_t K = 0u;
@@ -345,12 +365,13 @@ __global__ __launch_bounds__(BT, route_waves(IT * kPer<DT>)) void route_forward_
     for (int turn = 0;; ++turn) {
       float b = bound;
       if (SIG && fabsf(b) <= FLT_MAX) b -= near_margin(b);
-      b = fmaxf(b, -FLT_MAX);
-      mine = 0;   // from the last item, in the highest bit, to the first
+      b = minus(__builtin_amdgcn_fmed3f(b, -FLT_MAX, FLT_MAX));
+      // from the last item, in the highest bit, to the first; a bit is clear where
+      // c - b is not below zero
+      uint32_t below[2] = {~0u, ~0u};
 #pragma unroll
-      for (int i = IT - 1; i >= 0; --i)
-#pragma unroll
-        for (int v = V - 1; v >= 0; --v) mine = mine + mine + (c[i][v] >= b ? 1 : 0);
+      for (int q = IT * V - 1; q >= 0; --q) below[q / 32] = push_sign(below[q / 32], c[q / V][q % V] + b);
+      mine = static_cast<mask_t>(~((static_cast<uint64_t>(below[1]) << 32) | below[0]));
       have = IT * V > 32 ? __popcll(mine) : __popc(static_cast<uint32_t>(mine));
       incl = team_incl_add<LT>(have);
       count = team_max<LT>(incl);
@@ -389,16 +410,16 @@ __global__ __launch_bounds__(BT, route_waves(IT * kPer<DT>)) void route_forward_
         crow[e] = exps && y > -INFINITY ? expf(y - m) : y;
       }
       wave_lds_sync();
-      uint64_t stay = ~0ull;
+      lanes_t<LT> stay = 0;
       if (a.groups > 1) {
         float score;
-        stay = __ballot(group_kept<LT>(a, crow, tm.gscore, l, &score));
-        if constexpr (LT == 16) stay >>= threadIdx.x & 48;
+        const uint64_t all = __ballot(group_kept<LT>(a, crow, tm.gscore, l, &score));
+        stay = static_cast<lanes_t<LT>>(LT == 16 ? all >> (threadIdx.x & 48) : all);
       }
 #pragma unroll 1
       for (int e = l; e < E; e += LT) {
         if (exps) crow[e] = clean(Elem<DT>::get(row[e]));
-        if (a.groups > 1 && !group_bit(a, stay, e)) crow[e] = -INFINITY;
+        if (a.groups > 1 && !group_bit<LT>(a, stay, e)) crow[e] = -INFINITY;
       }
       count = 0;
       for (int j = 0; j < k; ++j) {
@@ -428,8 +449,10 @@ __global__ __launch_bounds__(BT, route_waves(IT * kPer<DT>)) void route_forward_
     int rank = 0;
     const auto rank_by = [&](auto key) {
       rank = 0;
-      if constexpr (LT == 16) {
-        each_rotation([&](auto ctl) { rank += dpp_move<decltype(ctl)::value>(key, key) > key ? 1 : 0; });
+      if constexpr (LT == 16 && std::is_same_v<decltype(key), float>) {
+        rank = row_count_above(__builtin_amdgcn_fmed3f(key, -FLT_MAX, FLT_MAX));
+      } else if constexpr (LT == 16) {
+        each_rotation([&](auto ctl) { rank += row_move<decltype(ctl)::value>(key) > key ? 1 : 0; });
       } else {
         for (int j = 0; j < count; ++j) rank += readlane_as(key, j) > key ? 1 : 0;
       }
@@ -475,24 +498,25 @@ __global__ __launch_bounds__(BT, route_waves(IT * kPer<DT>)) void route_forward_
   }
 }
 
-// counts[e] = sum of the workgroups' counts: 32 experts a workgroup.  (Atomics
+// counts[e] = sum of the workgroups' counts: eight experts a workgroup.  (Atomics
 // on the counts themselves would need them cleared first, a launch as this is
 // one.)
 __global__ __launch_bounds__(1024) void route_counts_kernel(const int* __restrict__ parts, int blocks,
                                                             int E, int* __restrict__ counts) {
-  __shared__ int sums[32][33];
-  const int e = blockIdx.x * 32 + threadIdx.x % 32;
-  const int part = threadIdx.x / 32;
+  __shared__ int sums[16][8];
+  const int e = blockIdx.x * 8 + threadIdx.x % 8;
   int s = 0;
   if (e < E) {
-#pragma unroll 8
-    for (int b = part; b < blocks; b += 32) s += parts[static_cast<int64_t>(b) * E + e];
+#pragma unroll 4
+    for (int b = threadIdx.x / 8; b < blocks; b += 128) s += parts[static_cast<int64_t>(b) * E + e];
   }
-  sums[part][threadIdx.x % 32] = s;
+#pragma unroll
+  for (int d = 8; d < kWave; d *= 2) s += __shfl_xor(s, d);
+  if (lane_id() < 8) sums[threadIdx.x / kWave][lane_id()] = s;
   __syncthreads();
-  if (part == 0 && e < E) {
+  if (threadIdx.x < 8 && e < E) {
     int t = 0;
-    for (int q = 0; q < 32; ++q) t += sums[q][threadIdx.x];
+    for (int q = 0; q < 16; ++q) t += sums[q][threadIdx.x];
     counts[e] = t;
   }
 }
@@ -607,11 +631,15 @@ bool by_team(int experts, bool narrow, F&& f) {
   return narrow ? pick(std::integral_constant<int, 16>{}) : pick(std::integral_constant<int, 64>{});
 }
 
-// Workgroups that fit the device together, each with the same number of turns.
-int64_t route_grid(int64_t tokens, bool narrow) {
+// Workgroups, each with the same number of turns: a turn each, so that a compute
+// unit that is done takes the next (65536 tokens: 28.6 us, 32.6 with those that
+// fit the device together), but with counts, which each has to clear, add up and
+// leave to the second kernel, no more than fit (37.4 in all, 38.7 with a turn each).
+int64_t route_grid(int64_t tokens, bool narrow, bool counts) {
   const int64_t per = BT / (narrow ? 16 : 64);
   const int64_t want = (tokens + per - 1) / per;
-  const int64_t turns = (want + kRouteBlocks - 1) / kRouteBlocks;
+  const int64_t most = counts ? kRouteBlocks : kRouteMost;
+  const int64_t turns = (want + most - 1) / most;
   return (want + turns - 1) / turns;
 }
 
@@ -640,12 +668,12 @@ bool backward_type(const RouteGradArgs& a, bool narrow, int64_t grid, hipStream_
 }  // namespace
 
 int64_t route_blocks(int64_t tokens, int experts, int top_k, int groups) {
-  return route_grid(tokens, narrow_team(experts, top_k, groups));
+  return route_grid(tokens, narrow_team(experts, top_k, groups), true);
 }
 
 hipError_t launch_route_forward(RouteArgs a, int dtype, int* parts, hipStream_t s) {
   const bool narrow = narrow_team(a.experts, a.top_k, a.groups);
-  const int64_t grid = route_grid(a.tokens, narrow);
+  const int64_t grid = route_grid(a.tokens, narrow, a.counts != nullptr);
   int* const counts = a.counts;
   if (counts && grid > 1) a.counts = parts;
   const int team = narrow ? 16 : 64;
@@ -671,14 +699,14 @@ hipError_t launch_route_forward(RouteArgs a, int dtype, int* parts, hipStream_t 
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !counts || grid <= 1) return e;
   { ProfScope ps_("route_counts", s);
-  hipLaunchKernelGGL(route_counts_kernel, dim3(static_cast<unsigned>((a.experts + 31) / 32)),
+  hipLaunchKernelGGL(route_counts_kernel, dim3(static_cast<unsigned>((a.experts + 7) / 8)),
                      dim3(1024), 0, s, parts, static_cast<int>(grid), a.experts, counts); }
   return hipGetLastError();
 }
 
 hipError_t launch_route_backward(const RouteGradArgs& a, int dtype, hipStream_t s) {
   const bool narrow = narrow_team(a.experts, a.top_k, 1);
-  const int64_t grid = route_grid(a.tokens, narrow);
+  const int64_t grid = route_grid(a.tokens, narrow, false);
   bool done;
   { ProfScope ps_("route_backward", s);
   done = dtype == 0 ? backward_type<0>(a, narrow, grid, s)

@@ -70,6 +70,24 @@ __device__ __forceinline__ void wave_lds_sync() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
+// The value of the lane that a control names where every lane has one in its
+// row of 16 (rotations, permutations of four, mirrors): nothing to keep, so
+// that the move becomes part of the operation that reads it.
+template <int CTRL, typename T>
+__device__ __forceinline__ T row_move(T x) {
+  static_assert(sizeof(T) == 4 || sizeof(T) == 8, "32- or 64-bit values");
+  const auto word = [](uint32_t w) {
+    return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(w), CTRL, 0xf, 0xf, true));
+  };
+  if constexpr (sizeof(T) == 4) {
+    return __builtin_bit_cast(T, word(__builtin_bit_cast(uint32_t, x)));
+  } else {
+    const uint64_t b = __builtin_bit_cast(uint64_t, x);
+    return __builtin_bit_cast(T, (static_cast<uint64_t>(word(static_cast<uint32_t>(b >> 32))) << 32) |
+                                     word(static_cast<uint32_t>(b)));
+  }
+}
+
 // f(control) for the 15 rotations of a row of 16 lanes.
 template <class F, int... D>
 __device__ __forceinline__ void each_rotation(F&& f, std::integer_sequence<int, D...>) {
@@ -85,21 +103,47 @@ __device__ __forceinline__ void each_rotation(F&& f) {
 template <int LT, typename T, typename Op>
 __device__ __forceinline__ T team_reduce(T v, Op op) {
   static_assert(LT == 16 || LT == 64, "a row of lanes or a wave");
-  v = op(v, dpp_move<0x128>(v, v));
-  v = op(v, dpp_move<0x124>(v, v));
-  v = op(v, dpp_move<0x122>(v, v));
-  v = op(v, dpp_move<0x121>(v, v));
+  v = op(v, row_move<0x128>(v));
+  v = op(v, row_move<0x124>(v));
+  v = op(v, row_move<0x122>(v));
+  v = op(v, row_move<0x121>(v));
   if constexpr (LT == 64)
     v = op(op(readlane_as(v, 0), readlane_as(v, 16)), op(readlane_as(v, 32), readlane_as(v, 48)));
   return v;
 }
+// (floats as the middle of three, one instruction; no NaN comes here)
+__device__ __forceinline__ float max_f32(float a, float b) { return __builtin_amdgcn_fmed3f(a, b, INFINITY); }
+__device__ __forceinline__ float min_f32(float a, float b) { return __builtin_amdgcn_fmed3f(a, b, -INFINITY); }
 template <int LT, typename T>
 __device__ __forceinline__ T team_max(T v) {
-  return team_reduce<LT>(v, [](T a, T b) { return a > b ? a : b; });
+  if constexpr (std::is_same_v<T, float>) return team_reduce<LT>(v, max_f32);
+  else return team_reduce<LT>(v, [](T a, T b) { return a > b ? a : b; });
 }
 template <int LT, typename T>
 __device__ __forceinline__ T team_min(T v) {
-  return team_reduce<LT>(v, [](T a, T b) { return a < b ? a : b; });
+  if constexpr (std::is_same_v<T, float>) return team_reduce<LT>(v, min_f32);
+  else return team_reduce<LT>(v, [](T a, T b) { return a < b ? a : b; });
+}
+// bits, with the sign of f for a new lowest bit.
+__device__ __forceinline__ uint32_t push_sign(uint32_t bits, float f) {
+  return __builtin_amdgcn_alignbit(bits, __float_as_uint(f), 31);
+}
+// 0 - x, +0 for both zeros; the sum it goes into is not to be made a difference
+// with x, whose sign is another for zeros.
+__device__ __forceinline__ float minus(float x) {
+  float y = 0.0f - x;
+  asm("" : "+v"(y));
+  return y;
+}
+// How many of the row's 16 lanes hold a larger value than this one.  The values
+// are finite, so that the sign of a difference is the comparison (a
+// difference of zeros is +0); one instruction subtracts and one
+// keeps the sign, where a comparison and its count take three.
+__device__ __forceinline__ int row_count_above(float x) {
+  const float neg = minus(x);
+  uint32_t bits = 0u;
+  each_rotation([&](auto ctl) { bits = push_sign(bits, x + row_move<decltype(ctl)::value>(neg)); });
+  return __popc(bits);
 }
 template <int LT, typename T>
 __device__ __forceinline__ T team_sum(T v) {

@@ -105,6 +105,31 @@ def test_route_ties_go_to_the_lowest_index(lib, experts, score):
                 assert idx[t].tolist() == S.best(_np64(x[t]), k)
 
 
+@pytest.mark.parametrize("experts", [8, 64, 256, 320, 704])
+@pytest.mark.parametrize("groups", [1, 8])
+def test_route_zeros_of_both_signs_are_equal(lib, experts, groups):
+    """Zeros the largest logits, and so the largest groups, a few or many of
+    them; and the largest finite values next to infinity."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(experts + groups)
+    rand = lambda: torch.rand(48, experts, generator=gen, device="cuda")
+    x = -torch.rand(48, experts, generator=gen, device="cuda")
+    share = torch.linspace(0.02, 1.0, 48, device="cuda")[:, None]
+    zero = torch.where(rand() < 0.5, 0.0, -0.0)
+    big = torch.where(rand() < 0.5, float("inf"), 3.4028234663852886e38)
+    for top in (zero, big, -big):
+        y = torch.where(rand() < share, top, x)
+        for k in (1, 4, 8):
+            kept = max(1, groups // 2)
+            if k > kept * (experts // groups):
+                continue
+            _, idx = lib.lapsum_route_forward(y, k, groups=groups, topk_groups=kept)
+            for t in range(y.shape[0]):
+                c = S.route_values(S.clean_logits(_np64(y[t])), "softmax", None, groups, kept, 1)
+                ref = S.best(c, k)
+                assert idx[t].tolist() == ref + [-1] * (k - len(ref)), (t, k)
+
+
 @pytest.mark.parametrize("experts", [6, 64, 160, 800])
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 @pytest.mark.parametrize("dtype", DTYPES)
