@@ -188,7 +188,8 @@ __device__ __forceinline__ bool group_kept(const RouteArgs& a, const float* crow
   if constexpr (LT == 16) {
     // by score alone; where equal ones do not leave topk_groups, by index too
     const float s = speaks ? __builtin_amdgcn_fmed3f(score, -FLT_MAX, FLT_MAX) : -FLT_MAX;
-    const bool stays = speaks && row_count_above(s) < a.topk_groups;
+    const int above = row_count_above(s);   // (of every lane: the others' values come from it)
+    const bool stays = speaks && above < a.topk_groups;
     const uint32_t row = static_cast<uint32_t>(__ballot(stays) >> (threadIdx.x & 48)) & 0xffffu;
     if (!__any(__popc(row) != a.topk_groups)) return stays;
   }

@@ -141,8 +141,14 @@ __device__ __forceinline__ float minus(float x) {
 // keeps the sign, where a comparison and its count take three.
 __device__ __forceinline__ int row_count_above(float x) {
   const float neg = minus(x);
+  float d[15];
+  each_rotation([&](auto ctl) { d[decltype(ctl)::value - 0x121] = x + row_move<decltype(ctl)::value>(neg); });
+  asm("" : "+v"(d[0]), "+v"(d[1]), "+v"(d[2]), "+v"(d[3]), "+v"(d[4]));
+  asm("" : "+v"(d[5]), "+v"(d[6]), "+v"(d[7]), "+v"(d[8]), "+v"(d[9]));
+  asm("" : "+v"(d[10]), "+v"(d[11]), "+v"(d[12]), "+v"(d[13]), "+v"(d[14]));
   uint32_t bits = 0u;
-  each_rotation([&](auto ctl) { bits = push_sign(bits, x + row_move<decltype(ctl)::value>(neg)); });
+#pragma unroll
+  for (int i = 0; i < 15; ++i) bits = push_sign(bits, d[i]);
   return __popc(bits);
 }
 template <int LT, typename T>
