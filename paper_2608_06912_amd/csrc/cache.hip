@@ -20,6 +20,7 @@ namespace lapsum {
 namespace {
 constexpr uint32_t kStays = 0xffffffffu;
 constexpr uint32_t kTopKey = 0xff800000u;   // of +inf, the largest of a number
+constexpr uint32_t kLowKey = 0x007fffffu;   // of -inf, the smallest
 
 __device__ __forceinline__ uint32_t stay_key(float acc, int32_t pos, int32_t first_old, int sink) {
   if (pos < 0) return 0u;
@@ -455,6 +456,13 @@ __global__ __launch_bounds__(ET) void cache_select_long_kernel(EvictArgs a) {
         whi = whi < kTopKey ? whi : kTopKey;
       }
     }
+    // Ends that are no number's key (below -inf, and that of a zero's lower
+    // neighbour, which would read -0) go up to the next that is: the comparison of
+    // the values is then that of the keys, so an entry above the window by the one
+    // is above it by the other.
+    if (wlo > 1u && wlo < kLowKey) wlo = kLowKey;
+    if (whi < kLowKey) whi = kLowKey;
+    if (whi == 0x7fffffffu) whi = 0x80000000u;
     // 2. one pass: what is above the window stays, what is in it is marked. As
     // floats; NaN (key 1) is below every window but an open one.
     const bool open = wlo <= 1u;

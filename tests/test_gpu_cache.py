@@ -163,6 +163,42 @@ def test_evict_long_rows_that_a_sample_misleads(lib, slots):
         _check_evict(lib, k, v, acc, seen, budget, sink, recent)
 
 
+def test_evict_long_rows_whose_window_ends_between_numbers(lib):
+    """The last kept entry among NaN ones, below every number, and among the
+    smallest negative numbers, next to zeros: the ends of the sample's bins are
+    then no number's key."""
+    import torch
+    slots = 40_000
+    k, v, _ = _cache(8, 1, 4, slots, 2)
+    gen = torch.Generator(device="cuda").manual_seed(17)
+    order = torch.stack([torch.randperm(slots, generator=gen, device="cuda") for _ in range(4)])
+    seen = torch.tensor([slots], dtype=torch.int32, device="cuda")
+
+    # 12000 entries are there, 9000 of them NaN
+    acc = torch.rand(1, 4, slots, generator=gen, device="cuda")
+    pos = torch.full((1, 4, slots), -1, dtype=torch.int32, device="cuda")
+    for h in range(4):
+        pos[0, h, order[h, :12_000]] = order[h, :12_000].to(torch.int32)
+        acc[0, h, order[h, :9000]] = float("nan")
+    acc[0, 1] = -acc[0, 1]
+    acc[0, 2, order[2, 9000:9100]] = -float("inf")
+    for budget in (11_100, 11_500, 11_990):
+        _check_evict(lib, k, v, acc, seen, budget, 0, 0, pos)
+    _check_evict(lib, k, v, acc, seen, 11_500, 3, 40, pos)
+
+    # a range whose bins, 2^20 keys wide, end at zero
+    low = np.uint32(0xbfffffff).view(np.float32)
+    acc[:] = float(low)
+    for h in range(4):
+        acc[0, h, order[h, 0]] = 1.0
+        acc[0, h, order[h, 1:9000]] = torch.rand(8999, generator=gen, device="cuda")
+        acc[0, h, order[h, 9000:10_000]] = 0.0
+        tiny = torch.randint(1, 1 << 20, (9000,), generator=gen, device="cuda", dtype=torch.int64)
+        acc[0, h, order[h, 10_000:19_000]] = (tiny - (1 << 31)).to(torch.int32).view(torch.float32)
+    for budget in (12_000, 15_000, 18_000):
+        _check_evict(lib, k, v, acc, seen, budget, 0, 0)
+
+
 @pytest.mark.parametrize("slots", [40, 2000, 36_000])
 def test_evict_by_positions(lib, slots):
     """Slots that earlier steps left in any order, with empty ones between."""
