@@ -539,7 +539,7 @@ int lapsum_beam_reorder(const lapsum_beam_state* states, int64_t count,
  *   seen      [batch] int32, or NULL (all of the columns)
  *   acc_in    [batch, kv_heads, keys] float32, or NULL; may be acc
  *   acc       [batch, kv_heads, keys] float32
- * batch, queries and keys may be 0.
+ * batch, queries and keys may be 0; G queries <= 2^30.
  *
  * lapsum_cache_evict: of each (sequence, head) the `budget` entries that stay,
  * copied in the order of their slots.  A sequence has seen positions 0 ..

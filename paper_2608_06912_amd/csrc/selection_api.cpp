@@ -254,6 +254,8 @@ int lapsum_cache_accumulate(const void* weights, int dtype, int64_t batch, int64
       queries < 0 || keys < 0 || !int32_range(keys) || stride_batch < 0 || stride_head < 0 ||
       stride_query < 0)
     return LAPSUM_ERR_INVALID_ARG;
+  // (the rows of one sum are counted in 32 bits)
+  if (queries > (int64_t(1) << 30) / (heads / kv_heads)) return LAPSUM_ERR_INVALID_ARG;
   const bool work = batch > 0 && keys > 0;
   if (work && (!acc || (queries > 0 && !weights))) return LAPSUM_ERR_INVALID_ARG;
   if (work && (kv_heads > kMaxBlocks / batch || batch * kv_heads > kMaxBlocks / ((keys + 255) / 256)))

@@ -158,3 +158,8 @@ def test_the_binding_refuses_host_tensors():
                  lambda: L.lapsum_cache_step(c, c, c, i, c, c, c, i)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_cache_accumulate_refuses_more_rows_than_it_counts(lib):
+    for heads, kv, queries in ((8, 4, 2 ** 29 + 1), (4, 4, 2 ** 31), (4, 1, 2 ** 28 + 1), (2 ** 31, 1, 1)):
+        assert lib.lapsum_cache_accumulate(P, 0, 1, heads, kv, queries, 1, 0, 0, 0, 0, 0, P, None) == INVALID
