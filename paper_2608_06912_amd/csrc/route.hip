@@ -37,7 +37,7 @@
 //
 // Bound: vector issue and the latency between its steps.  65536 tokens of 256
 // bfloat16 logits in eight groups, 8 chosen: 34 us, and 4.7 for the counts
-// (their bytes take 7.4 at the rate of a copy); 675 vector instructions for four
+// (their bytes take 7.4 at the rate of a copy); 670 vector instructions for four
 // tokens, 17 us without groups.  With comparisons counted as such, not as the
 // sign of a difference, and the groups' scores passed through LDS, it took 37
 // (785 instructions); with the exact score of every logit as well 72.  16
