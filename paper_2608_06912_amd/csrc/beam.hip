@@ -17,17 +17,19 @@
 // is known: where rounding makes s equal for different logits (a beam at the
 // lowest float, say) the index decides.
 //
-// e^x is formed as 2^(x log2 e - N), N an integer power that moves only when a
-// logit exceeds it by far, with log2 e in two parts; sums are float64, of eight
-// terms in float32 each.  A row's parts do not depend on its address, so equal
-// rows get equal sums.
+// The choice compares beams by lse, so it is that of the exact sum, rounded once:
+// each e^x is formed in float64, within 2e-12 of itself and the same wherever a
+// row is divided (the parts depend on how many rows there are), and summed in
+// float64 over a power of two that moves only when a logit exceeds it by far.
 //
-// Bound: the scan by the read of the logits and the vector issue beside it,
-// about even (256 rows of 128000 bfloat16: 21.6 us, 3.0 TB/s; 16.7 on its own,
-// where part of the logits is in the caches).  Lists of the best logits kept in
-// the scan, as a first form had them, took 43: the candidates' steps wait on
+// Bound: the scan by vector issue, 16 operations a logit of which 14 are float64
+// (they issue at nearly the rate of float32 ones): 256 rows of 128000 bfloat16
+// 36 us, 1.8 TB/s; 29 where part of the logits is in the caches.  Float32
+// exponentials, eight added in float32 at a time, took 22 and left lse up to
+// 1e-6 off, by another amount for other parts.  Lists of the best logits kept
+// in the scan, as a first form had them, took 43: the candidates' steps wait on
 // each other.  The finish is such a chain (lse, bound, the steps' second read,
-// the lists): 12.7 us for 32 requests of 8 beams, 6.5 for one of 4.
+// the lists): 13 us for 32 requests of 8 beams, 7.0 for one of 4.
 #include "select_common.hpp"
 
 namespace lapsum {
@@ -179,27 +181,32 @@ struct Step {
   }
 };
 
-// sum of f(x) over the step, eight float32 terms at a time.
-template <int U, int VE, class F>
-__device__ __forceinline__ double step_sum(const float (&x)[U][VE], F&& f) {
-  double sum = 0.0;
-#pragma unroll
-  for (int u = 0; u < U; u += 8 / VE) {
-    float t = 0.0f;
-#pragma unroll
-    for (int q = 0; q < 8 / VE; ++q)
-#pragma unroll
-      for (int j = 0; j < VE; ++j) t += f(x[u + q][j]);
-    sum += static_cast<double>(t);
-  }
-  return sum;
+// e^x / 2^N for x from kLow below a reference to kRise above it, N the integer
+// nearest its log2 e: with n the integer nearest x log2 e, 2^(n - N) 2^f, where
+// 2^f = 1 + f q(f) and q interpolates (2^f - 1) / f at eight Chebyshev nodes of
+// [-1/2, 1/2] (relative error of 2^f 2e-12).  shift is 1.5 2^52 - N: the sum
+// with it rounds to an integer and leaves n - N in the low bits.
+constexpr float kRise = 300.0f;
+constexpr float kLow = 600.0f;
+constexpr float kFar = 1073741824.0f;   // from here on a float is 64 above the one before it at least
+constexpr double kShift = 6755399441055744.0;
+constexpr double kLn2 = 0.69314718055994530942;
+__device__ __forceinline__ double exp_by(float x, double shift) {
+  const double y = static_cast<double>(x);
+  const double t = __builtin_fma(y, kLog2e, shift);
+  const double f = __builtin_fma(y, kLog2e, shift - t);
+  double q = 1.325080551750225e-06;
+  q = __builtin_fma(q, f, 1.5303700711365693e-05);
+  q = __builtin_fma(q, f, 1.5403475186530786e-04);
+  q = __builtin_fma(q, f, 1.3333478473685416e-03);
+  q = __builtin_fma(q, f, 9.61812913523614e-03);
+  q = __builtin_fma(q, f, 5.5504109063258665e-02);
+  q = __builtin_fma(q, f, 2.4022650695888503e-01);
+  q = __builtin_fma(q, f, 6.931471805568324e-01);
+  const double p = __builtin_fma(q, f, 1.0);
+  return __hiloint2double(__double2hiint(p) + (__double2loint(t) << 20), __double2loint(p));
 }
 
-constexpr float kLog2eHi = 1.44269502162933349609375f;
-constexpr float kLog2eLo = 1.925963033500011e-8f;
-constexpr double kLn2 = 0.69314718055994530942;
-constexpr float kMove = 80.0f;          // 2^80 times 2^31 terms stays below the largest float
-constexpr float kFar = 1048576.0f;      // logits past it are referred to the largest itself
 }  // namespace
 
 // grid (parts, rows), a wave a part of `steps` steps.  refs and sums: sum of
@@ -214,48 +221,63 @@ __global__ __launch_bounds__(BT) void beam_scan_kernel(BeamArgs a) {
   if (part >= a.parts) return;   // (whole waves; no barrier below)
   const int64_t s0 = part * a.steps;
   const int64_t s1 = s0 + a.steps < a.row_steps ? s0 + a.steps : a.row_steps;
-  float N = 0.0f, R = 0.0f, kept = -INFINITY;
-  bool have = false, far = false;   // the reference is R where it is far, else N ln 2
-  double ref = 0.0, sum = 0.0;
+  float kept = -INFINITY;
+  bool none = false;                // a logit of NaN or +inf
+  bool have = false, far = false;   // a reference, one past kFar
+  float ref = 0.0f;
+  double N = 0.0, sum = 0.0;        // the sum over 2^N, or e^ref where it is far
   S next;
   next.fetch(row, s0, a.vocab);
   for (int64_t st = s0; st < s1; ++st) {
     float x[S::U][S::VE];
     next.get(x);
     if (st + 1 < s1) next.fetch(row, st + 1, a.vocab);   // under way while this one is worked on
-    float mx = -INFINITY;
+    float mx = -INFINITY;   // (NaN where one is)
 #pragma unroll
     for (int u = 0; u < S::U; ++u)
 #pragma unroll
-      for (int j = 0; j < S::VE; ++j) mx = fmaxf(mx, x[u][j]);
+      for (int j = 0; j < S::VE; ++j) mx = __builtin_elementwise_maximum(mx, x[u][j]);
+    none = none || __any(!(mx < INFINITY));
     const float top = wave_max(mx, -INFINITY);
     const int at = static_cast<int>(st - s0);
     kept = lane == (at & 63) ? top : kept;
     if ((at & 63) == 63 || st + 1 == s1) {
       if (lane <= (at & 63)) a.tops[r * a.row_steps + s0 + (at & ~63) + lane] = kept;
     }
-    // the reference: the first largest that is no mask, moved where one is far
-    // above it
-    if (!have ? top > -INFINITY : (far ? top > R : top * kLog2eHi > N + kMove)) {
-      const double old = ref;
+    if (!(top > -INFINITY)) continue;   // (all of it masked)
+    // the reference: the first largest that is no mask, moved where one is far above it
+    if (!have || (far ? top > ref : top - ref > kRise)) {
+      const bool now_far = fabsf(top) >= kFar;
+      const double old = N;
+      N = rint(static_cast<double>(top) * kLog2e);
+      // (what lies 64 below has no weight in a float64 sum)
+      sum = far || now_far ? 0.0 : ldexp(sum, static_cast<int>(fmax(old - N, -4000.0)));
       have = true;
-      far = fabsf(top) > kFar;
-      N = rintf(top * kLog2eHi);
-      R = top;
-      ref = far ? static_cast<double>(R) : static_cast<double>(N) * kLn2;
-      if (sum != 0.0) sum *= exp(old - ref);
+      far = now_far;
+      ref = top;
     }
     if (!far) {
-      sum += step_sum(x, [&](float y) {
-        return exp2_fast(__builtin_fmaf(y, kLog2eLo, __builtin_fmaf(y, kLog2eHi, -N)));
-      });
+      const float low = ref - kLow;
+      const double shift = kShift - N;
+      double t[4] = {};
+#pragma unroll
+      for (int u = 0; u < S::U; ++u)
+#pragma unroll
+        for (int j = 0; j < S::VE; ++j) t[j % 4] += exp_by(__builtin_elementwise_maximum(x[u][j], low), shift);
+      sum += (t[0] + t[1]) + (t[2] + t[3]);
     } else {
-      sum += step_sum(x, [&](float y) { return exp2_fast((y - R) * kLog2eHi); });
+      int same = 0;
+#pragma unroll
+      for (int u = 0; u < S::U; ++u)
+#pragma unroll
+        for (int j = 0; j < S::VE; ++j) same += x[u][j] == ref ? 1 : 0;
+      sum += static_cast<double>(same);
     }
   }
+  if (none) sum = static_cast<double>(NAN);
   sum = wave_sum(sum);
   if (lane == 0) {
-    a.refs[r * a.parts + part] = ref;
+    a.refs[r * a.parts + part] = far ? static_cast<double>(ref) : N * kLn2;
     a.sums[r * a.parts + part] = sum;
   }
 }
