@@ -110,17 +110,29 @@ __device__ __forceinline__ void each_item(float (&x)[IT][V], int l, F&& f) {
 
 // max and sum of e^{x - max} over the team's row; a row without a finite logit
 // has max 0 and sum 0.  NaN and +inf, which make the sum NaN, are cleaned from
-// x first where there are any.
+// x first where there are any.  compared: a selection reads the sum, which is then
+// added up in float64 and rounded once, so that it is the same for every
+// arrangement of the row over lanes.
 template <int IT, int LT, int V>
-__device__ __forceinline__ void softmax_stats(float (&x)[IT][V], int l, float* m_out, float* sum_out) {
+__device__ __forceinline__ void softmax_stats(float (&x)[IT][V], int l, float* m_out, float* sum_out,
+                                              bool compared = false) {
   for (;;) {
     float m = -INFINITY;
     each_item<IT, LT>(x, l, [&](float& y, int) { m = fmaxf(m, y); });
     m = team_max<LT>(m);
     m = m == -INFINITY ? 0.0f : m;
-    float s = 0.0f;
-    each_item<IT, LT>(x, l, [&](float& y, int) { s += expf(y - m); });
-    s = team_sum<LT>(s);
+    float s;
+    if (compared) {
+      double t = 0.0;
+      float most = m;
+      asm volatile("" : "+v"(most));   // (exponentials formed for both ways would take registers)
+      each_item<IT, LT>(x, l, [&](float& y, int) { t += static_cast<double>(expf(y - most)); });
+      s = static_cast<float>(team_sum<LT>(t));
+    } else {
+      s = 0.0f;
+      each_item<IT, LT>(x, l, [&](float& y, int) { s += expf(y - m); });
+      s = team_sum<LT>(s);
+    }
     if (!__any(s != s)) {
       *m_out = m;
       *sum_out = s;
@@ -283,7 +295,7 @@ __global__ __launch_bounds__(BT, route_waves(IT * kPer<DT>)) void route_forward_
           c[i][v] = fmaxf(c[i][v] + bias[(i * LT + l) * V + v], -INFINITY);
     } else {
       each_item<IT, LT>(c, l, [&](float& y, int e) { y = e < E ? clean(y) : -INFINITY; });
-      if (!a.renorm || a.bias || (a.groups > 1 && exps)) softmax_stats<IT, LT>(c, l, &m, &sum);
+      if (!a.renorm || a.bias || (a.groups > 1 && exps)) softmax_stats<IT, LT>(c, l, &m, &sum, !raw_order);
       if (!raw_order) {
 #pragma unroll
         for (int i = 0; i < IT; ++i)
