@@ -60,9 +60,13 @@ __device__ __forceinline__ float sigmoid_f32(float x) { return 1.0f / (1.0f + ex
 // is within kNear of the exact one: the product's, the exponential's, the sum's
 // and the reciprocal's rounding, each weighted by s (1 - s) or s, are below
 // 3e-7 (over all float32, 1.8e-7 at most).  Comparisons of c leave twice that
-// much, and four roundings of c itself.
+// much, and four roundings of c itself.  A group's score of two terms is off by
+// twice kNear and, its terms and their sum each rounded on both sides, 2^-22 of
+// |t1| + |t2|, which can be far above the score where the biases' signs differ; the
+// rest of 4e-7 is for the roundings of the comparison.
 constexpr float kNear = 1e-6f;
 __device__ __forceinline__ float near_margin(float c) { return 2.0f * kNear + 5e-7f * fabsf(c); }
+__device__ __forceinline__ float group_margin(float size) { return 2.0f * kNear + 4e-7f * fminf(size, FLT_MAX); }
 
 // A logit as it counts: NaN is masked, +inf the largest float.
 __device__ __forceinline__ float clean(float x) { return x > -INFINITY ? fminf(x, FLT_MAX) : -INFINITY; }
@@ -155,10 +159,10 @@ constexpr int kRow = IT * LT * kPer<DT> + 4;
 
 // Whether the group that this lane takes part in (2^sub lanes to a group)
 // stays, on the lane that speaks for it, the first of them, from the row's
-// values in LDS; *score_out: the group's score.
+// values in LDS; *score_out: the group's score, *size_out: its terms' sizes added up.
 template <int LT>
 __device__ __forceinline__ bool group_kept(const RouteArgs& a, const float* crow, float* gscore, int l,
-                                           float* score_out) {
+                                           float* score_out, float* size_out) {
   const int sub = 1 << a.sub, size = a.group_size;
   const int g = l >> a.sub, q = l & (sub - 1);
   float t1 = -INFINITY, t2 = -INFINITY;
@@ -194,9 +198,11 @@ __device__ __forceinline__ bool group_kept(const RouteArgs& a, const float* crow
     for (int d = 1; d < sub; d *= 2) join(__shfl_xor(t1, d, LT), __shfl_xor(t2, d, LT));
   }
   // (an expert that cannot be chosen adds nothing)
-  const float score = a.group_top > 1 && t2 > -INFINITY ? t1 + t2 : t1;
+  const bool two = a.group_top > 1 && t2 > -INFINITY;
+  const float score = two ? t1 + t2 : t1;
   const bool speaks = q == 0 && g < a.groups;
   *score_out = score;
+  *size_out = fabsf(t1) + (two ? fabsf(t2) : 0.0f);
   if constexpr (LT == 16) {
     // by score alone; where equal ones do not leave topk_groups, by index too
     const float s = speaks ? __builtin_amdgcn_fmed3f(score, -FLT_MAX, FLT_MAX) : -FLT_MAX;
@@ -317,16 +323,17 @@ __global__ __launch_bounds__(BT, route_waves(IT * kPer<DT>)) void route_forward_
         __builtin_memcpy(crow + (i * LT + l) * V, y, sizeof(y));
       }
       wave_lds_sync();
-      float score;
-      const bool kept = group_kept<LT>(a, crow, tm.gscore, l, &score);
+      float score, size;
+      const bool kept = group_kept<LT>(a, crow, tm.gscore, l, &score, &size);
       const uint64_t all = __ballot(kept);
       if constexpr (SIG) {
-        // approximate scores settle it where the last group that stays and the
-        // first that does not are clearly apart
+        // approximate scores settle it where every group that stays is above every
+        // one that does not by more than the two may be off
         const bool speaks = (l & ((1 << a.sub) - 1)) == 0 && l >> a.sub < a.groups;
-        const float in = team_min<LT>(kept ? score : INFINITY);
-        const float out = team_max<LT>(speaks && !kept ? score : -INFINITY);
-        slow = __any(!(in - out >= 4.0f * near_margin(in)));
+        const float off = group_margin(size);
+        const float in = team_min<LT>(kept ? score - off : INFINITY);
+        const float out = team_max<LT>(speaks && !kept ? score + off : -INFINITY);
+        slow = __any(!(in > out));
       }
       const lanes_t<LT> stay =
           static_cast<lanes_t<LT>>(LT == 16 ? (all >> (threadIdx.x & 48)) & 0xffffull : all);
@@ -425,8 +432,8 @@ __global__ __launch_bounds__(BT, route_waves(IT * kPer<DT>)) void route_forward_
       wave_lds_sync();
       lanes_t<LT> stay = 0;
       if (a.groups > 1) {
-        float score;
-        const uint64_t all = __ballot(group_kept<LT>(a, crow, tm.gscore, l, &score));
+        float score, size;
+        const uint64_t all = __ballot(group_kept<LT>(a, crow, tm.gscore, l, &score, &size));
         stay = static_cast<lanes_t<LT>>(LT == 16 ? all >> (threadIdx.x & 48) : all);
       }
 #pragma unroll 1

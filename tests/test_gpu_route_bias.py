@@ -1,7 +1,9 @@
-"""What the routing compares where a softmax has a bias, to the last bit.
+"""What the routing compares where a bias takes part, to the last bit: the
+softmax's denominator, and groups whose experts' biases have opposite signs.
 
-c = s + bias in float32, from s = e / float32(sum of e) with e = exp(x - max),
-the sum formed in 64 bits.  The bias is large beside the scores, so that c holds few of their
+c = s + bias in float32, from s = e / float32(sum of e) with e = exp(x - max)
+for a softmax (the sum formed in 64 bits), s = 1 / (1 + exp(-x)) for a
+sigmoid.  The bias is large beside the scores, so that c holds few of their
 bits: many experts are equal or a spacing apart, and a bit of s decides."""
 import pytest
 
@@ -53,3 +55,38 @@ def test_softmax_choice_is_that_of_the_rounded_sum(lib, experts, k):
         w, idx = lib.lapsum_route_forward(x, k, bias=bias)
         assert torch.equal(idx.long(), want)
         assert torch.equal(w, s.gather(1, want))
+
+
+@pytest.mark.parametrize("size,masked", [(2, 0), (8, 6), (400, 398)])
+@pytest.mark.parametrize("high", [4.0, 64.0, 1000.0])
+def test_groups_with_biases_of_opposite_signs(lib, size, masked, high):
+    """Two groups, the sum of two experts each, one bias +high and one -high:
+    the sum is small, its terms' spacing is not.  In every row the first
+    group's score is a little below the second's, by less than a spacing, mostly in
+    the same one (the groups are then equal and the first stays), or clearly below."""
+    import torch
+    tokens = 60_000
+    gen = torch.Generator(device="cuda").manual_seed(int(high) + size)
+    # logits whose scores lie just below the middle of two values that c can have
+    step = torch.tensor(high, device="cuda").nextafter(torch.tensor(1e9, device="cuda")) - high
+    cells = torch.randint(int(0.15 / float(step)) + 1, int(0.85 / float(step)) + 2, (tokens,), generator=gen,
+                          device="cuda")
+    middle = (cells.double() + 0.5) * step.double()
+    close = torch.rand(tokens, generator=gen, device="cuda").double() * 4e-7
+    second = torch.logit(middle - close).float()
+    first = torch.logit(middle - 0.25 * step.double()).float()
+    # a row in four is close: tokens that share a wave are not all looked at again
+    second[torch.arange(tokens, device="cuda") % 4 != 1] -= 1.0
+    x = torch.full((tokens, 2, size), -float("inf"), device="cuda")
+    x[:, 0, masked], x[:, 1, masked] = first, second
+    x[:, :, masked + 1] = torch.randn(tokens, 1, generator=gen, device="cuda")
+    bias = torch.zeros(2, size, device="cuda")
+    bias[:, masked], bias[:, masked + 1] = high, -high
+    s = 1.0 / (1.0 + torch.exp(-x))
+    c = (s + bias)[:, :, masked:masked + 2]
+    score = c.sum(-1)
+    stays = (score[:, 1] > score[:, 0]).int()             # the first where they are equal
+    assert 0.05 < float((score[:, 0] == score[:, 1]).float().mean())
+    w, idx = lib.lapsum_route_forward(x.flatten(1), 2, score="sigmoid", bias=bias.flatten(), groups=2,
+                                      topk_groups=1, group_top=2)
+    assert torch.equal(idx[:, 0] // size, stays) and torch.equal(idx[:, 1] // size, stays)
