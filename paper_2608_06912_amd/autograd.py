@@ -302,6 +302,12 @@ def soft_topk(scores, k, alpha, *, path: str = "auto", sample: str = "n23", z: f
 _ROUTE_SCORES = {"softmax": 0, "sigmoid": 1}
 
 
+def _has_tangent(x):
+    """x is a dual tensor of forward-mode AD, whether it requires grad or not."""
+    forward = torch.autograd.forward_ad
+    return forward._current_level >= 0 and forward.unpack_dual(x).tangent is not None
+
+
 class RouteFunction(torch.autograd.Function):
     """The weights of lapsum_route_forward as an autograd node: the gradient
     with respect to the logits, the chosen experts held fixed."""
@@ -333,10 +339,12 @@ def route_topk(logits, top_k: int, *, score: str = "softmax", bias=None, groups:
                scale: float = 1.0, counts: bool = False):
     """The top_k experts of each token and their weights, differentiable in the
     logits (soft_topk trains the choice itself, this its weights).  Arguments
-    and results as lapsum_route_forward: (weights, indices[, counts])."""
+    and results as lapsum_route_forward: (weights, indices[, counts]).  The
+    derivative is that of reverse mode; forward mode is refused."""
     options = {"score": score, "bias": bias, "groups": groups, "topk_groups": topk_groups,
                "group_top": group_top, "renormalise": renormalise, "scale": scale}
-    if torch.is_grad_enabled() and isinstance(logits, torch.Tensor) and logits.requires_grad:
+    if isinstance(logits, torch.Tensor) and (
+            torch.is_grad_enabled() and logits.requires_grad or _has_tangent(logits)):
         node = _node or _load_node()
         if (node and type(logits) in _PLAIN and (bias is None or type(bias) in _PLAIN)
                 and score in _ROUTE_SCORES and _eager()):
