@@ -32,6 +32,14 @@ bool dense(const Tensor& t, at::ScalarType type, const Tensor& like) {
   return plain(t) && t.scalar_type() == type && t.is_contiguous() && t.device() == like.device();
 }
 
+// What a call writes in place: nothing that requires grad in grad mode (the
+// binding says so), and autograd is told afterwards, as after an in-place call of
+// torch's.
+bool may_write(const Tensor& t) { return !(t.requires_grad() && at::GradMode::is_enabled()); }
+void written(const Tensor& t) {
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 // Logits as rows: contiguous, or two dimensions with dense rows.
 struct Rows {
   int64_t rows = 0, n = 0, stride = 0;
@@ -181,7 +189,7 @@ bool beam_reorder(const std::vector<Tensor>& states, const Tensor& parents, std:
   for (size_t i = 0; i < states.size(); ++i) {
     const Tensor &s = states[i], &o = outs[i];
     if (!dense(s, s.scalar_type(), parents) || s.dim() < 1 || s.size(0) != batch * beams ||
-        !dense(o, s.scalar_type(), parents) || o.sizes() != s.sizes())
+        !dense(o, s.scalar_type(), parents) || o.sizes() != s.sizes() || !may_write(o))
       return false;
     const int64_t size = s.element_size(), row = s.numel() / s.size(0) * size;
     items[i] = {s.data_ptr(), o.data_ptr(), row, 1, row, row};
@@ -197,6 +205,7 @@ bool beam_reorder(const std::vector<Tensor>& states, const Tensor& parents, std:
   check(lapsum_beam_reorder(items.data(), static_cast<int64_t>(items.size()), parents.data_ptr<int32_t>(),
                             batch > 1 ? parents.stride(0) : beams, batch, beams, stream_of(parents)),
         "lapsum_beam_reorder");
+  for (const Tensor& o : outs) written(o);
   return true;
 }
 
@@ -206,7 +215,7 @@ OptTensor cache_accumulate(const Tensor& w, int64_t kv, const OptTensor& seen, c
   const int64_t batch = w.size(0), keys = w.size(3);
   if (seen && !(dense(*seen, at::kInt, w) && seen->dim() == 1 && seen->size(0) == batch)) return std::nullopt;
   if (acc && !(dense(*acc, at::kFloat, w) && acc->dim() == 3 && acc->size(0) == batch &&
-               acc->size(1) == kv && acc->size(2) == keys))
+               acc->size(1) == kv && acc->size(2) == keys && may_write(*acc)))
     return std::nullopt;
   const c10::DeviceGuard guard(w.device());
   Tensor out = acc ? *acc : at::empty({batch, kv, keys}, w.options().dtype(at::kFloat).requires_grad(false));
@@ -216,6 +225,7 @@ OptTensor cache_accumulate(const Tensor& w, int64_t kv, const OptTensor& seen, c
                                 acc ? acc->data_ptr<float>() : nullptr, out.data_ptr<float>(),
                                 stream_of(w)),
         "lapsum_cache_accumulate");
+  if (acc) written(out);
   return out;
 }
 
@@ -268,7 +278,8 @@ OptTensor cache_step(const Tensor& weights, const Tensor& k_new, const Tensor& v
   const Cache kc(k, true), vc(v, true);
   if (!kc.ok || !vc.ok || v.sizes() != k.sizes() || v.scalar_type() != k.scalar_type() ||
       v.device() != k.device() || !of_cache(acc, at::kFloat, k) || !of_cache(pos, at::kInt, k) ||
-      !dense(seen, at::kInt, k) || seen.dim() != 1 || seen.size(0) != k.size(0))
+      !dense(seen, at::kInt, k) || seen.dim() != 1 || seen.size(0) != k.size(0) || !may_write(k) ||
+      !may_write(v) || !may_write(acc))
     return std::nullopt;
   const int64_t batch = k.size(0), kv = k.size(1), slots = k.size(2), dim = k.size(3);
   const int64_t wd = weights.dim();
@@ -288,6 +299,7 @@ OptTensor cache_step(const Tensor& weights, const Tensor& k_new, const Tensor& v
                           acc.data_ptr<float>(), pos.data_ptr<int32_t>(), batch, weights.size(1), kv,
                           slots, sink, recent, slot.data_ptr<int32_t>(), stream_of(k)),
         "lapsum_cache_step");
+  for (const Tensor* t : {&k, &v, &acc, &pos}) written(*t);
   return slot;
 }
 

@@ -120,6 +120,17 @@ def _expect(x, name, shape, dtype, device, dense=True):
     return x
 
 
+def _may_write(x, name):
+    """Refuse to write over what autograd would take for unchanged."""
+    if x.requires_grad and _torch().is_grad_enabled():
+        raise RuntimeError(f"{name} requires grad and is written in place, which has no gradient")
+
+
+def _written(*tensors):
+    """Tell autograd, which may have saved them, that these changed."""
+    _torch().autograd.graph.increment_version(tensors)
+
+
 def _count(value, name):
     if int(value) != value:
         raise ValueError(f"{name} must be an integer")
@@ -269,7 +280,8 @@ def lapsum_beam_reorder(states, parents, *, length: int | None = None, out=None)
     on in: row (b, i) <- row (b, parents[b, i]).  length: of states
     [batch * beams, heads, room, dim] (any dimensions before room), move only
     the first `length` of room.  In place, or with `out` (as many tensors of
-    the same shapes) into those.  Returns the tensors written."""
+    the same shapes) into those.  Returns the tensors written, which autograd
+    takes as changed; in grad mode none of them may require grad."""
     states = list(states)
     outs = states if out is None else list(out)
     node = _native or _node()
@@ -300,6 +312,7 @@ def lapsum_beam_reorder(states, parents, *, length: int | None = None, out=None)
         if o is not s and (o.shape != s.shape or o.dtype is not s.dtype or o.device != dev
                            or not o.is_contiguous()):
             raise ValueError("out must be like the states")
+        _may_write(o, "a state" if o is s else "out")
         size = s.element_size()
         row = s.stride(0) * size if s.shape[0] > 1 else s.numel() * size
         item.src, item.dst, item.row_bytes = s.data_ptr(), o.data_ptr(), row
@@ -315,6 +328,7 @@ def lapsum_beam_reorder(states, parents, *, length: int | None = None, out=None)
         _check(lib.lapsum_beam_reorder(ctypes.addressof(array), len(states), _ptr(parents),
                                        parents.stride(0) if batch > 1 else beams, batch, beams,
                                        _stream(dev)), "lapsum_beam_reorder")
+    _written(*outs)
     return outs
 
 
@@ -334,7 +348,8 @@ def lapsum_cache_accumulate(weights, kv_heads: int, *, seen=None, acc=None):
     """Attention weight per cache entry: weights [batch, heads, queries, keys]
     summed over the query heads that share a key head and over the queries, to
     float32 [batch, kv_heads, keys].  seen (int32 [batch]): only the first
-    seen[b] columns of a sequence count.  acc: added to, in place."""
+    seen[b] columns of a sequence count.  acc: added to, in place (in grad mode
+    it may not require grad)."""
     node = _native or _node()
     if node:
         try:
@@ -359,11 +374,14 @@ def lapsum_cache_accumulate(weights, kv_heads: int, *, seen=None, acc=None):
         out = torch.empty((batch, max(kv, 0), keys), dtype=torch.float32, device=dev)
     else:
         out = _expect(acc, "acc", (batch, kv, keys), torch.float32, dev)
+        _may_write(acc, "acc")
     sb, sh, sq, _ = w.stride()
     with _on_device(dev):
         _check(lib.lapsum_cache_accumulate(_ptr(w), code, batch, heads, kv, queries, keys, sb, sh, sq,
                                            _ptr(seen), _ptr(acc), _ptr(out), _stream(dev)),
                "lapsum_cache_accumulate")
+    if acc is not None:
+        _written(acc)
     return out
 
 
@@ -422,7 +440,8 @@ def lapsum_cache_step(weights, k_new, v_new, seen, k, v, acc, pos, *, sink: int 
     then k_new, v_new [batch, kv_heads, dim] (or [batch, kv_heads, 1, dim])
     take the first empty slot (pos -1) or that of the smallest acc outside the
     first `sink` and last `recent` positions, at position seen[b].  Returns the slots, int32
-    [batch, kv_heads].  The caller advances seen."""
+    [batch, kv_heads].  The caller advances seen.  Autograd takes k, v, acc and
+    pos as changed; in grad mode none of them may require grad."""
     node = _native or _node()
     if node:
         try:
@@ -460,6 +479,8 @@ def lapsum_cache_step(weights, k_new, v_new, seen, k, v, acc, pos, *, sink: int 
     _expect(acc, "acc", (batch, kv, slots), torch.float32, dev)
     _expect(pos, "pos", (batch, kv, slots), torch.int32, dev)
     _expect(seen, "seen", (batch,), torch.int32, dev)
+    for name, x in (("k", k), ("v", v), ("acc", acc)):
+        _may_write(x, name)
     slot = torch.empty((batch, kv), dtype=torch.int32, device=dev)
     with _on_device(dev):
         _check(lib.lapsum_cache_step(_ptr(w), code, w.stride(0), w.stride(1), _ptr(rows[0]),
@@ -467,4 +488,5 @@ def lapsum_cache_step(weights, k_new, v_new, seen, k, v, acc, pos, *, sink: int 
                                      dim * k.element_size(), _ptr(acc), _ptr(pos), batch, w.shape[1],
                                      kv, slots, _count(sink, "sink"), _count(recent, "recent"),
                                      _ptr(slot), _stream(dev)), "lapsum_cache_step")
+    _written(k, v, acc, pos)
     return slot
