@@ -501,8 +501,12 @@ int lapsum_route_backward(const float* grad_weights, const void* logits,
  * rows each.  Of a row, the `outer` pieces of live_bytes, outer_stride bytes
  * apart, are moved (keys of one layer as [heads, room, dim]: outer = heads,
  * live_bytes = length * dim * size, outer_stride = room * dim * size).  in == out
- * reorders in place; else the two must not overlap.  A parent outside
- * [0, beams) leaves the row what it is (copies it).
+ * reorders in place.  What is written may be nothing else that the call reads
+ * or writes: a state listed twice in place, an out that overlaps another state
+ * or its own in are refused.  (States in one another's memory have to lie side by
+ * side, in rows of the same row_bytes or pieces of the same outer_stride.)
+ * Several states may read the same memory.  A parent outside [0, beams) leaves
+ * the row what it is (copies it).
  *   states         host array, read before the call returns
  *   parents        int32, rows parent_stride apart (>= beams)
  * ------------------------------------------------------------------------ */

@@ -2,6 +2,10 @@
 // launch order of routing, beam search and the bounded cache.
 #include <math.h>
 
+#include <algorithm>
+#include <memory>
+#include <new>
+
 #include "host.hpp"
 #include "kernels.hpp"
 
@@ -47,6 +51,63 @@ BeamWs carve_beam(Carve& c, int64_t rows, int64_t row_steps, int64_t parts) {
 bool valid_beam(int64_t batch, int64_t beams, int64_t vocab, int64_t num) {
   return batch >= 0 && beams >= 1 && beams <= kBeamMaxBeams && batch <= 65535 / beams && vocab >= 1 &&
          vocab <= 2147483647LL / beams && num >= 1 && num <= kBeamMaxNum;
+}
+
+// What a reorder reads or writes of a state: `rows` rows, of each `outer` pieces.
+struct Region {
+  uint64_t begin, row, outer, stride, live;
+  bool write;
+  uint64_t extent() const { return (outer - 1) * stride + live; }   // of a row
+  unsigned __int128 end(uint64_t rows) const {
+    return static_cast<unsigned __int128>(rows - 1) * row + begin + extent();
+  }
+};
+// Two that begin in this order and have no byte in common: one ends before the
+// other begins, or they lie side by side in each row, or in each piece's stride
+// (regions of other strides that reach into one another count as overlapping).
+bool apart(const Region& a, const Region& b, uint64_t rows) {
+  if (a.end(rows) <= b.begin) return true;
+  uint64_t d = b.begin - a.begin;
+  if (rows > 1) {
+    if (a.row != b.row) return false;
+    d %= a.row;   // (a row holds a piece: not 0)
+    if (d >= a.extent() && d + b.extent() <= a.row) return true;
+  }
+  const uint64_t stride = a.outer > 1 ? a.stride : b.stride;
+  if ((a.outer == 1 && b.outer == 1) || (a.outer > 1 && b.outer > 1 && a.stride != b.stride) ||
+      (rows > 1 && a.row % stride))
+    return false;
+  d %= stride;
+  return d >= a.live && d + b.live <= stride;
+}
+// Whether nothing that is written is read or written as another state, as the
+// same state's other side or as the parents (4-byte, `parents_count` from the
+// first to the last): the threads that move a column know only their own.
+bool none_shared(const lapsum_beam_state* states, int64_t count, uint64_t rows, const int32_t* parents,
+                 uint64_t parents_count) {
+  const std::unique_ptr<Region[]> all(new (std::nothrow) Region[2 * static_cast<size_t>(count) + 1]);
+  if (!all) return false;
+  all[0] = Region{bits_of(parents), 0, 1, 0, 4 * parents_count, false};
+  size_t n = 1;
+  for (int64_t t = 0; t < count; ++t) {
+    const lapsum_beam_state& s = states[t];
+    if (s.outer == 0 || s.live_bytes == 0) continue;
+    const Region r{bits_of(s.out), static_cast<uint64_t>(s.row_bytes), static_cast<uint64_t>(s.outer),
+                   static_cast<uint64_t>(s.outer > 1 ? s.outer_stride : 0),
+                   static_cast<uint64_t>(s.live_bytes), true};
+    all[n++] = r;
+    if (s.in == s.out) continue;
+    all[n] = r;
+    all[n].begin = bits_of(s.in);
+    all[n++].write = false;
+  }
+  std::sort(all.get(), all.get() + n, [](const Region& a, const Region& b) { return a.begin < b.begin; });
+  for (size_t i = 0; i < n; ++i) {
+    const unsigned __int128 end = all[i].end(rows);
+    for (size_t j = i + 1; j < n && all[j].begin < end; ++j)
+      if ((all[i].write || all[j].write) && !apart(all[i], all[j], rows)) return false;
+  }
+  return true;
 }
 
 bool valid_cache(int64_t batch, int64_t kv, int64_t slots, int64_t sink, int64_t recent) {
@@ -201,6 +262,9 @@ int lapsum_beam_reorder(const lapsum_beam_state* states, int64_t count, const in
         s.row_bytes < (s.outer - 1) * s.outer_stride + s.live_bytes)
       return LAPSUM_ERR_INVALID_ARG;
   }
+  if (batch > 0 && !none_shared(states, count, static_cast<uint64_t>(batch * beams), parents,
+                                static_cast<uint64_t>((batch - 1) * parent_stride + beams)))
+    return LAPSUM_ERR_INVALID_ARG;
   const int dst = check_device();
   if (dst != LAPSUM_OK) return dst;
   if (batch == 0) return LAPSUM_OK;

@@ -280,7 +280,8 @@ def lapsum_beam_reorder(states, parents, *, length: int | None = None, out=None)
     on in: row (b, i) <- row (b, parents[b, i]).  length: of states
     [batch * beams, heads, room, dim] (any dimensions before room), move only
     the first `length` of room.  In place, or with `out` (as many tensors of
-    the same shapes) into those.  Returns the tensors written, which autograd
+    the same shapes) into those; what is written must not be part of another
+    state or out.  Returns the tensors written, which autograd
     takes as changed; in grad mode none of them may require grad."""
     states = list(states)
     outs = states if out is None else list(out)
