@@ -61,9 +61,9 @@ def test_softmax_choice_is_that_of_the_rounded_sum(lib, experts, k):
 @pytest.mark.parametrize("high", [4.0, 64.0, 1000.0])
 def test_groups_with_biases_of_opposite_signs(lib, size, masked, high):
     """Two groups, the sum of two experts each, one bias +high and one -high:
-    the sum is small, its terms' spacing is not.  In every row the first
-    group's score is a little below the second's, by less than a spacing, mostly in
-    the same one (the groups are then equal and the first stays), or clearly below."""
+    the sum is small, its terms' spacing is not.  In a row of four the second
+    group's score is the higher by less than a spacing, mostly the same one (the
+    groups are then equal and the first stays); in the others it is clearly lower."""
     import torch
     tokens = 60_000
     gen = torch.Generator(device="cuda").manual_seed(int(high) + size)
@@ -75,7 +75,7 @@ def test_groups_with_biases_of_opposite_signs(lib, size, masked, high):
     close = torch.rand(tokens, generator=gen, device="cuda").double() * 4e-7
     second = torch.logit(middle - close).float()
     first = torch.logit(middle - 0.25 * step.double()).float()
-    # a row in four is close: tokens that share a wave are not all looked at again
+    # the other three rows: tokens that share a wave are not all looked at again
     second[torch.arange(tokens, device="cuda") % 4 != 1] -= 1.0
     x = torch.full((tokens, 2, size), -float("inf"), device="cuda")
     x[:, 0, masked], x[:, 1, masked] = first, second
@@ -90,3 +90,22 @@ def test_groups_with_biases_of_opposite_signs(lib, size, masked, high):
     w, idx = lib.lapsum_route_forward(x.flatten(1), 2, score="sigmoid", bias=bias.flatten(), groups=2,
                                       topk_groups=1, group_top=2)
     assert torch.equal(idx[:, 0] // size, stays) and torch.equal(idx[:, 1] // size, stays)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+def test_sigmoid_scores_are_torchs_on_every_value(lib, dtype):
+    """The exact score of a routing is 1 / (1 + exp(-x)) as torch rounds it, for
+    every float of the type (those of float32 in parts)."""
+    import torch
+    kind = getattr(torch, dtype)
+    bits = 32 if dtype == "float32" else 16
+    part = 1 << min(bits, 26)
+    for start in range(0, 1 << bits, part):
+        raw = torch.arange(start, start + part, device="cuda")
+        x = (raw.to(torch.int32).view(kind) if bits == 32 else raw.to(torch.int16).view(kind))
+        x = x[x > -float("inf")].clamp_max(torch.finfo(torch.float32).max)
+        if not x.numel():
+            continue
+        w, idx = lib.lapsum_route_forward(x[:, None], 1, score="sigmoid")
+        assert bool((idx == 0).all())
+        assert torch.equal(w[:, 0], 1.0 / (1.0 + torch.exp(-x.float()))), hex(start)
