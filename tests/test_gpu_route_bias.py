@@ -10,6 +10,14 @@ import pytest
 pytestmark = pytest.mark.gpu
 
 
+@pytest.fixture(autouse=True, scope="module")
+def _leave_no_large_blocks():
+    """Tests that count on what the allocator holds follow these."""
+    yield
+    import torch
+    torch.cuda.empty_cache()
+
+
 def _best(value, k):
     """The k largest of float32 values, equal ones by the lowest index."""
     import torch

@@ -12,6 +12,15 @@ import pytest
 
 pytestmark = pytest.mark.gpu
 
+
+@pytest.fixture(autouse=True, scope="module")
+def _leave_no_large_blocks():
+    """Tests that count on what the allocator holds follow these."""
+    yield
+    import torch
+    torch.cuda.empty_cache()
+
+
 REQUESTS, BEAMS, VOCAB = 32, 8, 128_000   # rows enough for parts of several steps
 
 
