@@ -484,7 +484,8 @@ int lapsum_route_backward(const float* grad_weights, const void* logits,
  * Beam search: the num best continuations of each request over its beams and
  * the vocabulary.  With x the logits of beam w and cum_w its score so far,
  *   lse_w = log sum_v e^x_wv,   s(w, v) = cum_w + (x_wv - lse_w),
- * each step rounded to float32; equal s by the lowest w * vocab + v.  A
+ * lse formed in float64 and each step rounded to float32 (the results do not
+ * depend on the rest of the batch); equal s by the lowest w * vocab + v.  A
  * continuation whose s is NaN or -inf is none: a logit of -inf is masked, a
  * beam with cum -inf or NaN, or with a logit of NaN or +inf, offers nothing.
  * Where fewer than num are left the rest gets score -inf, token -1 and parent -1.

@@ -29,7 +29,7 @@
 // 1e-6 off, by another amount for other parts.  Lists of the best logits kept
 // in the scan, as a first form had them, took 43: the candidates' steps wait on
 // each other.  The finish is such a chain (lse, bound, the steps' second read,
-// the lists): 13 us for 32 requests of 8 beams, 7.0 for one of 4.
+// the lists): 14 us for 32 requests of 8 beams, 7.1 for one of 4.
 #include "select_common.hpp"
 
 namespace lapsum {

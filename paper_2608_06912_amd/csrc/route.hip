@@ -35,14 +35,14 @@
 // settles what cannot be chosen; the candidates, and rows whose groups are
 // closer than that, get the exact one.
 //
-// Bound: vector issue and the latency between its steps.  65536 tokens of 256
-// bfloat16 logits in eight groups, 8 chosen: 34 us, and 4.7 for the counts
-// (their bytes take 7.4 at the rate of a copy); 670 vector instructions for four
-// tokens, 17 us without groups.  With comparisons counted as such, not as the
-// sign of a difference, and the groups' scores passed through LDS, it took 37
-// (785 instructions); with the exact score of every logit as well 72.  16
-// tokens: 4.4 us, one wave's chain of steps.  Backward: 32768 tokens of 128
-// float32 logits, dense, 10.8 us (bytes 6.6).
+// Bound: vector issue, about half, and the waits between its steps.  65536
+// tokens of 256 bfloat16 logits in eight groups, 8 chosen: 30 us, 17 without
+// groups; with counts 32 and 4.7 for their kernel (the bytes take 7.4 at the rate
+// of a copy); 673 vector instructions for four tokens, 18 us.  With comparisons
+// counted as such, not as the sign of a difference, and the groups' scores passed
+// through LDS, it took 785 instructions and 3 us more; with the exact score of
+// every logit as well twice the time.  16 tokens: 4.3 us, one wave's chain of
+// steps.  Backward: 32768 tokens of 128 float32 logits, dense, 10.8 us (bytes 6.6).
 #include "select_common.hpp"
 
 namespace lapsum {
@@ -624,7 +624,8 @@ __global__ __launch_bounds__(BT) void route_backward_kernel(RouteGradArgs a) {
 namespace {
 // 16 lanes hold a token of up to 512 experts (32 values each); a team has to
 // have a lane per chosen expert and per group, and to leave most rows fewer
-// candidates than lanes.
+// candidates than lanes.  65536 tokens of 256, sigmoid: 18 us with 8 chosen, and
+// by the wave 51 with 9, 60 with 16; 32768 of 512: 15 with 8, 32 with 10.
 bool narrow_team(int experts, int top_k, int groups) {
   return experts <= 512 && top_k <= 8 && groups <= 16;
 }
@@ -652,9 +653,10 @@ bool by_team(int experts, bool narrow, F&& f) {
 }
 
 // Workgroups, each with the same number of turns: a turn each, so that a compute
-// unit that is done takes the next (65536 tokens: 28.6 us, 32.6 with those that
-// fit the device together), but with counts, which each has to clear, add up and
-// leave to the second kernel, no more than fit (37.4 in all, 38.7 with a turn each).
+// unit that is done takes the next (65536 tokens of 256 in eight groups: 30.2 us,
+// 33.7 with those that fit the device together), but with counts, which each has
+// to clear, add up and leave to the second kernel, no more than fit (38.4 in all,
+// 39.6 with a turn each).
 int64_t route_grid(int64_t tokens, bool narrow, bool counts) {
   const int64_t per = BT / (narrow ? 16 : 64);
   const int64_t want = (tokens + per - 1) / per;
