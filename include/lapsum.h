@@ -417,7 +417,10 @@ int lapsum_backward_band(const float* grad_p, const float* p, const void* band,
 typedef enum lapsum_dtype {
     LAPSUM_F32 = 0,
     LAPSUM_BF16 = 1,
-    LAPSUM_F16 = 2
+    LAPSUM_F16 = 2,
+    /* a paged cache only: codes of 8 bits, with a float32 scale per row */
+    LAPSUM_I8 = 3,
+    LAPSUM_E4M3 = 4
 } lapsum_dtype;
 
 /* ------------------------------------------------------------------------
@@ -600,6 +603,160 @@ int lapsum_cache_step(const void* weights, int dtype, int64_t stride_batch,
                       float* acc, int32_t* pos, int64_t batch, int64_t heads,
                       int64_t kv_heads, int64_t slots, int64_t sink,
                       int64_t recent, int32_t* slot, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * The experts that lapsum_route_forward chose: their rows' order, products and
+ * weighted sum.
+ *
+ * lapsum_expert_order: the places (token, slot) of the router's indices by expert.
+ *   indices    [count] int32; one outside [0, experts) is a place without an expert
+ *   order      [count] int32: the places by expert, in each expert by number,
+ *              those without an expert last
+ *   place      [count] int32: each place's position in the order, -1 without an expert
+ *   offsets    [experts + 1] int32: expert e has the positions
+ *              offsets[e] <= i < offsets[e + 1]; the last is the number of places with one
+ *   0 <= count <= 2^30, 1 <= experts <= 2048
+ *   workspace  lapsum_expert_order_workspace_size bytes (0 up to 8192 places)
+ *
+ * lapsum_expert_matmul: y[i] = x[row(i)] w_e for the rows i of expert e, and 0 for the
+ * rows of none; row(i) = order[i] / top_k, or i without an order.  Sums are formed in
+ * float32 and rounded once.
+ *   x          [x_rows] rows of `in` elements, x_stride apart; a row(i) that is none
+ *              of them counts as zeros
+ *   offsets    as above (the first counts as 0, and none beyond `rows`)
+ *   w          by three strides (expert, in, out), of which that of `in` or of
+ *              `out` is 1: matrices stored either way round
+ *   y          [rows, out] dense, of type y_dtype: that of x, or float32
+ *   rows <= 2^30 (at most x_rows without an order), in and out <= 2^24
+ *
+ * lapsum_expert_matmul_weights: its gradient with respect to w,
+ * grad_w[e] = sum over e's rows of x[row(i)]^T grad_y[i], 0 for an expert
+ * without rows.  (That with respect to x is lapsum_expert_matmul of
+ * grad_y and w with the strides of `in` and `out` exchanged, then
+ * lapsum_expert_combine without weights where x came through an order.)
+ *   grad_y     [rows] rows of `out` elements, grad_stride apart
+ *   grad_w     like w, its matrices not overlapping; written whole
+ *
+ * lapsum_expert_combine: out[t] = sum_j weights[t, j] y[place[t, j]], in the order of
+ * the slots, in float32, rounded once; a place outside [0, rows) has no share.
+ *   y          [rows, dim] dense
+ *   weights    [tokens, top_k] float32, or NULL (1 each)
+ *   out        [tokens, dim] dense, the type of y (any where y is float32)
+ * Backward: grad_y[place[t, j]] = weights[t, j] grad_out[t], 0 for the rows from
+ * offsets[experts] on; grad_weights[t, j] = <grad_out[t], y[place[t, j]]>, 0
+ * without a row.  place and offsets are those of one lapsum_expert_order: rows
+ * before the last offset that no place names are not written.
+ * ------------------------------------------------------------------------ */
+size_t lapsum_expert_order_workspace_size(int64_t count, int64_t experts);
+
+int lapsum_expert_order(const int32_t* indices, int64_t count, int64_t experts,
+                        int32_t* order, int32_t* place, int32_t* offsets,
+                        void* workspace, size_t workspace_bytes,
+                        hipStream_t stream);
+
+int lapsum_expert_matmul(const void* x, int dtype, int64_t x_rows,
+                         int64_t x_stride, const int32_t* order, int64_t top_k,
+                         const int32_t* offsets, int64_t experts, int64_t rows,
+                         int64_t in, int64_t out, const void* w,
+                         const int64_t* w_strides, void* y, int y_dtype,
+                         hipStream_t stream);
+
+int lapsum_expert_matmul_weights(const void* x, int dtype, int64_t x_rows,
+                                 int64_t x_stride, const int32_t* order,
+                                 int64_t top_k, const int32_t* offsets,
+                                 int64_t experts, int64_t rows, int64_t in,
+                                 int64_t out, const void* grad_y,
+                                 int64_t grad_stride, void* grad_w,
+                                 const int64_t* w_strides, hipStream_t stream);
+
+int lapsum_expert_combine(const void* y, int dtype, int64_t rows, int64_t dim,
+                          const float* weights, const int32_t* place,
+                          int64_t tokens, int64_t top_k, void* out,
+                          int out_dtype, hipStream_t stream);
+
+int lapsum_expert_combine_backward(const void* grad_out, const void* y,
+                                   int dtype, int64_t rows, int64_t dim,
+                                   const float* weights, const int32_t* place,
+                                   const int32_t* offsets, int64_t experts,
+                                   int64_t tokens, int64_t top_k, void* grad_y,
+                                   float* grad_weights, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * A key-value cache in pages, of the inputs' type or in 8 bits.
+ *
+ * data is [pages, kv_heads, slots] rows of `dim` elements (dense, dim <= 256) by
+ * three strides.  Position p of sequence b is slot p % slots of page
+ * table[b, p / slots]; without a table (NULL) page b is sequence b's, and slots
+ * its room.  A table entry outside [0, pages) is a page that is not there:
+ * nothing is written to it, and its positions count as masked.  Lengths beyond
+ * the table's room count as the room.
+ *
+ * Rows in 8 bits (kind LAPSUM_I8 or LAPSUM_E4M3) have a scale
+ * s = max(r max |x|, 2^-126), r the float32 nearest 1 / 127 or 1 / 448, in scale
+ * [pages, kv_heads, slots] (slots dense): a code is x / s rounded to the
+ * nearest, ties to even, and stands for code * s.  A row with an infinity or NaN reads back as NaN.
+ *
+ * lapsum_cache_append: writes new entry i of sequence b at position seen[b] + i, for
+ * i < count[b] (all `fresh` of them without counts); positions outside the room are not
+ * written.  The caller advances seen.
+ *   k_new, v_new   [batch, kv_heads, fresh] rows by three strides, of type dtype
+ *   kind           the caches' type: dtype, LAPSUM_I8 or LAPSUM_E4M3
+ *   seen           [batch] int32;  count  [batch] int32, or NULL
+ *   table          [batch, width] int32, or NULL.  No two positions that one
+ *                  call writes may be one slot (a page of two sequences' ends)
+ *
+ * lapsum_cache_read: out[b, h, p] = the entry of position p < lens[b], in float32 and
+ * rounded once to dtype; 0 for the positions from lens[b] on and those not there.
+ *   out            [batch, kv_heads, room, dim] dense; room >= 0 is the caller's choice
+ *
+ * lapsum_cache_attend: one new token's attention.  For query head g, of key head
+ * h = g / (heads / kv_heads), over the positions p < lens[b] (with a
+ * window > 0 only the last `window` of them):
+ *   s_p = scale <q, k_p>,  out = sum e^(s_p - m) v_p / l,  m = max s,
+ *   l = sum e^(s_p - m),  lse = m + log l,  weights_p = e^(s_p - lse).
+ * A row without positions (or with every score -inf) gets out 0, lse -inf, weights 0.
+ *   q         [batch, heads] rows of dim elements by two strides, of type dtype
+ *   out       [batch, heads, dim] dense, of type dtype
+ *   lse       [batch, heads] float32, or NULL
+ *   weights   [batch, heads, room] float32 (room: width * slots, or slots without
+ *             a table), or NULL; with it lse is needed too
+ *   scale     finite
+ *   workspace lapsum_cache_attend_workspace_size bytes
+ * batch, fresh and lengths may be 0; batch * heads <= 2^23; room <= 2^30.
+ * ------------------------------------------------------------------------ */
+typedef struct lapsum_paged {
+    void* data;
+    float* scale;              /* NULL unless in 8 bits */
+    int64_t pages, slots;
+    int64_t stride_page, stride_head, stride_slot;   /* in elements */
+    int64_t scale_stride_page, scale_stride_head;
+} lapsum_paged;
+
+int lapsum_cache_append(const void* k_new, const int64_t* k_strides,
+                        const void* v_new, const int64_t* v_strides, int dtype,
+                        int64_t batch, int64_t kv_heads, int64_t fresh,
+                        int64_t dim, const int32_t* seen, const int32_t* count,
+                        const lapsum_paged* k, const lapsum_paged* v, int kind,
+                        const int32_t* table, int64_t width,
+                        hipStream_t stream);
+
+int lapsum_cache_read(const lapsum_paged* cache, int kind, int64_t batch,
+                      int64_t kv_heads, int64_t room, int64_t dim,
+                      const int32_t* lens, const int32_t* table, int64_t width,
+                      void* out, int dtype, hipStream_t stream);
+
+size_t lapsum_cache_attend_workspace_size(int64_t batch, int64_t heads,
+                                          int64_t kv_heads, int64_t dim,
+                                          int64_t room, int64_t window);
+
+int lapsum_cache_attend(const void* q, int64_t q_stride_batch,
+                        int64_t q_stride_head, int dtype, const lapsum_paged* k,
+                        const lapsum_paged* v, int kind, int64_t batch,
+                        int64_t heads, int64_t kv_heads, int64_t dim,
+                        const int32_t* lens, const int32_t* table,
+                        int64_t width, double scale, int64_t window, void* out,
+                        float* lse, float* weights, void* workspace,
+                        size_t workspace_bytes, hipStream_t stream);
 
 /* ------------------------------------------------------------------------
  * Diagnostics: per-kernel timing with HIP events.  Off by default.  While

@@ -11,7 +11,8 @@ not built, or the tensors are not on a gfx950 device, the calls raise.
     p, b, info, m_idx = lapsum_forward_bracketed(scores, k, alpha, noise)
 
 The hard selections of a language model (routing to experts, beam search, a
-bounded key-value cache) are in selection.py and exported here too.
+bounded key-value cache) are in selection.py, the experts' products in experts.py
+and the paged key-value cache in paged.py, all exported here too.
 
 `scores` is a float32 CUDA tensor of shape [n] or [batch, n]; k and alpha
 are Python floats with 0 < k < n and alpha < 0.
@@ -607,5 +608,9 @@ def lapsum_profile_stop() -> dict:
 
 from .selection import *            # noqa: E402,F401,F403  (it uses what stands above)
 from .selection import __all__ as _selection_names   # noqa: E402
+from .experts import *              # noqa: E402,F401,F403
+from .experts import __all__ as _experts_names       # noqa: E402
+from .paged import *                # noqa: E402,F401,F403
+from .paged import __all__ as _paged_names           # noqa: E402
 
-__all__ += _selection_names
+__all__ += _selection_names + _experts_names + _paged_names

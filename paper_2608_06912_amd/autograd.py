@@ -28,12 +28,14 @@ import os
 import torch
 
 from . import (HERE, LapsumError, lapsum_backward, lapsum_backward_band, lapsum_bracket_noise,
-               lapsum_forward, lapsum_forward_bracketed, lapsum_hard_mask, lapsum_route_backward,
-               lapsum_route_forward, load, new_band)
+               lapsum_expert_combine, lapsum_expert_combine_backward, lapsum_expert_matmul,
+               lapsum_expert_matmul_weights, lapsum_forward, lapsum_forward_bracketed,
+               lapsum_hard_mask, lapsum_route_backward, lapsum_route_forward, load, new_band)
 
 __all__ = ["soft_topk", "hard_topk_mask", "straight_through", "choose_path", "sample_size",
            "bracket_noise", "bracket_indices", "LapSumFunction", "FULL_SORT_MAX_N", "route_topk",
-           "RouteFunction"]
+           "RouteFunction", "expert_matmul", "ExpertMatmulFunction", "expert_combine",
+           "ExpertCombineFunction"]
 
 # A row up to this length takes the full path (which sorts only for a
 # permutation; the names are older); longer rows the sample bracket.
@@ -358,3 +360,87 @@ def route_topk(logits, top_k: int, *, score: str = "softmax", bias=None, groups:
                 return tuple(out)
         return RouteFunction.apply(logits, top_k, options, counts)
     return lapsum_route_forward(logits, top_k, counts=counts, **options)
+
+
+def _gather(gather):
+    """(order, place, top_k) of a gather=(order, place) argument."""
+    if gather is None:
+        return None, None, 1
+    order, place = gather
+    if place.dim() != 2 or order.numel() != place.numel():
+        raise ValueError("gather must be the (order, place) of lapsum_expert_order over [tokens, top_k] places")
+    return order, place, max(place.shape[1], 1)
+
+
+class ExpertMatmulFunction(torch.autograd.Function):
+    """lapsum_expert_matmul as an autograd node: the gradients of rows and matrices."""
+
+    @staticmethod
+    def forward(ctx, x, weight, offsets, order, place, top_k):
+        y = lapsum_expert_matmul(x.detach(), weight.detach(), offsets, order=order, top_k=top_k)
+        ctx.save_for_backward(x, weight, offsets, order, place)
+        ctx.top_k = top_k
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad):
+        x, weight, offsets, order, place = ctx.saved_tensors
+        grad = grad.contiguous()
+        grad_x = grad_w = None
+        if ctx.needs_input_grad[0]:
+            back = weight.detach().transpose(1, 2)
+            if order is None:
+                grad_x = lapsum_expert_matmul(grad, back, offsets)
+            else:   # a token's rows are summed before they are rounded
+                rows = lapsum_expert_matmul(grad, back, offsets, dtype=torch.float32)
+                grad_x = lapsum_expert_combine(rows, place, dtype=x.dtype)
+        if ctx.needs_input_grad[1]:
+            grad_w = lapsum_expert_matmul_weights(x.detach(), grad, offsets, weight, order=order,
+                                                  top_k=ctx.top_k)
+        return grad_x, grad_w, None, None, None, None
+
+
+def expert_matmul(x, weight, offsets, *, gather=None):
+    """x[row(i)] @ weight[e] for the rows i of each expert e, differentiable in x and
+    weight: [rows, out], zeros for the rows of no expert.  x [rows, in] in the
+    experts' order, weight [experts, in, out] (stored either way round), offsets of
+    lapsum_expert_order.  With gather=(order, place), of the same call over [tokens,
+    top_k] places, x is [tokens, in] and row(i) = order[i] // top_k.  The
+    derivative is that of reverse mode; forward mode is refused."""
+    order, place, top_k = _gather(gather)
+    if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad) or _has_tangent(x) \
+            or _has_tangent(weight):
+        if order is not None and place.shape[0] != x.shape[0]:
+            raise ValueError("place must have a row for each row of x")
+        return ExpertMatmulFunction.apply(x, weight, offsets, order, place, top_k)
+    return lapsum_expert_matmul(x, weight, offsets, order=order, top_k=top_k)
+
+
+class ExpertCombineFunction(torch.autograd.Function):
+    """lapsum_expert_combine as an autograd node: the gradients of outputs and weights."""
+
+    @staticmethod
+    def forward(ctx, y, weights, place, offsets):
+        out = lapsum_expert_combine(y.detach(), place, weights.detach())
+        ctx.save_for_backward(y, weights, place, offsets)
+        return out
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad):
+        y, weights, place, offsets = ctx.saved_tensors
+        grad_y, grad_w = lapsum_expert_combine_backward(grad.contiguous(), y.detach(), place,
+                                                        weights.detach(), offsets)
+        return grad_y, grad_w, None, None
+
+
+def expert_combine(y, weights, place, offsets):
+    """out[t] = sum_j weights[t, j] y[place[t, j]], differentiable in y [rows, dim] and
+    weights float32 [tokens, top_k] (those of route_topk); place and offsets of
+    lapsum_expert_order.  The derivative is that of reverse mode; forward mode is
+    refused."""
+    if torch.is_grad_enabled() and (y.requires_grad or weights.requires_grad) or _has_tangent(y) \
+            or _has_tangent(weights):
+        return ExpertCombineFunction.apply(y, weights, place, offsets)
+    return lapsum_expert_combine(y, place, weights)

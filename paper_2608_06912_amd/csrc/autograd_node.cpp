@@ -129,4 +129,5 @@ Tensor full(const Tensor& scores, const std::optional<Tensor>& k_like,
 PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
   m.def("full", lapsum_node::entry(full));
   bind_selection(m);
+  bind_products(m);
 }

@@ -51,6 +51,24 @@ inline int check_ws(void* ws, size_t have, size_t need) {
   return LAPSUM_OK;
 }
 
+// -------------------------------------------------------- argument checks --
+constexpr int64_t kMaxBlocks = int64_t(1) << 23;   // workgroups of a launch
+
+inline bool valid_dtype(int dtype) { return dtype >= LAPSUM_F32 && dtype <= LAPSUM_F16; }
+
+inline bool int32_range(int64_t v) { return v >= 0 && v <= 2147483647LL; }
+
+// The widest power of two, up to 16, that divides everything or'ed into bits.
+inline int vector_width(uint64_t bits) {
+  int w = 16;
+  while (w > 1 && bits % static_cast<uint64_t>(w)) w /= 2;
+  return w;
+}
+inline uint64_t bits_of(const void* p) { return reinterpret_cast<uintptr_t>(p); }
+inline uint64_t bits_of(const int64_t* strides) {
+  return static_cast<uint64_t>(strides[0] | strides[1] | strides[2]);
+}
+
 #define LAPSUM_TRY(expr)                         \
   do {                                           \
     if ((expr) != hipSuccess) return LAPSUM_ERR_HIP; \

@@ -499,4 +499,109 @@ struct StepArgs {
 };
 hipError_t launch_cache_step(const StepArgs& a, int dtype, hipStream_t s);
 
+// -------------------------------------------------------- experts' rows ----
+constexpr int kExpertMost = 2048;
+struct OrderArgs {
+  const int32_t* indices;
+  int64_t count;
+  int experts;
+  int32_t *order, *place, *offsets;
+  int* parts;                // [order_blocks][experts + 1], where that is above one
+};
+int64_t order_blocks(int64_t count);
+hipError_t launch_expert_order(const OrderArgs& a, hipStream_t s);
+
+struct CombineArgs {
+  const void* y;             // [rows, dim]
+  const float* weights;      // [tokens, top_k], or null
+  const int32_t* place;
+  void* out;                 // [tokens, dim]
+  int64_t tokens, dim, rows, pieces;   // pieces set by the launcher
+  int top_k;
+};
+// vec: rows and addresses are whole vectors of 16 bytes (and 8 elements).
+hipError_t launch_expert_combine(CombineArgs a, int dtype, int out_dtype, bool vec, hipStream_t s);
+struct CombineGradArgs {
+  const void *grad, *y;
+  const float* weights;
+  const int32_t *place, *ends;   // ends: [experts + 1]
+  void* grad_y;
+  float* grad_weights;
+  int64_t tokens, dim, rows;
+  int top_k, experts;
+};
+hipError_t launch_expert_combine_backward(const CombineGradArgs& a, int dtype, bool vec, hipStream_t s);
+
+// Products grouped by expert.  Rows: y[i] = x[row(i)] w_e for the rows of each
+// expert.  Grad: c_e[m][n] = sum over the expert's rows of a[row][m] b[row][n].
+struct RowsArgs {
+  const void* x;             // [x_rows, k], rows x_stride apart
+  const void* w;             // matrices [k, n]: n dense (w_n_dense), or k dense
+  void* y;                   // [rows, n] dense
+  const int32_t *order, *offsets;
+  int64_t x_rows, x_stride, w_expert, w_row;   // in elements; w_row: from one dense row to the next
+  int rows, k, n, experts, top_k;
+  int tiles_n;               // set by the launcher
+};
+hipError_t launch_expert_rows(RowsArgs a, int dtype, bool w_n_dense, bool out_f32, bool vec, hipStream_t s);
+struct GradArgs {
+  const void *a, *b;         // the side by expert's row order comes through order where gather says so
+  void* c;                   // matrices [m, n], n dense
+  const int32_t *order, *offsets;
+  int64_t a_rows, b_rows, a_stride, b_stride, c_expert, c_row;
+  int rows, m, n, experts, top_k, gather;   // gather: 0 none, 1 of a, 2 of b
+  int tiles_m, tiles_n;
+};
+hipError_t launch_expert_grad(GradArgs a, int dtype, bool vec, hipStream_t s);
+
+// ---------------------------------------------------------- paged cache ----
+constexpr int kPagedMaxDim = 256;
+// A cache [pages, kv, slots] of rows of dim elements; strides in elements.
+struct PagedCache {
+  void* data;
+  float* scale;              // null: not quantised
+  int64_t page, head, slot;  // strides of data
+  int64_t scale_page, scale_head;
+};
+struct PageTable {
+  const int32_t* table;      // [batch, width], or null: page b is sequence b's
+  int64_t pages;
+  int width, size;           // pages of a sequence, slots of a page
+};
+struct AppendArgs {
+  const void* src[2];
+  int64_t src_b[2], src_h[2], src_i[2];
+  PagedCache cache[2];
+  PageTable t;
+  const int32_t *seen, *count;
+  int batch, kv, fresh, dim;
+  int chunks;                // set by the launcher
+};
+hipError_t launch_cache_append(AppendArgs a, int dtype, int kind, bool vec, hipStream_t s);
+struct ReadArgs {
+  PagedCache cache;
+  PageTable t;
+  const int32_t* lens;
+  void* out;                 // [batch, kv, room, dim]
+  int batch, kv, room, dim;
+  int chunks;
+};
+hipError_t launch_cache_read(ReadArgs a, int dtype, int kind, bool vec, hipStream_t s);
+struct AttendArgs {
+  const void* q;             // [batch, heads, dim]
+  int64_t q_b, q_h;
+  PagedCache k, v;
+  PageTable t;
+  const int32_t* lens;
+  void* out;                 // [batch, heads, dim]
+  float *lse, *weights;      // [batch, heads], [batch, heads, room], or null
+  float* part;               // [splits][batch][heads][dim + 2]: sum, maximum, total
+  int batch, heads, kv, dim, group, tiles, window, splits, chunk;
+  int64_t room;
+  float scale;
+};
+hipError_t launch_cache_attend(const AttendArgs& a, int dtype, int kind, bool vec, hipStream_t s);
+void attend_plan(int64_t batch, int64_t heads, int64_t kv, int64_t room, int64_t window, int* splits,
+                 int* chunk);
+
 }  // namespace lapsum

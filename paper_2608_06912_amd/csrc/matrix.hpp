@@ -1,0 +1,116 @@
+// Tiles of a matrix product on the matrix cores: operands in LDS as chunks of 16
+// bytes, and the fragments of a 16 x 16 tile of results read from them.
+//
+// The contraction goes in stages of 128 bytes (64 elements of 16 bits, 32
+// floats), a stage in two steps of four chunks.  Lane l of a wave holds, of
+// row l & 15, the chunk l >> 4 of a step: eight elements for one 16x16x32
+// instruction, or four floats for four 16x16x4 ones (the order of the
+// contraction is the operands' own business, as long as it is the same for both).
+#pragma once
+
+#include "select_common.hpp"
+
+namespace lapsum {
+
+typedef float Acc __attribute__((ext_vector_type(4)));
+typedef __bf16 Bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 F16x8 __attribute__((ext_vector_type(8)));
+typedef short Half4 __attribute__((ext_vector_type(4)));
+
+// c += a b^T of a step: rows of a and b as above; c[i] of lane l is row
+// 4 (l >> 4) + i of a and row l & 15 of b.
+template <int DT>
+__device__ __forceinline__ Acc mma(Move16 a, Move16 b, Acc c) {
+  if constexpr (DT == 0) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[j]), __uint_as_float(b[j]), c, 0, 0, 0);
+    return c;
+  } else if constexpr (DT == 1) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(Bf16x8, a), __builtin_bit_cast(Bf16x8, b),
+                                                   c, 0, 0, 0);
+  } else {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(F16x8, a), __builtin_bit_cast(F16x8, b), c,
+                                                  0, 0, 0);
+  }
+}
+
+// The chunk at p of which `left` elements exist (the others are 0).  VEC: a chunk
+// exists whole or not at all, at a multiple of 16 bytes.
+template <int DT, bool VEC>
+__device__ __forceinline__ Move16 load_chunk(const typename Elem<DT>::raw* p, int64_t left) {
+  constexpr int N = 16 / sizeof(typename Elem<DT>::raw);
+  Move16 v = {0u, 0u, 0u, 0u};
+  if constexpr (VEC) {
+    if (left > 0) v = *reinterpret_cast<const Move16*>(p);
+  } else if (left >= N) {
+    // (global memory serves vectors at any alignment of their elements)
+    struct __attribute__((packed, aligned(sizeof(*p)))) Any {
+      uint32_t x, y, z, w;
+    };
+    const Any u = *reinterpret_cast<const Any*>(p);
+    v = Move16{u.x, u.y, u.z, u.w};
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (j < left) {
+        if constexpr (DT == 0) v[j] = p[j];
+        else v[j / 2] |= static_cast<uint32_t>(p[j]) << (16 * (j % 2));
+      }
+  }
+  return v;
+}
+
+// An operand of R rows in LDS.  Dense along the contraction (TR false): R rows of
+// eight chunks.  Dense along the rows (TR true): a row of R elements for each
+// element of the contraction.  Chunks are permuted within a row by the row's
+// number, so that the lanes that read together meet different banks.
+template <int DT, int R, bool TR>
+struct Operand {
+  static constexpr int E = DT == 0 ? 4 : 2;              // bytes of an element
+  static constexpr int N = 16 / E;                       // elements of a chunk
+  static constexpr int Stage = 128 / E;                  // contraction of a stage
+  static constexpr int Rows = TR ? Stage : R;
+  static constexpr int Chunks = TR ? R * E / 16 : 8;     // of a row
+  static constexpr int Total = Rows * Chunks;
+  static constexpr int Bytes = Total * 16;
+
+  static __device__ __forceinline__ int swizzle(int r) {
+    if constexpr (!TR) return r & 7;
+    else if constexpr (DT == 0) return ((r >> 2) & 3) << 2;
+    else return ((r & 3) | ((r >> 1) & 4)) << 1;
+  }
+  static __device__ __forceinline__ int slot(int r, int c) { return r * Chunks + (c ^ swizzle(r)); }
+
+  // The fragment of rows r0 .. r0 + 15 (a multiple of 16) and step s.
+  static __device__ __forceinline__ Move16 fragment(const char* lds, int r0, int s) {
+    const int i = threadIdx.x & 15, g = (threadIdx.x >> 4) & 3;
+    if constexpr (!TR) {
+      return *reinterpret_cast<const Move16*>(lds + 16 * slot(r0 + i, 4 * s + g));
+    } else if constexpr (DT == 0) {
+      Move16 v;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int r = 16 * s + 4 * g + j, c = r0 + i;
+        v[j] = *reinterpret_cast<const uint32_t*>(lds + 16 * slot(r, c / 4) + 4 * (c % 4));
+      }
+      return v;
+    } else {
+      // 16 lanes read four rows of 16 elements, and each gets a column of them
+      Move16 v;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int r = 32 * s + 8 * g + 4 * h + (i >> 2), c = r0 + 4 * (i & 3);
+        const char* p = lds + 16 * slot(r, c / 8) + 2 * (c % 8);
+        const Half4 t = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) Half4*)(p));
+        const Move8 w = __builtin_bit_cast(Move8, t);
+        v[2 * h] = w[0];
+        v[2 * h + 1] = w[1];
+      }
+      return v;
+    }
+  }
+};
+
+}  // namespace lapsum

@@ -74,6 +74,30 @@ inline Tensor bytes(size_t n, const Tensor& like) {
 
 inline void* ptr(const Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
 
+using OptTensor = std::optional<Tensor>;
+
+inline int dtype_of(const Tensor& t) {
+  switch (t.scalar_type()) {
+    case at::kFloat: return LAPSUM_F32;
+    case at::kBFloat16: return LAPSUM_BF16;
+    case at::kHalf: return LAPSUM_F16;
+    default: return -1;
+  }
+}
+inline bool plain(const Tensor& t) { return t.is_cuda() && t.layout() == at::kStrided && !t.is_quantized(); }
+inline bool dense(const Tensor& t, at::ScalarType type, const Tensor& like) {
+  return plain(t) && t.scalar_type() == type && t.is_contiguous() && t.device() == like.device();
+}
+
+// What a call writes in place: nothing that requires grad in grad mode (the
+// binding says so), and autograd is told afterwards, as after an in-place call of
+// torch's.
+inline bool may_write(const Tensor& t) { return !(t.requires_grad() && at::GradMode::is_enabled()); }
+inline void written(const Tensor& t) {
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 }  // namespace lapsum_node
 
 void bind_selection(py::module_& m);
+void bind_products(py::module_& m);

@@ -13,23 +13,6 @@ using namespace lapsum;
 
 namespace {
 
-constexpr int64_t kMaxBlocks = int64_t(1) << 23;   // workgroups of a launch
-
-bool valid_dtype(int dtype) { return dtype >= LAPSUM_F32 && dtype <= LAPSUM_F16; }
-
-bool int32_range(int64_t v) { return v >= 0 && v <= 2147483647LL; }
-
-// The widest power of two, up to 16, that divides everything or'ed into bits.
-int vector_width(uint64_t bits) {
-  int w = 16;
-  while (w > 1 && bits % static_cast<uint64_t>(w)) w /= 2;
-  return w;
-}
-uint64_t bits_of(const void* p) { return reinterpret_cast<uintptr_t>(p); }
-uint64_t bits_of(const int64_t* strides) {
-  return static_cast<uint64_t>(strides[0] | strides[1] | strides[2]);
-}
-
 bool valid_route(int dtype, int64_t tokens, int64_t experts, int64_t row_stride, int score,
                  int64_t top_k, double scale) {
   return valid_dtype(dtype) && tokens >= 0 && experts >= 1 && experts <= kRouteMaxExperts &&

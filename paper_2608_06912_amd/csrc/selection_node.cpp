@@ -10,35 +10,9 @@
 
 namespace {
 
-using lapsum_node::bytes;
-using lapsum_node::check;
-using lapsum_node::ptr;
-using lapsum_node::stream_of;
-using torch::Tensor;
+using namespace lapsum_node;
 using torch::autograd::AutogradContext;
 using torch::autograd::variable_list;
-using OptTensor = std::optional<Tensor>;
-
-int dtype_of(const Tensor& t) {
-  switch (t.scalar_type()) {
-    case at::kFloat: return LAPSUM_F32;
-    case at::kBFloat16: return LAPSUM_BF16;
-    case at::kHalf: return LAPSUM_F16;
-    default: return -1;
-  }
-}
-bool plain(const Tensor& t) { return t.is_cuda() && t.layout() == at::kStrided && !t.is_quantized(); }
-bool dense(const Tensor& t, at::ScalarType type, const Tensor& like) {
-  return plain(t) && t.scalar_type() == type && t.is_contiguous() && t.device() == like.device();
-}
-
-// What a call writes in place: nothing that requires grad in grad mode (the
-// binding says so), and autograd is told afterwards, as after an in-place call of
-// torch's.
-bool may_write(const Tensor& t) { return !(t.requires_grad() && at::GradMode::is_enabled()); }
-void written(const Tensor& t) {
-  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
-}
 
 // Logits as rows: contiguous, or two dimensions with dense rows.
 struct Rows {
