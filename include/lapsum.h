@@ -636,6 +636,8 @@ int lapsum_cache_step(const void* weights, int dtype, int64_t stride_batch,
  * lapsum_expert_combine without weights where x came through an order.)
  *   grad_y     [rows] rows of `out` elements, grad_stride apart
  *   grad_w     like w, its matrices not overlapping; written whole
+ *   workspace  lapsum_expert_matmul_weights_workspace_size bytes (0 unless the
+ *              matrices are small and the rows many)
  *
  * lapsum_expert_combine: out[t] = sum_j weights[t, j] y[place[t, j]], in the order of
  * the slots, in float32, rounded once; a place outside [0, rows) has no share.
@@ -661,13 +663,17 @@ int lapsum_expert_matmul(const void* x, int dtype, int64_t x_rows,
                          const int64_t* w_strides, void* y, int y_dtype,
                          hipStream_t stream);
 
+size_t lapsum_expert_matmul_weights_workspace_size(int64_t experts, int64_t rows,
+                                                   int64_t in, int64_t out);
+
 int lapsum_expert_matmul_weights(const void* x, int dtype, int64_t x_rows,
                                  int64_t x_stride, const int32_t* order,
                                  int64_t top_k, const int32_t* offsets,
                                  int64_t experts, int64_t rows, int64_t in,
                                  int64_t out, const void* grad_y,
                                  int64_t grad_stride, void* grad_w,
-                                 const int64_t* w_strides, hipStream_t stream);
+                                 const int64_t* w_strides, void* workspace,
+                                 size_t workspace_bytes, hipStream_t stream);
 
 int lapsum_expert_combine(const void* y, int dtype, int64_t rows, int64_t dim,
                           const float* weights, const int32_t* place,

@@ -30,7 +30,7 @@ HIP_SOURCES = ["row_kernels.hip", "stream_kernels.hip", "sort_kernels.hip",
                "comparator_kernels.hip", "noalloc.hip",
                "long_solve.hip", "short_rows.hip", "hard_mask.hip",
                "route.hip", "beam.hip", "cache.hip",
-               "experts.hip", "expert_matmul.hip", "paged.hip", "attend.hip"]
+               "experts.hip", "expert_rows.hip", "expert_grad.hip", "paged.hip", "attend.hip"]
 HOST_SOURCES = ["lapsum_api.cpp", "selection_api.cpp", "experts_api.cpp", "paged_api.cpp"]
 NODE_SOURCE = "autograd_node.cpp"
 NODE_SOURCES = [NODE_SOURCE, "selection_node.cpp", "products_node.cpp"]

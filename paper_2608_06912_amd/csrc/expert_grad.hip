@@ -1,0 +1,206 @@
+// The gradient of the experts' matrices: for each expert a product over its rows,
+//
+//   c_e[m][n] = sum_i a[row(i)][m] b[row(i)][n],      offsets[e] <= i < offsets[e+1].
+//
+// Both operands are dense along the results, so both are transposed on their way out
+// of LDS.  Where the matrices are too few to fill the chip, an expert's rows are
+// split over several workgroups, whose float32 parts expert_grad_join_kernel adds in
+// their order.
+#include "expert_tile.hpp"
+
+namespace lapsum {
+namespace {
+
+template <int DT, class S>
+__device__ __forceinline__ void direct(const GradArgs& a, int lo, int hi, int m0, int n0, int wm, int wn,
+                                       Acc (&acc)[S::TM / 16][S::TN / 16]) {
+  using A = Operand<DT, S::M, true>;
+  using B = Operand<DT, S::N, true>;
+  using raw = typename Elem<DT>::raw;
+  __shared__ __attribute__((aligned(16))) char lds[2 * (A::Bytes + B::Bytes)];
+  constexpr int E = A::E;
+  Direct<A, S::T> da;
+  Direct<B, S::T> db;
+  // A side whose rows follow one another is counted from `lo`; one that comes through
+  // the order finds the rows of a stage a stage ahead.
+  int64_t ahead_a[da.Each], ahead_b[db.Each];
+  const auto look = [&](auto& d, int64_t (&ahead)[std::remove_reference_t<decltype(d)>::Each], int64_t count, int k0) {
+#pragma unroll
+    for (int i = 0; i < d.Each; ++i) {
+      const int r = lo + k0 + d.row(i);
+      ahead[i] = r < hi ? source_row(a.order, a.top_k, count, r) : -1;
+    }
+  };
+  const auto set = [&](auto& d, auto op, const void* p, int64_t count, int64_t stride, bool gather, int first,
+                       int width) {
+    using Op = decltype(op);
+    const int64_t base = gather ? 0 : lo;
+    d.from = buffer_of(static_cast<const raw*>(p) + base * stride, ((count - base - 1) * stride + width) * E);
+    d.step = static_cast<uint32_t>(stride * E);
+#pragma unroll
+    for (int i = 0; i < d.Each; ++i) {
+      const int r = d.row(i), c = first + Op::N * d.chunk(i);
+      d.at[i] = static_cast<uint32_t>((gather ? c : r * stride + c) * E);
+      d.past[i] = c < width ? hi - lo - r : 0;
+    }
+  };
+  set(da, A{}, a.a, a.a_rows, a.a_stride, a.gather == 1, m0, a.m);
+  set(db, B{}, a.b, a.b_rows, a.b_stride, a.gather == 2, n0, a.n);
+  const auto bring_one = [&](auto& d, int64_t (&ahead)[std::remove_reference_t<decltype(d)>::Each], int64_t count,
+                             bool gather, char* lds, int k0) {
+    if (!gather) {
+      d.bring(lds, k0);
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < d.Each; ++i)
+      d.put(lds, i, k0 < d.past[i] && ahead[i] >= 0 ? d.at[i] + static_cast<uint32_t>(ahead[i]) * d.step : kBeyond);
+    look(d, ahead, count, k0 + A::Stage);
+  };
+  if (a.gather == 1) look(da, ahead_a, a.a_rows, 0);
+  if (a.gather == 2) look(db, ahead_b, a.b_rows, 0);
+  const auto bring = [&](char* la, char* lb, int k0) {
+    bring_one(da, ahead_a, a.a_rows, a.gather == 1, la, k0);
+    bring_one(db, ahead_b, a.b_rows, a.gather == 2, lb, k0);
+  };
+  contract<DT, A, B, S>(lds, bring, hi - lo, wm, wn, acc);
+}
+
+template <int DT, class S>
+__device__ __forceinline__ void staged(const GradArgs& a, int lo, int hi, int m0, int n0, int wm, int wn,
+                                       Acc (&acc)[S::TM / 16][S::TN / 16]) {
+  using A = Operand<DT, S::M, true>;
+  using B = Operand<DT, S::N, true>;
+  using raw = typename Elem<DT>::raw;
+  __shared__ __attribute__((aligned(16))) char la[A::Bytes], lb[B::Bytes];
+  Staged<A, S::T> sa;
+  Staged<B, S::T> sb;
+  const auto side = [&](auto& s, const void* p, const int32_t* order, int64_t count, int64_t stride, int r0,
+                        int first, int width) {
+#pragma unroll
+    for (int i = 0; i < s.Each; ++i) {
+      const int r = r0 + s.row(i), c = first + A::N * s.chunk(i);
+      const int64_t src = r < hi ? source_row(order, a.top_k, count, r) : -1;
+      s.v[i] = load_chunk<DT, false>(static_cast<const raw*>(p) + src * stride + c, src < 0 ? 0 : width - c);
+    }
+  };
+  const auto load = [&](int r0) {
+    side(sa, a.a, a.gather == 1 ? a.order : nullptr, a.a_rows, a.a_stride, r0, m0, a.m);
+    side(sb, a.b, a.gather == 2 ? a.order : nullptr, a.b_rows, a.b_stride, r0, n0, a.n);
+  };
+  load(lo);
+  for (int r0 = lo; r0 < hi; r0 += A::Stage) {
+    sa.put(la);
+    sb.put(lb);
+    __syncthreads();
+    if (r0 + A::Stage < hi) load(r0 + A::Stage);
+    multiply<DT, A, B, S>(la, lb, wm, wn, acc);
+    __syncthreads();
+  }
+}
+
+template <int DT, bool DIRECT, class S>
+__global__ __launch_bounds__(S::T, S::M >= 128 ? 2 : 4) void expert_grad_kernel(GradArgs a) {
+  const int tiles_m = (a.m + S::M - 1) / S::M, tiles_n = (a.n + S::N - 1) / S::N;
+  const int tiles = tiles_m * tiles_n;
+  const int block = static_cast<int>(tile_of_block());
+  const int piece = block / tiles, t = block % tiles;
+  const int e = piece / a.splits, split = piece % a.splits;
+  const int m0 = t / tiles_n * S::M, n0 = t % tiles_n * S::N;
+  int lo = e == 0 ? 0 : min(max(a.offsets[e], 0), a.rows);
+  int hi = min(max(a.offsets[e + 1], lo), a.rows);
+  if (a.splits > 1) {   // whole stages each
+    constexpr int stage = 128 / (DT == 0 ? 4 : 2);
+    const int each = ((hi - lo + a.splits - 1) / a.splits + stage - 1) / stage * stage;
+    const int end = hi;
+    lo = static_cast<int>(min(static_cast<int64_t>(end), lo + static_cast<int64_t>(each) * split));
+    hi = min(end, lo + each);
+  }
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int wm = wave / S::WavesN * S::TM, wn = wave % S::WavesN * S::TN;
+  Acc acc[S::TM / 16][S::TN / 16] = {};
+  if constexpr (DIRECT) direct<DT, S>(a, lo, hi, m0, n0, wm, wn, acc);
+  else staged<DT, S>(a, lo, hi, m0, n0, wm, wn, acc);
+  using raw = typename Elem<DT>::raw;
+#pragma unroll
+  for (int i = 0; i < S::TM / 16; ++i) {
+    const int m = m0 + wm + 16 * i + (lane & 15);
+    if (m >= a.m) continue;
+#pragma unroll
+    for (int j = 0; j < S::TN / 16; ++j) {
+      const int n = n0 + wn + 16 * j + 4 * (lane >> 4);
+      if (n >= a.n) continue;
+      if (a.splits > 1)
+        store4<0, DIRECT>(reinterpret_cast<uint32_t*>(a.part) +
+                              ((static_cast<int64_t>(split) * a.experts + e) * a.m + m) * a.n + n,
+                          acc[i][j], a.n - n);
+      else
+        store4<DT, DIRECT>(static_cast<raw*>(a.c) + a.c_expert * e + m * a.c_row + n, acc[i][j], a.n - n);
+    }
+  }
+}
+
+// The splits' parts, added in their order.
+template <int DT>
+__global__ __launch_bounds__(256) void expert_grad_join_kernel(GradArgs a) {
+  const int64_t each = static_cast<int64_t>(a.m) * a.n, total = a.experts * each;
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < total;
+       i += static_cast<int64_t>(gridDim.x) * 256) {
+    float sum = 0.0f;
+#pragma unroll 4
+    for (int s = 0; s < a.splits; ++s) sum += a.part[s * total + i];
+    const int64_t e = i / each, m = (i - e * each) / a.n, n = i - e * each - m * a.n;
+    static_cast<typename Elem<DT>::raw*>(a.c)[a.c_expert * e + m * a.c_row + n] = Elem<DT>::put(sum);
+  }
+}
+
+}  // namespace
+
+// ------------------------------------------------------------- launchers ---
+// How many workgroups share an expert's rows: enough for two of 64 x 64 results per
+// compute unit, as long as each has 256 rows.
+int grad_splits(int64_t experts, int64_t rows, int64_t m, int64_t n) {
+  const int64_t tiles = experts * ((m + 63) / 64) * ((n + 63) / 64);
+  const int64_t most = rows / experts / 256;
+  const int64_t want = (511 + tiles) / tiles;
+  return static_cast<int>(want < most ? (want < 1 ? 1 : want) : (most < 1 ? 1 : most));
+}
+
+hipError_t launch_expert_grad(GradArgs a, int dtype, bool vec, hipStream_t s) {
+  const int64_t size = dtype == 0 ? 4 : 2;
+  const auto spans = [&](int64_t rows, int64_t stride, bool gather) {
+    return (gather ? rows : a.rows + int64_t(1)) * stride * size < kMostBytes;
+  };
+  const bool direct = vec && spans(a.a_rows, a.a_stride, a.gather == 1) && spans(a.b_rows, a.b_stride, a.gather == 2);
+  const auto launch = [&](auto dt, auto way, auto shape) {
+    using S = decltype(shape);
+    const int64_t tiles = static_cast<int64_t>((a.m + S::M - 1) / S::M) * ((a.n + S::N - 1) / S::N);
+    hipLaunchKernelGGL((expert_grad_kernel<decltype(dt)::value, decltype(way)::value, S>),
+                       dim3(static_cast<unsigned>(a.experts * a.splits * tiles)), dim3(S::T), 0, s, a);
+  };
+  const auto shapes = [&](auto dt) {
+    const int64_t tiles = static_cast<int64_t>(a.experts) * ((a.m + 127) / 128) * ((a.n + 127) / 128);
+    const std::true_type yes;
+    const std::false_type no;
+    {
+      ProfScope ps_("expert_grad", s);
+      if (direct && tiles >= 2048 && a.splits == 1) launch(dt, yes, Shape<256, 256, 128, 64>{});
+      else if (direct && tiles >= 512 && a.splits == 1) launch(dt, yes, Shape<128, 128, 64, 64>{});
+      else if (direct) launch(dt, yes, Shape<64, 64, 32, 32>{});
+      else if (tiles >= 512 && a.splits == 1) launch(dt, no, Shape<128, 128, 64, 64>{});
+      else launch(dt, no, Shape<64, 64, 32, 32>{});
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.splits == 1) return e;
+    ProfScope ps_("expert_grad_join", s);
+    const int64_t blocks = (static_cast<int64_t>(a.experts) * a.m * a.n + 255) / 256;
+    hipLaunchKernelGGL((expert_grad_join_kernel<decltype(dt)::value>),
+                       dim3(static_cast<unsigned>(blocks < (1 << 16) ? blocks : (1 << 16))), dim3(256), 0, s, a);
+    return hipGetLastError();
+  };
+  if (dtype == 0) return shapes(std::integral_constant<int, 0>{});
+  if (dtype == 1) return shapes(std::integral_constant<int, 1>{});
+  return shapes(std::integral_constant<int, 2>{});
+}
+
+}  // namespace lapsum

@@ -1,0 +1,207 @@
+// Products grouped by expert: the rows of each expert, consecutive after the order,
+// times the expert's matrix,
+//
+//   y[i][n] = sum_k x[row(i)][k] w_e[k][n],      offsets[e] <= i < offsets[e+1].
+//
+// The gradient of the rows is the same with w read the other way round, so w may
+// be dense along k or along n.  A workgroup computes a tile of one expert's
+// results; which one it finds by itself from the offsets, as the host does not know
+// them.
+#include "expert_tile.hpp"
+
+namespace lapsum {
+namespace {
+
+// The expert and the first row of the t-th tile of `height` rows, experts' tiles one
+// after another, the rows of no expert last.
+struct Tile {
+  int expert;      // experts: rows of none; -1: no such tile
+  int row, end;    // the tile's first row, the end of the expert's
+};
+__device__ __forceinline__ Tile find_tile(const int32_t* offsets, int experts, int rows, int height, int t) {
+  const int lane = lane_id();
+  int before = 0;
+  for (int e0 = 0; e0 <= experts; e0 += kWave) {
+    const int e = e0 + lane;
+    int lo = 0, hi = 0;
+    if (e <= experts) {
+      // (whatever the offsets hold, rows stay rows)
+      lo = e == 0 ? 0 : min(max(offsets[e], 0), rows);
+      hi = e == experts ? rows : min(max(offsets[e + 1], lo), rows);
+    }
+    const int mine = (hi - lo + height - 1) / height;
+    const int upto = before + wave_incl_add(mine);
+    const uint64_t past = __ballot(upto > t);
+    if (past) {
+      const int l = __builtin_ctzll(past);
+      const int first = __builtin_amdgcn_readlane(upto - mine, l);
+      const int row = __builtin_amdgcn_readlane(lo, l) + (t - first) * height;
+      return Tile{e0 + l, row, __builtin_amdgcn_readlane(hi, l)};
+    }
+    before = __builtin_amdgcn_readlane(upto, kWave - 1);
+  }
+  return Tile{-1, 0, 0};
+}
+
+template <int DT, bool N_DENSE, class S>
+struct Product {
+  using A = Operand<DT, S::M, false>;
+  using B = Operand<DT, S::N, N_DENSE>;
+  using raw = typename Elem<DT>::raw;
+};
+
+template <int DT, bool N_DENSE, class S>
+__device__ __forceinline__ void direct(const RowsArgs& a, const Tile& t, int n0, int wm, int wn,
+                                       Acc (&acc)[S::TM / 16][S::TN / 16]) {
+  using P = Product<DT, N_DENSE, S>;
+  using A = typename P::A;
+  using B = typename P::B;
+  __shared__ __attribute__((aligned(16))) char lds[2 * (A::Bytes + B::Bytes)];
+  constexpr int E = A::E;
+  Direct<A, S::T> da;
+  Direct<B, S::T> db;
+  // rows that follow one another are counted from the tile's first
+  const int64_t first = a.order ? 0 : t.row;
+  da.from = buffer_of(static_cast<const typename P::raw*>(a.x) + first * a.x_stride,
+                      ((a.x_rows - first - 1) * a.x_stride + a.k) * E);
+  da.step = E;
+#pragma unroll
+  for (int i = 0; i < da.Each; ++i) {
+    const int r = t.row + da.row(i), k = A::N * da.chunk(i);
+    const int64_t src = r < t.end ? source_row(a.order, a.top_k, a.x_rows, r) : -1;
+    da.at[i] = static_cast<uint32_t>(((src - first) * a.x_stride + k) * E);
+    da.past[i] = src < 0 ? 0 : a.k - k;
+  }
+  const int64_t lines = N_DENSE ? a.k : a.n, length = N_DENSE ? a.n : a.k;
+  db.from = buffer_of(static_cast<const typename P::raw*>(a.w) + a.w_expert * t.expert,
+                      ((lines - 1) * a.w_row + length) * E);
+  db.step = static_cast<uint32_t>(N_DENSE ? a.w_row * E : E);
+#pragma unroll
+  for (int i = 0; i < db.Each; ++i) {
+    const int r = db.row(i), c = B::N * db.chunk(i);
+    const int k = N_DENSE ? r : c, n = n0 + (N_DENSE ? c : r);
+    db.at[i] = static_cast<uint32_t>((N_DENSE ? k * a.w_row + n : n * a.w_row + k) * E);
+    db.past[i] = n < a.n ? a.k - k : 0;
+  }
+  const auto bring = [&](char* la, char* lb, int k0) {
+    da.bring(la, k0);
+    db.bring(lb, k0);
+  };
+  contract<DT, A, B, S>(lds, bring, a.k, wm, wn, acc);
+}
+
+template <int DT, bool N_DENSE, class S>
+__device__ __forceinline__ void staged(const RowsArgs& a, const Tile& t, int n0, int wm, int wn,
+                                       Acc (&acc)[S::TM / 16][S::TN / 16]) {
+  using P = Product<DT, N_DENSE, S>;
+  using A = typename P::A;
+  using B = typename P::B;
+  __shared__ __attribute__((aligned(16))) char la[A::Bytes], lb[B::Bytes];
+  const auto* x = static_cast<const typename P::raw*>(a.x);
+  const auto* w = static_cast<const typename P::raw*>(a.w) + a.w_expert * t.expert;
+  Staged<A, S::T> sa;
+  Staged<B, S::T> sb;
+  int64_t at[sa.Each];
+#pragma unroll
+  for (int i = 0; i < sa.Each; ++i) {
+    const int r = t.row + sa.row(i);
+    const int64_t src = r < t.end ? source_row(a.order, a.top_k, a.x_rows, r) : -1;
+    at[i] = src < 0 ? -1 : src * a.x_stride;
+  }
+  const auto load = [&](int k0) {
+#pragma unroll
+    for (int i = 0; i < sa.Each; ++i) {
+      const int k = k0 + A::N * sa.chunk(i);
+      sa.v[i] = load_chunk<DT, false>(x + at[i] + k, at[i] < 0 ? 0 : a.k - k);
+    }
+#pragma unroll
+    for (int i = 0; i < sb.Each; ++i) {
+      const int r = sb.row(i), c = B::N * sb.chunk(i);
+      const int64_t line = N_DENSE ? k0 + r : n0 + r;
+      const int col = N_DENSE ? n0 + c : k0 + c;
+      const bool in = line < (N_DENSE ? a.k : a.n);
+      sb.v[i] = load_chunk<DT, false>(w + line * a.w_row + col, in ? (N_DENSE ? a.n : a.k) - col : 0);
+    }
+  };
+  load(0);
+  for (int k0 = 0; k0 < a.k; k0 += A::Stage) {
+    sa.put(la);
+    sb.put(lb);
+    __syncthreads();
+    if (k0 + A::Stage < a.k) load(k0 + A::Stage);
+    multiply<DT, A, B, S>(la, lb, wm, wn, acc);
+    __syncthreads();
+  }
+}
+
+template <int DT, int DO, bool N_DENSE, bool DIRECT, class S>
+__global__ __launch_bounds__(S::T, S::M >= 128 ? 2 : 4) void expert_rows_kernel(RowsArgs a) {
+  const int block = static_cast<int>(tile_of_block());
+  const Tile t = find_tile(a.offsets, a.experts, a.rows, S::M, block / a.tiles_n);
+  if (t.expert < 0) return;
+  const int n0 = block % a.tiles_n * S::N;
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int wm = wave / S::WavesN * S::TM, wn = wave % S::WavesN * S::TN;
+  Acc acc[S::TM / 16][S::TN / 16] = {};
+  if (t.expert < a.experts) {
+    if constexpr (DIRECT) direct<DT, N_DENSE, S>(a, t, n0, wm, wn, acc);
+    else staged<DT, N_DENSE, S>(a, t, n0, wm, wn, acc);
+  }
+  using out = typename Elem<DO>::raw;
+#pragma unroll
+  for (int i = 0; i < S::TM / 16; ++i) {
+    const int r = t.row + wm + 16 * i + (lane & 15);
+    if (r >= t.end) continue;
+    out* y = static_cast<out*>(a.y) + static_cast<int64_t>(r) * a.n;
+#pragma unroll
+    for (int j = 0; j < S::TN / 16; ++j) {
+      const int n = n0 + wn + 16 * j + 4 * (lane >> 4);
+      if (n < a.n) store4<DO, DIRECT>(y + n, acc[i][j], a.n - n);
+    }
+  }
+}
+
+}  // namespace
+
+// ------------------------------------------------------------- launchers ---
+hipError_t launch_expert_rows(RowsArgs a, int dtype, bool w_n_dense, bool out_f32, bool vec, hipStream_t s) {
+  const int64_t size = dtype == 0 ? 4 : 2;
+  const bool direct = vec && (a.order ? a.x_rows * a.x_stride : 256 * a.x_stride + a.k) * size < kMostBytes &&
+                      ((w_n_dense ? a.k : a.n) + 1) * a.w_row * size < kMostBytes;
+  ProfScope ps_("expert_rows", s);
+  const auto launch = [&](auto dt, auto dout, auto dense, auto way, auto shape) {
+    using S = decltype(shape);
+    a.tiles_n = (a.n + S::N - 1) / S::N;
+    // an expert's last tile is not full, and neither is that of the rows of none
+    const int64_t most = a.rows / S::M + (a.experts + 1 < a.rows ? a.experts + 1 : a.rows);
+    hipLaunchKernelGGL((expert_rows_kernel<decltype(dt)::value, decltype(dout)::value, decltype(dense)::value,
+                                           decltype(way)::value, S>),
+                       dim3(static_cast<unsigned>(most * a.tiles_n)), dim3(S::T), 0, s, a);
+  };
+  const auto shapes = [&](auto dt, auto dout, auto dense) {
+    const int64_t tiles = (a.rows / 128 + (a.experts < a.rows ? a.experts : a.rows)) * ((a.n + 127) / 128);
+    const std::true_type yes;
+    const std::false_type no;
+    if (direct && tiles >= 4 * 1024 && a.rows / a.experts >= 256)
+      launch(dt, dout, dense, yes, Shape<256, 256, 128, 64>{});
+    else if (direct && tiles >= 512) launch(dt, dout, dense, yes, Shape<128, 128, 64, 64>{});
+    else if (direct) launch(dt, dout, dense, yes, Shape<64, 64, 32, 32>{});
+    else if (tiles >= 512) launch(dt, dout, dense, no, Shape<128, 128, 64, 64>{});
+    else launch(dt, dout, dense, no, Shape<64, 64, 32, 32>{});
+  };
+  const auto types = [&](auto dt, auto dout) {
+    if (w_n_dense) shapes(dt, dout, std::true_type{});
+    else shapes(dt, dout, std::false_type{});
+  };
+  const std::integral_constant<int, 0> f32;
+  const std::integral_constant<int, 1> b16;
+  const std::integral_constant<int, 2> h16;
+  if (dtype == 0) types(f32, f32);
+  else if (dtype == 1 && out_f32) types(b16, f32);
+  else if (dtype == 1) types(b16, b16);
+  else if (out_f32) types(h16, f32);
+  else types(h16, h16);
+  return hipGetLastError();
+}
+
+}  // namespace lapsum

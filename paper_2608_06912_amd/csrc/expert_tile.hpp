@@ -1,0 +1,160 @@
+// What the products grouped by expert share: a workgroup's tile of results, its
+// operands on their way to LDS, and the products of a stage.
+//
+// Two ways to LDS.  Direct: the memory unit writes what it loads to LDS by itself
+// (16 bytes a lane, at the wave's address and on), so a stage is on its way while the
+// one before it is multiplied, in a second buffer, and takes no registers.  Elements
+// that do not exist are asked for beyond the buffer's end, where loads give 0.
+// That needs whole vectors, and operands of less than 4 GiB.  Else: through
+// registers, element by element at the ends.
+#pragma once
+
+#include "matrix.hpp"
+
+namespace lapsum {
+
+// Tiles of M x N results of W waves, each TM x TN of them.
+template <int M_, int N_, int TM_, int TN_>
+struct Shape {
+  static constexpr int M = M_, N = N_, TM = TM_, TN = TN_;
+  static constexpr int WavesN = N / TN, Waves = M / TM * WavesN, T = Waves * kWave;
+};
+
+constexpr uint32_t kBeyond = 0xfffffff0u;   // past the end of every buffer
+constexpr int64_t kMostBytes = (int64_t(1) << 32) - (int64_t(1) << 20);
+
+typedef __amdgpu_buffer_rsrc_t Buffer;
+__device__ __forceinline__ Buffer buffer_of(const void* base, int64_t bytes) {
+  const int64_t n = bytes < 0 ? 0 : bytes < kMostBytes ? bytes : kMostBytes;
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, static_cast<int>(static_cast<uint32_t>(n)),
+                                           0x00020000);
+}
+
+// The chunks of a stage that a thread brings: chunk i of thread t is slot
+// t + T i of the operand in LDS.
+template <class Op, int T>
+struct Chunks {
+  static constexpr int Each = Op::Total / T;
+  static_assert(Op::Total % T == 0, "whole turns");
+  static __device__ __forceinline__ int slot(int i) { return threadIdx.x + T * i; }
+  static __device__ __forceinline__ int row(int i) { return slot(i) / Op::Chunks; }
+  static __device__ __forceinline__ int chunk(int i) { return (slot(i) % Op::Chunks) ^ Op::swizzle(row(i)); }
+};
+
+// An operand on the direct way.  at: where its chunks are at the contraction's
+// start; past: from which element of the contraction on a chunk does not exist.
+template <class Op, int T>
+struct Direct : Chunks<Op, T> {
+  using C = Chunks<Op, T>;
+  Buffer from;
+  uint32_t at[C::Each], step;   // step: bytes of an element of the contraction
+  int past[C::Each];
+  __device__ __forceinline__ void bring(char* lds, int k0) const {
+#pragma unroll
+    for (int i = 0; i < C::Each; ++i) put(lds, i, k0 < past[i] ? at[i] + static_cast<uint32_t>(k0) * step : kBeyond);
+  }
+  __device__ __forceinline__ void put(char* lds, int i, uint32_t offset) const {
+    char* to = lds + 16 * (threadIdx.x / kWave * kWave + T * i);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16,
+                                             static_cast<int>(offset), 0, 0, 0);
+  }
+};
+
+// And through registers.
+template <class Op, int T>
+struct Staged : Chunks<Op, T> {
+  using C = Chunks<Op, T>;
+  Move16 v[C::Each];
+  __device__ __forceinline__ void put(char* lds) const {
+#pragma unroll
+    for (int i = 0; i < C::Each; ++i) *reinterpret_cast<Move16*>(lds + 16 * C::slot(i)) = v[i];
+  }
+};
+
+// The row of the tensor that row i of the order stands for, or -1.
+__device__ __forceinline__ int64_t source_row(const int32_t* order, int top_k, int64_t count, int i) {
+  int64_t r = i;
+  if (order) {
+    const int32_t at = order[i];
+    r = at < 0 ? -1 : at / top_k;
+  }
+  return r < count ? r : -1;
+}
+
+// The products of a stage in LDS: the wave's TM x TN results in tiles of 16 x 16.
+// (b goes first, so that a lane holds four results of one row, side by side)
+template <int DT, class A, class B, class S>
+__device__ __forceinline__ void multiply(const char* __restrict a, const char* __restrict b, int m0, int n0,
+                                         Acc (&acc)[S::TM / 16][S::TN / 16]) {
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    Move16 fa[S::TM / 16], fb[S::TN / 16];
+#pragma unroll
+    for (int i = 0; i < S::TN / 16; ++i) fb[i] = B::fragment(b, n0 + 16 * i, s);
+#pragma unroll
+    for (int i = 0; i < S::TM / 16; ++i) fa[i] = A::fragment(a, m0 + 16 * i, s);
+#pragma unroll
+    for (int i = 0; i < S::TM / 16; ++i)
+#pragma unroll
+      for (int j = 0; j < S::TN / 16; ++j) acc[i][j] = mma<DT>(fb[j], fa[i], acc[i][j]);
+  }
+}
+// The same with the next stage, k0 on, on its way to the other buffer (which none of
+// what is read here is part of: the reads need not wait for it).
+template <int DT, class A, class B, class S, class Bring>
+__device__ __forceinline__ void multiply_and_bring(const char* __restrict now, char* __restrict next, Bring& bring,
+                                                   int k0, int count, int m0, int n0,
+                                                   Acc (&acc)[S::TM / 16][S::TN / 16]) {
+  if (k0 < count) bring(next, next + A::Bytes, k0);
+  multiply<DT, A, B, S>(now, now + A::Bytes, m0, n0, acc);
+}
+
+// The contraction of `count` elements; lds: two buffers for a stage of both operands.
+// bring(lds_a, lds_b, k0) starts a stage's loads.
+template <int DT, class A, class B, class S, class Bring>
+__device__ __forceinline__ void contract(char* lds, Bring& bring, int count, int m0, int n0,
+                                         Acc (&acc)[S::TM / 16][S::TN / 16]) {
+  constexpr int bytes = A::Bytes + B::Bytes;
+  if (count <= 0) return;
+  bring(lds, lds + A::Bytes, 0);
+  int now = 0;
+  for (int k0 = 0; k0 < count; k0 += A::Stage, now ^= 1) {
+    __syncthreads();   // (waits for the loads too)
+    multiply_and_bring<DT, A, B, S>(lds + now * bytes, lds + (now ^ 1) * bytes, bring, k0 + A::Stage, count, m0,
+                                         n0, acc);
+  }
+}
+
+// Four results of a row that lie side by side.
+template <int DT, bool VEC>
+__device__ __forceinline__ void store4(typename Elem<DT>::raw* p, Acc v, int left) {
+  if (VEC && left >= 4) {
+    if constexpr (DT == 0) {
+      *reinterpret_cast<Acc*>(p) = v;
+    } else {
+      Move8 u;
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        u[j] = static_cast<uint32_t>(Elem<DT>::put(v[2 * j])) |
+               (static_cast<uint32_t>(Elem<DT>::put(v[2 * j + 1])) << 16);
+      *reinterpret_cast<Move8*>(p) = u;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (j < left) p[j] = Elem<DT>::put(v[j]);
+  }
+}
+
+// Workgroups are dealt out to the eight dies in turn, each with a cache of its own: in
+// every 256 of them a die takes 32 tiles that follow one another, which share
+// rows and matrices.
+__device__ __forceinline__ uint32_t tile_of_block() {
+  constexpr uint32_t dies = 8, run = 32;
+  const uint32_t b = blockIdx.x, whole = gridDim.x / (dies * run) * (dies * run);
+  if (b >= whole) return b;
+  const uint32_t in = b % (dies * run);
+  return b - in + in % dies * run + in / dies;
+}
+
+}  // namespace lapsum

@@ -112,11 +112,23 @@ int lapsum_expert_matmul(const void* x, int dtype, int64_t x_rows, int64_t x_str
   return LAPSUM_OK;
 }
 
+size_t lapsum_expert_matmul_weights_workspace_size(int64_t experts, int64_t rows, int64_t in, int64_t out) {
+  if (experts < 1 || experts > kExpertMost || rows < 1 || rows > (int64_t(1) << 30) || in < 1 ||
+      in > (int64_t(1) << 24) || out < 1 || out > (int64_t(1) << 24))
+    return 0;
+  const int splits = grad_splits(experts, rows, in, out);
+  if (splits <= 1) return 0;
+  Carve c(nullptr);
+  c.take<float>(static_cast<size_t>(splits * experts) * static_cast<size_t>(in) * static_cast<size_t>(out));
+  return c.size();
+}
+
 int lapsum_expert_matmul_weights(const void* x, int dtype, int64_t x_rows, int64_t x_stride,
                                  const int32_t* order, int64_t top_k, const int32_t* offsets,
                                  int64_t experts, int64_t rows, int64_t in, int64_t out,
                                  const void* grad_y, int64_t grad_stride, void* grad_w,
-                                 const int64_t* w_strides, hipStream_t stream) {
+                                 const int64_t* w_strides, void* workspace,
+                                 size_t workspace_bytes, hipStream_t stream) {
   if (!valid_product(dtype, x_rows, x_stride, order, top_k, experts, rows, in, out) || grad_stride < out)
     return LAPSUM_ERR_INVALID_ARG;
   const Matrices m(w_strides, in, out);
@@ -124,6 +136,9 @@ int lapsum_expert_matmul_weights(const void* x, int dtype, int64_t x_rows, int64
       (experts > 1 && w_strides[0] < (m.out_dense ? (in - 1) * m.row + out : (out - 1) * m.row + in)))
     return LAPSUM_ERR_INVALID_ARG;
   if (experts > kMaxBlocks * 16 / ((in + 63) / 64) / ((out + 63) / 64)) return LAPSUM_ERR_INVALID_ARG;
+  const int wst = check_ws(workspace, workspace_bytes,
+                           lapsum_expert_matmul_weights_workspace_size(experts, rows, in, out));
+  if (wst != LAPSUM_OK) return wst;
   const int dst = check_device();
   if (dst != LAPSUM_OK) return dst;
   GradArgs a{};
@@ -145,6 +160,8 @@ int lapsum_expert_matmul_weights(const void* x, int dtype, int64_t x_rows, int64
   a.rows = static_cast<int>(rows);
   a.experts = static_cast<int>(experts);
   a.top_k = static_cast<int>(top_k);
+  a.splits = rows > 0 ? grad_splits(experts, rows, in, out) : 1;
+  a.part = static_cast<float*>(workspace);
   const int64_t size = size_of(dtype);
   const bool vec = whole_vectors(dtype, bits_of(x) | bits_of(grad_y) | bits_of(grad_w) |
                                  static_cast<uint64_t>((x_stride | grad_stride | w_strides[0] | m.row) * size),

@@ -550,8 +550,10 @@ struct GradArgs {
   const int32_t *order, *offsets;
   int64_t a_rows, b_rows, a_stride, b_stride, c_expert, c_row;
   int rows, m, n, experts, top_k, gather;   // gather: 0 none, 1 of a, 2 of b
-  int tiles_m, tiles_n;
+  int splits;                // grad_splits
+  float* part;               // [splits][experts][m][n], where that is above one
 };
+int grad_splits(int64_t experts, int64_t rows, int64_t m, int64_t n);
 hipError_t launch_expert_grad(GradArgs a, int dtype, bool vec, hipStream_t s);
 
 // ---------------------------------------------------------- paged cache ----

@@ -77,8 +77,8 @@ struct Operand {
 
   static __device__ __forceinline__ int swizzle(int r) {
     if constexpr (!TR) return r & 7;
-    else if constexpr (DT == 0) return ((r >> 2) & 3) << 2;
-    else return ((r & 3) | ((r >> 1) & 4)) << 1;
+    else if constexpr (DT == 0) return (((r >> 2) & 3) << 2) & (Chunks - 1);
+    else return (((r & 3) | ((r >> 1) & 4)) << 1) & (Chunks - 1);
   }
   static __device__ __forceinline__ int slot(int r, int c) { return r * Chunks + (c ^ swizzle(r)); }
 

@@ -19,7 +19,8 @@ from .selection import _count, _device_tensor, _dtype, _expect, _node
 
 __all__ = [
     "lapsum_expert_order_workspace_size", "lapsum_expert_order", "lapsum_expert_matmul",
-    "lapsum_expert_matmul_weights", "lapsum_expert_combine", "lapsum_expert_combine_backward",
+    "lapsum_expert_matmul_weights_workspace_size", "lapsum_expert_matmul_weights",
+    "lapsum_expert_combine", "lapsum_expert_combine_backward",
 ]
 
 _lib = None
@@ -39,8 +40,10 @@ def _load():
     lib.lapsum_expert_matmul.argtypes = [vp, i32, i64, i64, vp, i64, vp, i64, i64, i64, i64, vp, vp, vp,
                                          i32, vp]
     lib.lapsum_expert_matmul.restype = i32
+    lib.lapsum_expert_matmul_weights_workspace_size.argtypes = [i64, i64, i64, i64]
+    lib.lapsum_expert_matmul_weights_workspace_size.restype = sz
     lib.lapsum_expert_matmul_weights.argtypes = [vp, i32, i64, i64, vp, i64, vp, i64, i64, i64, i64, vp,
-                                                 i64, vp, vp, vp]
+                                                 i64, vp, vp, vp, sz, vp]
     lib.lapsum_expert_matmul_weights.restype = i32
     lib.lapsum_expert_combine.argtypes = [vp, i32, i64, i64, vp, vp, i64, i64, vp, i32, vp]
     lib.lapsum_expert_combine.restype = i32
@@ -155,7 +158,11 @@ def lapsum_expert_matmul(x, weight, offsets, *, order=None, top_k: int = 1, dtyp
     return y
 
 
-def lapsum_expert_matmul_weights(x, grad_y, offsets, like, *, order=None, top_k: int = 1):
+def lapsum_expert_matmul_weights_workspace_size(experts: int, rows: int, n_in: int, n_out: int) -> int:
+    return int(_load().lapsum_expert_matmul_weights_workspace_size(experts, rows, n_in, n_out))
+
+
+def lapsum_expert_matmul_weights(x, grad_y, offsets, like, *, order=None, top_k: int = 1, workspace=None):
     """The gradient of lapsum_expert_matmul with respect to its weight, in the
     shape, type and storage of `like` (the weight; strides only are read of it)."""
     torch = _torch()
@@ -178,11 +185,14 @@ def lapsum_expert_matmul_weights(x, grad_y, offsets, like, *, order=None, top_k:
         grad = torch.empty((experts, n_out, n_in), dtype=x.dtype, device=dev).transpose(1, 2)
     else:
         grad = torch.empty((experts, n_in, n_out), dtype=x.dtype, device=dev)
+    ws, nbytes = _workspace(lib.lapsum_expert_matmul_weights_workspace_size(experts, rows, n_in, n_out),
+                            dev, workspace)
     with _on_device(dev):
         _check(lib.lapsum_expert_matmul_weights(
             _ptr(x), code, x.shape[0], stride, _ptr(order), _count(top_k, "top_k"), _ptr(offsets),
             experts, rows, n_in, n_out, _ptr(g), g_stride, _ptr(grad),
-            (ctypes.c_int64 * 3)(*grad.stride()), _stream(dev)), "lapsum_expert_matmul_weights")
+            (ctypes.c_int64 * 3)(*grad.stride()), _ptr(ws), nbytes, _stream(dev)),
+               "lapsum_expert_matmul_weights")
     return grad
 
 

@@ -61,10 +61,20 @@ def test_matmul_refuses(kw):
     dict(g=0), dict(g_stride=15), dict(grad=0), dict(strides=(127, 16, 1)), dict(strides=(128, 2, 16)),
     dict(strides=(100, 1, 8))])
 def test_matmul_weights_refuses(kw):
-    a = dict(PRODUCT, g=P, g_stride=16, grad=P, strides=(128, 16, 1))
+    a = dict(PRODUCT, g=P, g_stride=16, grad=P, strides=(128, 16, 1), ws=0, nbytes=0)
     a.update(kw)
     a["strides"] = _strides(*a["strides"])
     assert E._load().lapsum_expert_matmul_weights(*a.values(), None) == INVALID
+
+
+def test_matmul_weights_workspace():
+    lib = E._load()
+    assert L.lapsum_expert_matmul_weights_workspace_size(64, 10000, 2048, 1024) == 0
+    need = L.lapsum_expert_matmul_weights_workspace_size(2, 20000, 64, 72)
+    assert need > 0 and need % 256 == 0
+    for ws, n in ((0, need), (P, need - 1), (P + 8, need)):
+        assert lib.lapsum_expert_matmul_weights(P, 1, 20000, 64, 0, 1, P, 2, 20000, 64, 72, P, 72, P,
+                                                _strides(64 * 72, 72, 1), ws, n, None) == WORKSPACE
 
 
 @pytest.mark.parametrize("kw", [
