@@ -11,66 +11,82 @@
 namespace lapsum {
 namespace {
 
-template <int DT, class S>
+// A side of the product on the direct way.  One whose rows follow one another is counted
+// from the first, `lo`; one that comes through the order looks the rows of a stage up a
+// stage ahead of their loads.
+template <int DT, class Op, int T, bool GATHER>
+struct Side : Direct<Op, T> {
+  using D = Direct<Op, T>;
+  int32_t place[D::Each];
+  const int32_t* order;
+  int64_t count;
+  Divider by;
+  int lo, hi;
+  __device__ __forceinline__ void look(int k0) {
+#pragma unroll
+    for (int i = 0; i < D::Each; ++i) place[i] = order[min(lo + k0 + D::row(i), hi - 1)];
+  }
+  __device__ __forceinline__ void set(const GradArgs& a, const void* p, int64_t rows, int64_t stride, int first,
+                                      int width, int lo_, int hi_) {
+    constexpr int E = Op::E;
+    lo = lo_;
+    hi = hi_;
+    order = a.order;
+    count = rows;
+    by = a.by;
+    const int64_t base = GATHER ? 0 : lo;
+    D::from = buffer_of(static_cast<const typename Elem<DT>::raw*>(p) + base * stride,
+                        ((rows - base - 1) * stride + width) * E);
+    D::step = static_cast<uint32_t>(stride * E);
+#pragma unroll
+    for (int i = 0; i < D::Each; ++i) {
+      const int r = D::row(i), c = first + Op::N * D::chunk(i);
+      D::at[i] = static_cast<uint32_t>((GATHER ? c : r * stride + c) * E);
+      D::past[i] = c < width ? hi - lo - r : 0;
+    }
+    if constexpr (GATHER) look(0);
+  }
+  __device__ __forceinline__ void bring(char* lds, int k0) {
+    if constexpr (!GATHER) {
+      D::bring(lds, k0);
+    } else {
+      uint32_t to[D::Each];
+#pragma unroll
+      for (int i = 0; i < D::Each; ++i) {
+        const int64_t r = place_row(place[i], by, count);
+        to[i] = k0 < D::past[i] && r >= 0 ? D::at[i] + static_cast<uint32_t>(r) * D::step : kBeyond;
+      }
+      // (the lookups go out before this stage's loads: they are waited for in order)
+      look(k0 + Op::Stage);
+#pragma unroll
+      for (int i = 0; i < D::Each; ++i) D::put(lds, i, to[i]);
+    }
+  }
+};
+
+template <int DT, int GATHER, class S>
 __device__ __forceinline__ void direct(const GradArgs& a, int lo, int hi, int m0, int n0, int wm, int wn,
                                        Acc (&acc)[S::TM / 16][S::TN / 16]) {
-  using A = Operand<DT, S::M, true>;
-  using B = Operand<DT, S::N, true>;
-  using raw = typename Elem<DT>::raw;
-  __shared__ __attribute__((aligned(16))) char lds[2 * (A::Bytes + B::Bytes)];
-  constexpr int E = A::E;
-  Direct<A, S::T> da;
-  Direct<B, S::T> db;
-  // A side whose rows follow one another is counted from `lo`; one that comes through
-  // the order finds the rows of a stage a stage ahead.
-  int64_t ahead_a[da.Each], ahead_b[db.Each];
-  const auto look = [&](auto& d, int64_t (&ahead)[std::remove_reference_t<decltype(d)>::Each], int64_t count, int k0) {
-#pragma unroll
-    for (int i = 0; i < d.Each; ++i) {
-      const int r = lo + k0 + d.row(i);
-      ahead[i] = r < hi ? source_row(a.order, a.top_k, count, r) : -1;
-    }
-  };
-  const auto set = [&](auto& d, auto op, const void* p, int64_t count, int64_t stride, bool gather, int first,
-                       int width) {
-    using Op = decltype(op);
-    const int64_t base = gather ? 0 : lo;
-    d.from = buffer_of(static_cast<const raw*>(p) + base * stride, ((count - base - 1) * stride + width) * E);
-    d.step = static_cast<uint32_t>(stride * E);
-#pragma unroll
-    for (int i = 0; i < d.Each; ++i) {
-      const int r = d.row(i), c = first + Op::N * d.chunk(i);
-      d.at[i] = static_cast<uint32_t>((gather ? c : r * stride + c) * E);
-      d.past[i] = c < width ? hi - lo - r : 0;
-    }
-  };
-  set(da, A{}, a.a, a.a_rows, a.a_stride, a.gather == 1, m0, a.m);
-  set(db, B{}, a.b, a.b_rows, a.b_stride, a.gather == 2, n0, a.n);
-  const auto bring_one = [&](auto& d, int64_t (&ahead)[std::remove_reference_t<decltype(d)>::Each], int64_t count,
-                             bool gather, char* lds, int k0) {
-    if (!gather) {
-      d.bring(lds, k0);
-      return;
-    }
-#pragma unroll
-    for (int i = 0; i < d.Each; ++i)
-      d.put(lds, i, k0 < d.past[i] && ahead[i] >= 0 ? d.at[i] + static_cast<uint32_t>(ahead[i]) * d.step : kBeyond);
-    look(d, ahead, count, k0 + A::Stage);
-  };
-  if (a.gather == 1) look(da, ahead_a, a.a_rows, 0);
-  if (a.gather == 2) look(db, ahead_b, a.b_rows, 0);
+  using A = Operand<DT, S::M, true, S::Steps>;
+  using B = Operand<DT, S::N, true, S::Steps>;
+  __shared__ __attribute__((aligned(16))) char lds[S::Buffers * (A::Bytes + B::Bytes)];
+  if (lo >= hi) return;
+  Side<DT, A, S::T, GATHER == 1> da;
+  Side<DT, B, S::T, GATHER == 2> db;
+  da.set(a, a.a, a.a_rows, a.a_stride, m0, a.m, lo, hi);
+  db.set(a, a.b, a.b_rows, a.b_stride, n0, a.n, lo, hi);
   const auto bring = [&](char* la, char* lb, int k0) {
-    bring_one(da, ahead_a, a.a_rows, a.gather == 1, la, k0);
-    bring_one(db, ahead_b, a.b_rows, a.gather == 2, lb, k0);
+    da.bring(la, k0);
+    db.bring(lb, k0);
   };
-  contract<DT, A, B, S>(lds, bring, hi - lo, wm, wn, acc);
+  contract<DT, A, B, S, Chunks<A, S::T>::Each + Chunks<B, S::T>::Each>(lds, bring, hi - lo, wm, wn, acc);
 }
 
 template <int DT, class S>
 __device__ __forceinline__ void staged(const GradArgs& a, int lo, int hi, int m0, int n0, int wm, int wn,
                                        Acc (&acc)[S::TM / 16][S::TN / 16]) {
-  using A = Operand<DT, S::M, true>;
-  using B = Operand<DT, S::N, true>;
+  using A = Operand<DT, S::M, true, S::Steps>;
+  using B = Operand<DT, S::N, true, S::Steps>;
   using raw = typename Elem<DT>::raw;
   __shared__ __attribute__((aligned(16))) char la[A::Bytes], lb[B::Bytes];
   Staged<A, S::T> sa;
@@ -80,7 +96,7 @@ __device__ __forceinline__ void staged(const GradArgs& a, int lo, int hi, int m0
 #pragma unroll
     for (int i = 0; i < s.Each; ++i) {
       const int r = r0 + s.row(i), c = first + A::N * s.chunk(i);
-      const int64_t src = r < hi ? source_row(order, a.top_k, count, r) : -1;
+      const int64_t src = r < hi ? source_row(order, a.by, count, r) : -1;
       s.v[i] = load_chunk<DT, false>(static_cast<const raw*>(p) + src * stride + c, src < 0 ? 0 : width - c);
     }
   };
@@ -99,7 +115,8 @@ __device__ __forceinline__ void staged(const GradArgs& a, int lo, int hi, int m0
   }
 }
 
-template <int DT, bool DIRECT, class S>
+// WAY: operands straight to LDS, a's or b's through the order (0, 1, 2), or not (-1).
+template <int DT, int WAY, class S>
 __global__ __launch_bounds__(S::T, S::M >= 128 ? 2 : 4) void expert_grad_kernel(GradArgs a) {
   const int tiles_m = (a.m + S::M - 1) / S::M, tiles_n = (a.n + S::N - 1) / S::N;
   const int tiles = tiles_m * tiles_n;
@@ -110,7 +127,7 @@ __global__ __launch_bounds__(S::T, S::M >= 128 ? 2 : 4) void expert_grad_kernel(
   int lo = e == 0 ? 0 : min(max(a.offsets[e], 0), a.rows);
   int hi = min(max(a.offsets[e + 1], lo), a.rows);
   if (a.splits > 1) {   // whole stages each
-    constexpr int stage = 128 / (DT == 0 ? 4 : 2);
+    constexpr int stage = S::Steps * (DT == 0 ? 16 : 32);
     const int each = ((hi - lo + a.splits - 1) / a.splits + stage - 1) / stage * stage;
     const int end = hi;
     lo = static_cast<int>(min(static_cast<int64_t>(end), lo + static_cast<int64_t>(each) * split));
@@ -119,7 +136,8 @@ __global__ __launch_bounds__(S::T, S::M >= 128 ? 2 : 4) void expert_grad_kernel(
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int wm = wave / S::WavesN * S::TM, wn = wave % S::WavesN * S::TN;
   Acc acc[S::TM / 16][S::TN / 16] = {};
-  if constexpr (DIRECT) direct<DT, S>(a, lo, hi, m0, n0, wm, wn, acc);
+  constexpr bool DIRECT = WAY >= 0;
+  if constexpr (DIRECT) direct<DT, WAY, S>(a, lo, hi, m0, n0, wm, wn, acc);
   else staged<DT, S>(a, lo, hi, m0, n0, wm, wn, acc);
   using raw = typename Elem<DT>::raw;
 #pragma unroll
@@ -180,15 +198,19 @@ hipError_t launch_expert_grad(GradArgs a, int dtype, bool vec, hipStream_t s) {
   };
   const auto shapes = [&](auto dt) {
     const int64_t tiles = static_cast<int64_t>(a.experts) * ((a.m + 127) / 128) * ((a.n + 127) / 128);
-    const std::true_type yes;
-    const std::false_type no;
+    const std::integral_constant<int, -1> no;
+    const auto big = [&](auto yes) {
+      if (tiles >= 2048 && a.splits == 1) launch(dt, yes, Shape<256, 256, 128, 64, 1, 4>{});
+      else if (tiles >= 512 && a.splits == 1) launch(dt, yes, Shape<128, 128, 64, 64, 1, 4>{});
+      else launch(dt, yes, Shape<64, 64, 32, 32, 2, 2>{});
+    };
     {
       ProfScope ps_("expert_grad", s);
-      if (direct && tiles >= 2048 && a.splits == 1) launch(dt, yes, Shape<256, 256, 128, 64>{});
-      else if (direct && tiles >= 512 && a.splits == 1) launch(dt, yes, Shape<128, 128, 64, 64>{});
-      else if (direct) launch(dt, yes, Shape<64, 64, 32, 32>{});
-      else if (tiles >= 512 && a.splits == 1) launch(dt, no, Shape<128, 128, 64, 64>{});
-      else launch(dt, no, Shape<64, 64, 32, 32>{});
+      if (direct && a.gather == 0) big(std::integral_constant<int, 0>{});
+      else if (direct && a.gather == 1) big(std::integral_constant<int, 1>{});
+      else if (direct) big(std::integral_constant<int, 2>{});
+      else if (tiles >= 512 && a.splits == 1) launch(dt, no, Shape<128, 128, 64, 64, 2, 1>{});
+      else launch(dt, no, Shape<64, 64, 32, 32, 2, 1>{});
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;

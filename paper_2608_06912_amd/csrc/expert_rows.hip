@@ -45,8 +45,8 @@ __device__ __forceinline__ Tile find_tile(const int32_t* offsets, int experts, i
 
 template <int DT, bool N_DENSE, class S>
 struct Product {
-  using A = Operand<DT, S::M, false>;
-  using B = Operand<DT, S::N, N_DENSE>;
+  using A = Operand<DT, S::M, false, S::Steps>;
+  using B = Operand<DT, S::N, N_DENSE, S::Steps>;
   using raw = typename Elem<DT>::raw;
 };
 
@@ -56,7 +56,7 @@ __device__ __forceinline__ void direct(const RowsArgs& a, const Tile& t, int n0,
   using P = Product<DT, N_DENSE, S>;
   using A = typename P::A;
   using B = typename P::B;
-  __shared__ __attribute__((aligned(16))) char lds[2 * (A::Bytes + B::Bytes)];
+  __shared__ __attribute__((aligned(16))) char lds[S::Buffers * (A::Bytes + B::Bytes)];
   constexpr int E = A::E;
   Direct<A, S::T> da;
   Direct<B, S::T> db;
@@ -68,7 +68,7 @@ __device__ __forceinline__ void direct(const RowsArgs& a, const Tile& t, int n0,
 #pragma unroll
   for (int i = 0; i < da.Each; ++i) {
     const int r = t.row + da.row(i), k = A::N * da.chunk(i);
-    const int64_t src = r < t.end ? source_row(a.order, a.top_k, a.x_rows, r) : -1;
+    const int64_t src = r < t.end ? source_row(a.order, a.by, a.x_rows, r) : -1;
     da.at[i] = static_cast<uint32_t>(((src - first) * a.x_stride + k) * E);
     da.past[i] = src < 0 ? 0 : a.k - k;
   }
@@ -87,7 +87,7 @@ __device__ __forceinline__ void direct(const RowsArgs& a, const Tile& t, int n0,
     da.bring(la, k0);
     db.bring(lb, k0);
   };
-  contract<DT, A, B, S>(lds, bring, a.k, wm, wn, acc);
+  contract<DT, A, B, S, Chunks<A, S::T>::Each + Chunks<B, S::T>::Each>(lds, bring, a.k, wm, wn, acc);
 }
 
 template <int DT, bool N_DENSE, class S>
@@ -105,7 +105,7 @@ __device__ __forceinline__ void staged(const RowsArgs& a, const Tile& t, int n0,
 #pragma unroll
   for (int i = 0; i < sa.Each; ++i) {
     const int r = t.row + sa.row(i);
-    const int64_t src = r < t.end ? source_row(a.order, a.top_k, a.x_rows, r) : -1;
+    const int64_t src = r < t.end ? source_row(a.order, a.by, a.x_rows, r) : -1;
     at[i] = src < 0 ? -1 : src * a.x_stride;
   }
   const auto load = [&](int k0) {
@@ -183,11 +183,11 @@ hipError_t launch_expert_rows(RowsArgs a, int dtype, bool w_n_dense, bool out_f3
     const std::true_type yes;
     const std::false_type no;
     if (direct && tiles >= 4 * 1024 && a.rows / a.experts >= 256)
-      launch(dt, dout, dense, yes, Shape<256, 256, 128, 64>{});
-    else if (direct && tiles >= 512) launch(dt, dout, dense, yes, Shape<128, 128, 64, 64>{});
-    else if (direct) launch(dt, dout, dense, yes, Shape<64, 64, 32, 32>{});
-    else if (tiles >= 512) launch(dt, dout, dense, no, Shape<128, 128, 64, 64>{});
-    else launch(dt, dout, dense, no, Shape<64, 64, 32, 32>{});
+      launch(dt, dout, dense, yes, Shape<256, 256, 128, 64, 1, 4>{});
+    else if (direct && tiles >= 512) launch(dt, dout, dense, yes, Shape<128, 128, 64, 64, 1, 4>{});
+    else if (direct) launch(dt, dout, dense, yes, Shape<64, 64, 32, 32, 2, 2>{});
+    else if (tiles >= 512) launch(dt, dout, dense, no, Shape<128, 128, 64, 64, 2, 1>{});
+    else launch(dt, dout, dense, no, Shape<64, 64, 32, 32, 2, 1>{});
   };
   const auto types = [&](auto dt, auto dout) {
     if (w_n_dense) shapes(dt, dout, std::true_type{});

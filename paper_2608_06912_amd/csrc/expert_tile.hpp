@@ -2,8 +2,8 @@
 // operands on their way to LDS, and the products of a stage.
 //
 // Two ways to LDS.  Direct: the memory unit writes what it loads to LDS by itself
-// (16 bytes a lane, at the wave's address and on), so a stage is on its way while the
-// one before it is multiplied, in a second buffer, and takes no registers.  Elements
+// (16 bytes a lane, at the wave's address and on), so the next stages are on their way
+// while one is multiplied, in buffers of their own, and take no registers.  Elements
 // that do not exist are asked for beyond the buffer's end, where loads give 0.
 // That needs whole vectors, and operands of less than 4 GiB.  Else: through
 // registers, element by element at the ends.
@@ -13,10 +13,11 @@
 
 namespace lapsum {
 
-// Tiles of M x N results of W waves, each TM x TN of them.
-template <int M_, int N_, int TM_, int TN_>
+// Tiles of M x N results of several waves, each TM x TN of them; stages of STEPS steps,
+// BUFFERS of them in LDS where operands go there directly.
+template <int M_, int N_, int TM_, int TN_, int STEPS_, int BUFFERS_>
 struct Shape {
-  static constexpr int M = M_, N = N_, TM = TM_, TN = TN_;
+  static constexpr int M = M_, N = N_, TM = TM_, TN = TN_, Steps = STEPS_, Buffers = BUFFERS_;
   static constexpr int WavesN = N / TN, Waves = M / TM * WavesN, T = Waves * kWave;
 };
 
@@ -71,14 +72,17 @@ struct Staged : Chunks<Op, T> {
   }
 };
 
-// The row of the tensor that row i of the order stands for, or -1.
-__device__ __forceinline__ int64_t source_row(const int32_t* order, int top_k, int64_t count, int i) {
-  int64_t r = i;
-  if (order) {
-    const int32_t at = order[i];
-    r = at < 0 ? -1 : at / top_k;
-  }
-  return r < count ? r : -1;
+// The row of the tensor that a place of the order stands for, or -1: place / top_k by a
+// product with floor(2^shift / top_k) + 1, exact for places below 2^31 (shift = 31 +
+// the bits of top_k - 1).
+__device__ __forceinline__ int64_t place_row(int32_t place, const Divider& by, int64_t count) {
+  const uint64_t q = static_cast<uint64_t>(static_cast<uint32_t>(place)) * by.factor >> by.shift;
+  const int64_t r = static_cast<int64_t>(q);
+  return place >= 0 && r < count ? r : -1;
+}
+__device__ __forceinline__ int64_t source_row(const int32_t* order, const Divider& by, int64_t count, int i) {
+  if (order) return place_row(order[i], by, count);
+  return i < count ? i : -1;
 }
 
 // The products of a stage in LDS: the wave's TM x TN results in tiles of 16 x 16.
@@ -87,7 +91,7 @@ template <int DT, class A, class B, class S>
 __device__ __forceinline__ void multiply(const char* __restrict a, const char* __restrict b, int m0, int n0,
                                          Acc (&acc)[S::TM / 16][S::TN / 16]) {
 #pragma unroll
-  for (int s = 0; s < 2; ++s) {
+  for (int s = 0; s < A::Steps; ++s) {
     Move16 fa[S::TM / 16], fb[S::TN / 16];
 #pragma unroll
     for (int i = 0; i < S::TN / 16; ++i) fb[i] = B::fragment(b, n0 + 16 * i, s);
@@ -99,7 +103,7 @@ __device__ __forceinline__ void multiply(const char* __restrict a, const char* _
       for (int j = 0; j < S::TN / 16; ++j) acc[i][j] = mma<DT>(fb[j], fa[i], acc[i][j]);
   }
 }
-// The same with the next stage, k0 on, on its way to the other buffer (which none of
+// The same with another stage, from k0 on, on its way to another buffer (which none of
 // what is read here is part of: the reads need not wait for it).
 template <int DT, class A, class B, class S, class Bring>
 __device__ __forceinline__ void multiply_and_bring(const char* __restrict now, char* __restrict next, Bring& bring,
@@ -109,19 +113,34 @@ __device__ __forceinline__ void multiply_and_bring(const char* __restrict now, c
   multiply<DT, A, B, S>(now, now + A::Bytes, m0, n0, acc);
 }
 
-// The contraction of `count` elements; lds: two buffers for a stage of both operands.
-// bring(lds_a, lds_b, k0) starts a stage's loads.
-template <int DT, class A, class B, class S, class Bring>
+// All waves have read what they read of LDS, and all but the last N loads of each have
+// arrived.  (Loads arrive in the order of their issue.)
+template <int N>
+__device__ __forceinline__ void arrive() {
+  static_assert(N < 64, "the counter's range");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+// The contraction of `count` elements; lds: S::Buffers stages of both operands.
+// bring(lds_a, lds_b, k0) starts a stage's loads, at least LOADS of them; so once no
+// more than LOADS times the stages after a stage are on their way, it is there.
+template <int DT, class A, class B, class S, int LOADS, class Bring>
 __device__ __forceinline__ void contract(char* lds, Bring& bring, int count, int m0, int n0,
                                          Acc (&acc)[S::TM / 16][S::TN / 16]) {
-  constexpr int bytes = A::Bytes + B::Bytes;
-  if (count <= 0) return;
-  bring(lds, lds + A::Bytes, 0);
-  int now = 0;
-  for (int k0 = 0; k0 < count; k0 += A::Stage, now ^= 1) {
-    __syncthreads();   // (waits for the loads too)
-    multiply_and_bring<DT, A, B, S>(lds + now * bytes, lds + (now ^ 1) * bytes, bring, k0 + A::Stage, count, m0,
-                                         n0, acc);
+  constexpr int bytes = A::Bytes + B::Bytes, ahead = S::Buffers - 1;
+  static_assert(ahead >= 1 && ahead <= 3, "the waits below");
+#pragma unroll
+  for (int s = 0; s < ahead; ++s)
+    if (s * A::Stage < count) bring(lds + s * bytes, lds + s * bytes + A::Bytes, s * A::Stage);
+  int now = 0, next = ahead;
+  for (int k0 = 0; k0 < count; k0 += A::Stage) {
+    if (ahead > 2 && k0 + 2 * A::Stage < count) arrive<2 * LOADS>();
+    else if (ahead > 1 && k0 + A::Stage < count) arrive<LOADS>();
+    else arrive<0>();
+    multiply_and_bring<DT, A, B, S>(lds + now * bytes, lds + next * bytes, bring, k0 + ahead * A::Stage, count, m0,
+                                    n0, acc);
+    now = now + 1 < S::Buffers ? now + 1 : 0;
+    next = next + 1 < S::Buffers ? next + 1 : 0;
   }
 }
 

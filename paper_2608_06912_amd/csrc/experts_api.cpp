@@ -104,7 +104,7 @@ int lapsum_expert_matmul(const void* x, int dtype, int64_t x_rows, int64_t x_str
   a.k = static_cast<int>(in);
   a.n = static_cast<int>(out);
   a.experts = static_cast<int>(experts);
-  a.top_k = static_cast<int>(top_k);
+  a.by = divider(top_k);
   const int64_t size = size_of(dtype);
   const bool vec = whole_vectors(dtype, bits_of(x) | bits_of(w) | bits_of(y) |
                                  static_cast<uint64_t>((x_stride | w_strides[0] | m.row) * size), in | out);
@@ -159,7 +159,7 @@ int lapsum_expert_matmul_weights(const void* x, int dtype, int64_t x_rows, int64
   a.offsets = offsets;
   a.rows = static_cast<int>(rows);
   a.experts = static_cast<int>(experts);
-  a.top_k = static_cast<int>(top_k);
+  a.by = divider(top_k);
   a.splits = rows > 0 ? grad_splits(experts, rows, in, out) : 1;
   a.part = static_cast<float*>(workspace);
   const int64_t size = size_of(dtype);

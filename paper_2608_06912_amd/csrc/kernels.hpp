@@ -532,6 +532,16 @@ struct CombineGradArgs {
 };
 hipError_t launch_expert_combine_backward(const CombineGradArgs& a, int dtype, bool vec, hipStream_t s);
 
+// Division by a number as a product and a shift.
+struct Divider {
+  uint32_t factor;
+  int shift;
+};
+inline Divider divider(int64_t by) {
+  int bits = 0;
+  while ((int64_t(1) << bits) < by) ++bits;
+  return Divider{static_cast<uint32_t>((uint64_t(1) << (31 + bits)) / static_cast<uint64_t>(by) + 1), 31 + bits};
+}
 // Products grouped by expert.  Rows: y[i] = x[row(i)] w_e for the rows of each
 // expert.  Grad: c_e[m][n] = sum over the expert's rows of a[row][m] b[row][n].
 struct RowsArgs {
@@ -540,7 +550,8 @@ struct RowsArgs {
   void* y;                   // [rows, n] dense
   const int32_t *order, *offsets;
   int64_t x_rows, x_stride, w_expert, w_row;   // in elements; w_row: from one dense row to the next
-  int rows, k, n, experts, top_k;
+  Divider by;                // of places by top_k
+  int rows, k, n, experts;
   int tiles_n;               // set by the launcher
 };
 hipError_t launch_expert_rows(RowsArgs a, int dtype, bool w_n_dense, bool out_f32, bool vec, hipStream_t s);
@@ -549,7 +560,8 @@ struct GradArgs {
   void* c;                   // matrices [m, n], n dense
   const int32_t *order, *offsets;
   int64_t a_rows, b_rows, a_stride, b_stride, c_expert, c_row;
-  int rows, m, n, experts, top_k, gather;   // gather: 0 none, 1 of a, 2 of b
+  Divider by;
+  int rows, m, n, experts, gather;   // gather: 0 none, 1 of a, 2 of b
   int splits;                // grad_splits
   float* part;               // [splits][experts][m][n], where that is above one
 };

@@ -1,11 +1,11 @@
 // Tiles of a matrix product on the matrix cores: operands in LDS as chunks of 16
 // bytes, and the fragments of a 16 x 16 tile of results read from them.
 //
-// The contraction goes in stages of 128 bytes (64 elements of 16 bits, 32
-// floats), a stage in two steps of four chunks.  Lane l of a wave holds, of
-// row l & 15, the chunk l >> 4 of a step: eight elements for one 16x16x32
-// instruction, or four floats for four 16x16x4 ones (the order of the
-// contraction is the operands' own business, as long as it is the same for both).
+// The contraction goes in stages of one or two steps of four chunks (32 elements
+// of 16 bits, 16 floats).  Lane l of a wave holds, of row l & 15, the chunk l >> 4
+// of a step: eight elements for one 16x16x32 instruction, or four floats for four
+// 16x16x4 ones (the order of the contraction is the operands' own business, as
+// long as it is the same for both).
 #pragma once
 
 #include "select_common.hpp"
@@ -61,22 +61,23 @@ __device__ __forceinline__ Move16 load_chunk(const typename Elem<DT>::raw* p, in
   return v;
 }
 
-// An operand of R rows in LDS.  Dense along the contraction (TR false): R rows of
-// eight chunks.  Dense along the rows (TR true): a row of R elements for each
+// A stage of an operand of R rows in LDS.  Dense along the contraction (TR false): R rows
+// of four or eight chunks.  Dense along the rows (TR true): a row of R elements for each
 // element of the contraction.  Chunks are permuted within a row by the row's
 // number, so that the lanes that read together meet different banks.
-template <int DT, int R, bool TR>
+template <int DT, int R, bool TR, int STEPS>
 struct Operand {
   static constexpr int E = DT == 0 ? 4 : 2;              // bytes of an element
   static constexpr int N = 16 / E;                       // elements of a chunk
-  static constexpr int Stage = 128 / E;                  // contraction of a stage
+  static constexpr int Steps = STEPS;
+  static constexpr int Stage = STEPS * 4 * N;            // contraction of a stage
   static constexpr int Rows = TR ? Stage : R;
-  static constexpr int Chunks = TR ? R * E / 16 : 8;     // of a row
+  static constexpr int Chunks = TR ? R / N : STEPS * 4;  // of a row
   static constexpr int Total = Rows * Chunks;
   static constexpr int Bytes = Total * 16;
 
   static __device__ __forceinline__ int swizzle(int r) {
-    if constexpr (!TR) return r & 7;
+    if constexpr (!TR) return STEPS == 2 ? r & 7 : (r >> 1) & 3;
     else if constexpr (DT == 0) return (((r >> 2) & 3) << 2) & (Chunks - 1);
     else return (((r & 3) | ((r >> 1) & 4)) << 1) & (Chunks - 1);
   }
