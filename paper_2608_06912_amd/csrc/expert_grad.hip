@@ -88,7 +88,7 @@ __device__ __forceinline__ void staged(const GradArgs& a, int lo, int hi, int m0
   using A = Operand<DT, S::M, true, S::Steps>;
   using B = Operand<DT, S::N, true, S::Steps>;
   using raw = typename Elem<DT>::raw;
-  __shared__ __attribute__((aligned(16))) char la[A::Bytes], lb[B::Bytes];
+  __shared__ __attribute__((aligned(16))) char lds[A::Bytes + B::Bytes];
   Staged<A, S::T> sa;
   Staged<B, S::T> sb;
   const auto side = [&](auto& s, const void* p, const int32_t* order, int64_t count, int64_t stride, int r0,
@@ -106,11 +106,11 @@ __device__ __forceinline__ void staged(const GradArgs& a, int lo, int hi, int m0
   };
   load(lo);
   for (int r0 = lo; r0 < hi; r0 += A::Stage) {
-    sa.put(la);
-    sb.put(lb);
+    sa.put(lds);
+    sb.put(lds + A::Bytes);
     __syncthreads();
     if (r0 + A::Stage < hi) load(r0 + A::Stage);
-    multiply<DT, A, B, S>(la, lb, wm, wn, acc);
+    multiply<DT, A, B, S>(lds, wm, wn, acc);
     __syncthreads();
   }
 }
@@ -200,17 +200,17 @@ hipError_t launch_expert_grad(GradArgs a, int dtype, bool vec, hipStream_t s) {
     const int64_t tiles = static_cast<int64_t>(a.experts) * ((a.m + 127) / 128) * ((a.n + 127) / 128);
     const std::integral_constant<int, -1> no;
     const auto big = [&](auto yes) {
-      if (tiles >= 2048 && a.splits == 1) launch(dt, yes, Shape<256, 256, 128, 64, 1, 4>{});
-      else if (tiles >= 512 && a.splits == 1) launch(dt, yes, Shape<128, 128, 64, 64, 1, 4>{});
-      else launch(dt, yes, Shape<64, 64, 32, 32, 2, 2>{});
+      if (tiles >= 2048 && a.splits == 1) launch(dt, yes, Shape<256, 256, 128, 64, 2>{});
+      else if (tiles >= 512 && a.splits == 1) launch(dt, yes, Shape<128, 128, 64, 64, 2>{});
+      else launch(dt, yes, Shape<64, 64, 32, 32, 2>{});
     };
     {
       ProfScope ps_("expert_grad", s);
       if (direct && a.gather == 0) big(std::integral_constant<int, 0>{});
       else if (direct && a.gather == 1) big(std::integral_constant<int, 1>{});
       else if (direct) big(std::integral_constant<int, 2>{});
-      else if (tiles >= 512 && a.splits == 1) launch(dt, no, Shape<128, 128, 64, 64, 2, 1>{});
-      else launch(dt, no, Shape<64, 64, 32, 32, 2, 1>{});
+      else if (tiles >= 512 && a.splits == 1) launch(dt, no, Shape<128, 128, 64, 64, 1>{});
+      else launch(dt, no, Shape<64, 64, 32, 32, 1>{});
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;

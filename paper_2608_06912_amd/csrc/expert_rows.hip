@@ -96,7 +96,7 @@ __device__ __forceinline__ void staged(const RowsArgs& a, const Tile& t, int n0,
   using P = Product<DT, N_DENSE, S>;
   using A = typename P::A;
   using B = typename P::B;
-  __shared__ __attribute__((aligned(16))) char la[A::Bytes], lb[B::Bytes];
+  __shared__ __attribute__((aligned(16))) char lds[A::Bytes + B::Bytes];
   const auto* x = static_cast<const typename P::raw*>(a.x);
   const auto* w = static_cast<const typename P::raw*>(a.w) + a.w_expert * t.expert;
   Staged<A, S::T> sa;
@@ -125,11 +125,11 @@ __device__ __forceinline__ void staged(const RowsArgs& a, const Tile& t, int n0,
   };
   load(0);
   for (int k0 = 0; k0 < a.k; k0 += A::Stage) {
-    sa.put(la);
-    sb.put(lb);
+    sa.put(lds);
+    sb.put(lds + A::Bytes);
     __syncthreads();
     if (k0 + A::Stage < a.k) load(k0 + A::Stage);
-    multiply<DT, A, B, S>(la, lb, wm, wn, acc);
+    multiply<DT, A, B, S>(lds, wm, wn, acc);
     __syncthreads();
   }
 }
@@ -183,11 +183,11 @@ hipError_t launch_expert_rows(RowsArgs a, int dtype, bool w_n_dense, bool out_f3
     const std::true_type yes;
     const std::false_type no;
     if (direct && tiles >= 4 * 1024 && a.rows / a.experts >= 256)
-      launch(dt, dout, dense, yes, Shape<256, 256, 128, 64, 1, 4>{});
-    else if (direct && tiles >= 512) launch(dt, dout, dense, yes, Shape<128, 128, 64, 64, 1, 4>{});
-    else if (direct) launch(dt, dout, dense, yes, Shape<64, 64, 32, 32, 2, 2>{});
-    else if (tiles >= 512) launch(dt, dout, dense, no, Shape<128, 128, 64, 64, 2, 1>{});
-    else launch(dt, dout, dense, no, Shape<64, 64, 32, 32, 2, 1>{});
+      launch(dt, dout, dense, yes, Shape<256, 256, 128, 64, 2>{});
+    else if (direct && tiles >= 512) launch(dt, dout, dense, yes, Shape<128, 128, 64, 64, 2>{});
+    else if (direct) launch(dt, dout, dense, yes, Shape<64, 64, 32, 32, 2>{});
+    else if (tiles >= 512) launch(dt, dout, dense, no, Shape<128, 128, 64, 64, 1>{});
+    else launch(dt, dout, dense, no, Shape<64, 64, 32, 32, 1>{});
   };
   const auto types = [&](auto dt, auto dout) {
     if (w_n_dense) shapes(dt, dout, std::true_type{});

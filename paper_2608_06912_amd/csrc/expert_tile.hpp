@@ -13,11 +13,11 @@
 
 namespace lapsum {
 
-// Tiles of M x N results of several waves, each TM x TN of them; stages of STEPS steps,
-// BUFFERS of them in LDS where operands go there directly.
-template <int M_, int N_, int TM_, int TN_, int STEPS_, int BUFFERS_>
+// Tiles of M x N results of several waves, each TM x TN of them; BUFFERS stages in LDS
+// where operands go there directly.
+template <int M_, int N_, int TM_, int TN_, int BUFFERS_>
 struct Shape {
-  static constexpr int M = M_, N = N_, TM = TM_, TN = TN_, Steps = STEPS_, Buffers = BUFFERS_;
+  static constexpr int M = M_, N = N_, TM = TM_, TN = TN_, Steps = 2, Buffers = BUFFERS_;
   static constexpr int WavesN = N / TN, Waves = M / TM * WavesN, T = Waves * kWave;
 };
 
@@ -85,32 +85,36 @@ __device__ __forceinline__ int64_t source_row(const int32_t* order, const Divide
   return i < count ? i : -1;
 }
 
-// The products of a stage in LDS: the wave's TM x TN results in tiles of 16 x 16.
-// (b goes first, so that a lane holds four results of one row, side by side)
+// The fragments of a step: those of the wave's TM rows of a and TN of b.
 template <int DT, class A, class B, class S>
-__device__ __forceinline__ void multiply(const char* __restrict a, const char* __restrict b, int m0, int n0,
-                                         Acc (&acc)[S::TM / 16][S::TN / 16]) {
+struct Fragments {
+  static constexpr int MI = S::TM / 16, NI = S::TN / 16;
+  static constexpr int Reads = MI * A::Reads + NI * B::Reads;
+  Move16 a[MI], b[NI];
+  __device__ __forceinline__ void read(const char* __restrict lds, int m0, int n0, int s) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i) b[i] = B::fragment(lds + A::Bytes, n0 + 16 * i, s);
+#pragma unroll
+    for (int i = 0; i < MI; ++i) a[i] = A::fragment(lds, m0 + 16 * i, s);
+  }
+  // (b goes first, so that a lane holds four results of one row, side by side)
+  __device__ __forceinline__ void multiply(Acc (&acc)[MI][NI]) const {
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int j = 0; j < NI; ++j) acc[i][j] = mma<DT>(b[j], a[i], acc[i][j]);
+  }
+};
+
+// Through registers: the products of a stage.
+template <int DT, class A, class B, class S>
+__device__ __forceinline__ void multiply(const char* lds, int m0, int n0, Acc (&acc)[S::TM / 16][S::TN / 16]) {
 #pragma unroll
   for (int s = 0; s < A::Steps; ++s) {
-    Move16 fa[S::TM / 16], fb[S::TN / 16];
-#pragma unroll
-    for (int i = 0; i < S::TN / 16; ++i) fb[i] = B::fragment(b, n0 + 16 * i, s);
-#pragma unroll
-    for (int i = 0; i < S::TM / 16; ++i) fa[i] = A::fragment(a, m0 + 16 * i, s);
-#pragma unroll
-    for (int i = 0; i < S::TM / 16; ++i)
-#pragma unroll
-      for (int j = 0; j < S::TN / 16; ++j) acc[i][j] = mma<DT>(fb[j], fa[i], acc[i][j]);
+    Fragments<DT, A, B, S> f;
+    f.read(lds, m0, n0, s);
+    f.multiply(acc);
   }
-}
-// The same with another stage, from k0 on, on its way to another buffer (which none of
-// what is read here is part of: the reads need not wait for it).
-template <int DT, class A, class B, class S, class Bring>
-__device__ __forceinline__ void multiply_and_bring(const char* __restrict now, char* __restrict next, Bring& bring,
-                                                   int k0, int count, int m0, int n0,
-                                                   Acc (&acc)[S::TM / 16][S::TN / 16]) {
-  if (k0 < count) bring(next, next + A::Bytes, k0);
-  multiply<DT, A, B, S>(now, now + A::Bytes, m0, n0, acc);
 }
 
 // All waves have read what they read of LDS, and all but the last N loads of each have
@@ -121,26 +125,62 @@ __device__ __forceinline__ void arrive() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
+// The schedule of a step: its matrix instructions, with the reads of the next step's
+// fragments spread between them.
+template <int READS, int PRODUCTS>
+__device__ __forceinline__ void spread() {
+  constexpr int each = PRODUCTS / READS > 0 ? PRODUCTS / READS : 1;
+#pragma unroll
+  for (int i = 0; i < READS; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);      // an LDS read
+    __builtin_amdgcn_sched_group_barrier(0x008, each, 0);   // matrix instructions
+  }
+}
+
+// Stage `now` of two steps, the first one's fragments read already; on the way, stage
+// `after` arrives, the loads from k0 on start to `to`, and the first
+// fragments of `after` are read.  What is read is not part of what the loads write: they
+// start behind the barrier after which no wave reads `now`.
+template <int DT, class A, class B, class S, int LOADS, class Bring>
+__device__ __forceinline__ void stage(const char* __restrict now, const char* __restrict after, char* to, Bring& bring,
+                                      int k0, int count, int m0, int n0, Fragments<DT, A, B, S>& first,
+                                      Acc (&acc)[S::TM / 16][S::TN / 16]) {
+  using F = Fragments<DT, A, B, S>;
+  constexpr int products = F::MI * F::NI * (DT == 0 ? 4 : 1);
+  F second;
+  second.read(now, m0, n0, 1);
+  first.multiply(acc);
+  spread<F::Reads, products>();
+  if (S::Buffers > 2 && k0 < count) arrive<LOADS * (S::Buffers - 2)>();
+  else arrive<0>();
+  if (k0 < count) bring(to, to + A::Bytes, k0);
+  first.read(after, m0, n0, 0);
+  second.multiply(acc);
+  spread<F::Reads, products>();
+}
+
 // The contraction of `count` elements; lds: S::Buffers stages of both operands.
 // bring(lds_a, lds_b, k0) starts a stage's loads, at least LOADS of them; so once no
 // more than LOADS times the stages after a stage are on their way, it is there.
 template <int DT, class A, class B, class S, int LOADS, class Bring>
 __device__ __forceinline__ void contract(char* lds, Bring& bring, int count, int m0, int n0,
                                          Acc (&acc)[S::TM / 16][S::TN / 16]) {
-  constexpr int bytes = A::Bytes + B::Bytes, ahead = S::Buffers - 1;
-  static_assert(ahead >= 1 && ahead <= 3, "the waits below");
+  constexpr int bytes = A::Bytes + B::Bytes;
+  static_assert(A::Steps == 2 && S::Buffers >= 2, "stages of two steps");
+  if (count <= 0) return;
 #pragma unroll
-  for (int s = 0; s < ahead; ++s)
+  for (int s = 0; s < S::Buffers; ++s)
     if (s * A::Stage < count) bring(lds + s * bytes, lds + s * bytes + A::Bytes, s * A::Stage);
-  int now = 0, next = ahead;
+  if (count > (S::Buffers - 1) * A::Stage) arrive<LOADS * (S::Buffers - 1)>();
+  else arrive<0>();
+  Fragments<DT, A, B, S> first;
+  first.read(lds, m0, n0, 0);
+  int now = 0;
   for (int k0 = 0; k0 < count; k0 += A::Stage) {
-    if (ahead > 2 && k0 + 2 * A::Stage < count) arrive<2 * LOADS>();
-    else if (ahead > 1 && k0 + A::Stage < count) arrive<LOADS>();
-    else arrive<0>();
-    multiply_and_bring<DT, A, B, S>(lds + now * bytes, lds + next * bytes, bring, k0 + ahead * A::Stage, count, m0,
-                                    n0, acc);
-    now = now + 1 < S::Buffers ? now + 1 : 0;
-    next = next + 1 < S::Buffers ? next + 1 : 0;
+    const int after = now + 1 < S::Buffers ? now + 1 : 0;
+    stage<DT, A, B, S, LOADS>(lds + now * bytes, lds + after * bytes, lds + now * bytes, bring,
+                              k0 + S::Buffers * A::Stage, count, m0, n0, first, acc);
+    now = after;
   }
 }
 

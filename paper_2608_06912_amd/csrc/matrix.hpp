@@ -73,6 +73,7 @@ struct Operand {
   static constexpr int Stage = STEPS * 4 * N;            // contraction of a stage
   static constexpr int Rows = TR ? Stage : R;
   static constexpr int Chunks = TR ? R / N : STEPS * 4;  // of a row
+  static constexpr int Reads = TR ? (DT == 0 ? 4 : 2) : 1;   // of LDS, for a fragment
   static constexpr int Total = Rows * Chunks;
   static constexpr int Bytes = Total * 16;
 
