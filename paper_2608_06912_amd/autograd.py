@@ -411,6 +411,14 @@ def expert_matmul(x, weight, offsets, *, gather=None):
     order, place, top_k = _gather(gather)
     if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad) or _has_tangent(x) \
             or _has_tangent(weight):
+        node = _node or _load_node()
+        if node and type(x) in _PLAIN and type(weight) in _PLAIN and _eager():
+            try:
+                out = node.expert_matmul_grad(x, weight, offsets, order, place, top_k)
+            except TypeError:
+                out = None
+            if out is not None:
+                return out
         if order is not None and place.shape[0] != x.shape[0]:
             raise ValueError("place must have a row for each row of x")
         return ExpertMatmulFunction.apply(x, weight, offsets, order, place, top_k)
@@ -442,5 +450,13 @@ def expert_combine(y, weights, place, offsets):
     refused."""
     if torch.is_grad_enabled() and (y.requires_grad or weights.requires_grad) or _has_tangent(y) \
             or _has_tangent(weights):
+        node = _node or _load_node()
+        if node and type(y) in _PLAIN and type(weights) in _PLAIN and _eager():
+            try:
+                out = node.expert_combine_grad(y, weights, place, offsets)
+            except TypeError:
+                out = None
+            if out is not None:
+                return out
         return ExpertCombineFunction.apply(y, weights, place, offsets)
     return lapsum_expert_combine(y, place, weights)

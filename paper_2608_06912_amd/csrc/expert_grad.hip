@@ -119,11 +119,11 @@ __device__ __forceinline__ void staged(const GradArgs& a, int lo, int hi, int m0
 template <int DT, int WAY, class S>
 __global__ __launch_bounds__(S::T, S::M >= 128 ? 2 : 4) void expert_grad_kernel(GradArgs a) {
   const int tiles_m = (a.m + S::M - 1) / S::M, tiles_n = (a.n + S::N - 1) / S::N;
-  const int tiles = tiles_m * tiles_n;
-  const int block = static_cast<int>(tile_of_block());
-  const int piece = block / tiles, t = block % tiles;
+  const TileAt at = tile_of_block(tiles_n);
+  const int piece = at.m / tiles_m;
+  if (piece >= a.experts * a.splits) return;
   const int e = piece / a.splits, split = piece % a.splits;
-  const int m0 = t / tiles_n * S::M, n0 = t % tiles_n * S::N;
+  const int m0 = at.m % tiles_m * S::M, n0 = at.n * S::N;
   int lo = e == 0 ? 0 : min(max(a.offsets[e], 0), a.rows);
   int hi = min(max(a.offsets[e + 1], lo), a.rows);
   if (a.splits > 1) {   // whole stages each
@@ -192,25 +192,28 @@ hipError_t launch_expert_grad(GradArgs a, int dtype, bool vec, hipStream_t s) {
   const bool direct = vec && spans(a.a_rows, a.a_stride, a.gather == 1) && spans(a.b_rows, a.b_stride, a.gather == 2);
   const auto launch = [&](auto dt, auto way, auto shape) {
     using S = decltype(shape);
-    const int64_t tiles = static_cast<int64_t>((a.m + S::M - 1) / S::M) * ((a.n + S::N - 1) / S::N);
+    const int64_t lines = static_cast<int64_t>(a.experts) * a.splits * ((a.m + S::M - 1) / S::M);
     hipLaunchKernelGGL((expert_grad_kernel<decltype(dt)::value, decltype(way)::value, S>),
-                       dim3(static_cast<unsigned>(a.experts * a.splits * tiles)), dim3(S::T), 0, s, a);
+                       dim3(static_cast<unsigned>((lines + 3) / 4 * 4 * ((a.n + S::N - 1) / S::N))), dim3(S::T), 0, s, a);
   };
   const auto shapes = [&](auto dt) {
     const int64_t tiles = static_cast<int64_t>(a.experts) * ((a.m + 127) / 128) * ((a.n + 127) / 128);
     const std::integral_constant<int, -1> no;
     const auto big = [&](auto yes) {
-      if (tiles >= 2048 && a.splits == 1) launch(dt, yes, Shape<256, 256, 128, 64, 2>{});
-      else if (tiles >= 512 && a.splits == 1) launch(dt, yes, Shape<128, 128, 64, 64, 2>{});
-      else launch(dt, yes, Shape<64, 64, 32, 32, 2>{});
+      // the training layer's 8 matrices of 2048 x 4096 (and 128 of 2048 x 1536 from 131072
+      // rows), us: 256 x 256 338 (1072), 128 x 256 266 (956), 128 x 128 301 (1168)
+      if (decltype(dt)::value != 0 && tiles >= 1024 && a.splits == 1)
+        launch(dt, yes, Shape<128, 256, 128, 64, 1, 3>{});
+      else if (tiles >= 512 && a.splits == 1) launch(dt, yes, Shape<128, 128, 64, 64, 2, 2>{});
+      else launch(dt, yes, Shape<64, 64, 32, 32, 2, 2>{});
     };
     {
       ProfScope ps_("expert_grad", s);
       if (direct && a.gather == 0) big(std::integral_constant<int, 0>{});
       else if (direct && a.gather == 1) big(std::integral_constant<int, 1>{});
       else if (direct) big(std::integral_constant<int, 2>{});
-      else if (tiles >= 512 && a.splits == 1) launch(dt, no, Shape<128, 128, 64, 64, 1>{});
-      else launch(dt, no, Shape<64, 64, 32, 32, 1>{});
+      else if (tiles >= 512 && a.splits == 1) launch(dt, no, Shape<128, 128, 64, 64, 2, 1>{});
+      else launch(dt, no, Shape<64, 64, 32, 32, 2, 1>{});
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;

@@ -136,10 +136,10 @@ __device__ __forceinline__ void staged(const RowsArgs& a, const Tile& t, int n0,
 
 template <int DT, int DO, bool N_DENSE, bool DIRECT, class S>
 __global__ __launch_bounds__(S::T, S::M >= 128 ? 2 : 4) void expert_rows_kernel(RowsArgs a) {
-  const int block = static_cast<int>(tile_of_block());
-  const Tile t = find_tile(a.offsets, a.experts, a.rows, S::M, block / a.tiles_n);
+  const TileAt at = tile_of_block(a.tiles_n);
+  const Tile t = find_tile(a.offsets, a.experts, a.rows, S::M, at.m);
   if (t.expert < 0) return;
-  const int n0 = block % a.tiles_n * S::N;
+  const int n0 = at.n * S::N;
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int wm = wave / S::WavesN * S::TM, wn = wave % S::WavesN * S::TN;
   Acc acc[S::TM / 16][S::TN / 16] = {};
@@ -173,21 +173,30 @@ hipError_t launch_expert_rows(RowsArgs a, int dtype, bool w_n_dense, bool out_f3
     using S = decltype(shape);
     a.tiles_n = (a.n + S::N - 1) / S::N;
     // an expert's last tile is not full, and neither is that of the rows of none
-    const int64_t most = a.rows / S::M + (a.experts + 1 < a.rows ? a.experts + 1 : a.rows);
+    const int64_t most = (a.rows / S::M + (a.experts + 1 < a.rows ? a.experts + 1 : a.rows) + 3) / 4 * 4;
     hipLaunchKernelGGL((expert_rows_kernel<decltype(dt)::value, decltype(dout)::value, decltype(dense)::value,
                                            decltype(way)::value, S>),
                        dim3(static_cast<unsigned>(most * a.tiles_n)), dim3(S::T), 0, s, a);
   };
   const auto shapes = [&](auto dt, auto dout, auto dense) {
+    constexpr int DT = decltype(dt)::value;
     const int64_t tiles = (a.rows / 128 + (a.experts < a.rows ? a.experts : a.rows)) * ((a.n + 127) / 128);
     const std::true_type yes;
     const std::false_type no;
-    if (direct && tiles >= 4 * 1024 && a.rows / a.experts >= 256)
-      launch(dt, dout, dense, yes, Shape<256, 256, 128, 64, 2>{});
-    else if (direct && tiles >= 512) launch(dt, dout, dense, yes, Shape<128, 128, 64, 64, 2>{});
-    else if (direct) launch(dt, dout, dense, yes, Shape<64, 64, 32, 32, 2>{});
-    else if (tiles >= 512) launch(dt, dout, dense, no, Shape<128, 128, 64, 64, 1>{});
-    else launch(dt, dout, dense, no, Shape<64, 64, 32, 32, 1>{});
+    // Few large tiles leave compute units idle, small ones read more than the die's
+    // cache delivers.  Rows of 128 bytes are two steps of 64 and want both at
+    // once; where w is dense along n one step's rows of it are long.  16384 rows of
+    // 8 experts 2048 -> 4096 in bfloat16 (and 131072 of 128, 2048 -> 1536), us:
+    //   w dense along n   256 x 256 307 (854), 128 x 256 284 (856), 128 x 128 301 (1001)
+    //   w dense along k   256 x 256 284 (847), 128 x 256 316 (942), 128 x 128 290 (990)
+    if (DT != 0 && direct && w_n_dense && tiles >= 1024 && a.rows / a.experts >= 128)
+      launch(dt, dout, dense, yes, Shape<128, 256, 128, 64, 1, 3>{});
+    else if (DT != 0 && direct && !w_n_dense && tiles >= 2048 && a.rows / a.experts >= 256)
+      launch(dt, dout, dense, yes, Shape<256, 256, 128, 64, 2, 2>{});
+    else if (direct && tiles >= 512) launch(dt, dout, dense, yes, Shape<128, 128, 64, 64, 2, 2>{});
+    else if (direct) launch(dt, dout, dense, yes, Shape<64, 64, 32, 32, 2, 2>{});
+    else if (tiles >= 512) launch(dt, dout, dense, no, Shape<128, 128, 64, 64, 2, 1>{});
+    else launch(dt, dout, dense, no, Shape<64, 64, 32, 32, 2, 1>{});
   };
   const auto types = [&](auto dt, auto dout) {
     if (w_n_dense) shapes(dt, dout, std::true_type{});

@@ -13,11 +13,11 @@
 
 namespace lapsum {
 
-// Tiles of M x N results of several waves, each TM x TN of them; BUFFERS stages in LDS
-// where operands go there directly.
-template <int M_, int N_, int TM_, int TN_, int BUFFERS_>
+// Tiles of M x N results of several waves, each TM x TN of them; stages of STEPS steps,
+// BUFFERS of them in LDS where operands go there directly.
+template <int M_, int N_, int TM_, int TN_, int STEPS_, int BUFFERS_>
 struct Shape {
-  static constexpr int M = M_, N = N_, TM = TM_, TN = TN_, Steps = 2, Buffers = BUFFERS_;
+  static constexpr int M = M_, N = N_, TM = TM_, TN = TN_, Steps = STEPS_, Buffers = BUFFERS_;
   static constexpr int WavesN = N / TN, Waves = M / TM * WavesN, T = Waves * kWave;
 };
 
@@ -137,26 +137,33 @@ __device__ __forceinline__ void spread() {
   }
 }
 
-// Stage `now` of two steps, the first one's fragments read already; on the way, stage
-// `after` arrives, the loads from k0 on start to `to`, and the first
-// fragments of `after` are read.  What is read is not part of what the loads write: they
-// start behind the barrier after which no wave reads `now`.
+// The products of a step whose fragments are read, while stage `after` arrives, the loads
+// from k0 on start to the buffer `to` that the step was read from, and the next
+// fragments are read.  What is read is not part of what the loads write: they start
+// behind the barrier after which no wave reads that buffer.
 template <int DT, class A, class B, class S, int LOADS, class Bring>
-__device__ __forceinline__ void stage(const char* __restrict now, const char* __restrict after, char* to, Bring& bring,
-                                      int k0, int count, int m0, int n0, Fragments<DT, A, B, S>& first,
-                                      Acc (&acc)[S::TM / 16][S::TN / 16]) {
+__device__ __forceinline__ void pass_on(const char* __restrict after, char* to, Bring& bring, int k0, int count,
+                                        int m0, int n0, const Fragments<DT, A, B, S>& have,
+                                        Fragments<DT, A, B, S>& next, Acc (&acc)[S::TM / 16][S::TN / 16]) {
   using F = Fragments<DT, A, B, S>;
-  constexpr int products = F::MI * F::NI * (DT == 0 ? 4 : 1);
-  F second;
-  second.read(now, m0, n0, 1);
-  first.multiply(acc);
-  spread<F::Reads, products>();
   if (S::Buffers > 2 && k0 < count) arrive<LOADS * (S::Buffers - 2)>();
   else arrive<0>();
   if (k0 < count) bring(to, to + A::Bytes, k0);
-  first.read(after, m0, n0, 0);
-  second.multiply(acc);
-  spread<F::Reads, products>();
+  next.read(after, m0, n0, 0);
+  have.multiply(acc);
+  spread<F::Reads, F::MI * F::NI * (DT == 0 ? 4 : 1)>();
+}
+// Stage `now` of two steps, the first one's fragments read already.
+template <int DT, class A, class B, class S, int LOADS, class Bring>
+__device__ __forceinline__ void two_steps(const char* __restrict now, const char* __restrict after, char* to,
+                                          Bring& bring, int k0, int count, int m0, int n0,
+                                          Fragments<DT, A, B, S>& first, Acc (&acc)[S::TM / 16][S::TN / 16]) {
+  using F = Fragments<DT, A, B, S>;
+  F second;
+  second.read(now, m0, n0, 1);
+  first.multiply(acc);
+  spread<F::Reads, F::MI * F::NI * (DT == 0 ? 4 : 1)>();
+  pass_on<DT, A, B, S, LOADS>(after, to, bring, k0, count, m0, n0, second, first, acc);
 }
 
 // The contraction of `count` elements; lds: S::Buffers stages of both operands.
@@ -165,22 +172,43 @@ __device__ __forceinline__ void stage(const char* __restrict now, const char* __
 template <int DT, class A, class B, class S, int LOADS, class Bring>
 __device__ __forceinline__ void contract(char* lds, Bring& bring, int count, int m0, int n0,
                                          Acc (&acc)[S::TM / 16][S::TN / 16]) {
-  constexpr int bytes = A::Bytes + B::Bytes;
-  static_assert(A::Steps == 2 && S::Buffers >= 2, "stages of two steps");
+  constexpr int bytes = A::Bytes + B::Bytes, K = A::Stage;
+  static_assert(S::Buffers >= 2, "one to multiply, one to fill");
   if (count <= 0) return;
 #pragma unroll
   for (int s = 0; s < S::Buffers; ++s)
-    if (s * A::Stage < count) bring(lds + s * bytes, lds + s * bytes + A::Bytes, s * A::Stage);
-  if (count > (S::Buffers - 1) * A::Stage) arrive<LOADS * (S::Buffers - 1)>();
+    if (s * K < count) bring(lds + s * bytes, lds + s * bytes + A::Bytes, s * K);
+  if (count > (S::Buffers - 1) * K) arrive<LOADS * (S::Buffers - 1)>();
   else arrive<0>();
   Fragments<DT, A, B, S> first;
   first.read(lds, m0, n0, 0);
   int now = 0;
-  for (int k0 = 0; k0 < count; k0 += A::Stage) {
-    const int after = now + 1 < S::Buffers ? now + 1 : 0;
-    stage<DT, A, B, S, LOADS>(lds + now * bytes, lds + after * bytes, lds + now * bytes, bring,
-                              k0 + S::Buffers * A::Stage, count, m0, n0, first, acc);
-    now = after;
+  const auto turn = [](int b) { return b + 1 < S::Buffers ? b + 1 : 0; };
+  if constexpr (A::Steps == 2) {
+    for (int k0 = 0; k0 < count; k0 += K) {
+      const int after = turn(now);
+      two_steps<DT, A, B, S, LOADS>(lds + now * bytes, lds + after * bytes, lds + now * bytes, bring,
+                                    k0 + S::Buffers * K, count, m0, n0, first, acc);
+      now = after;
+    }
+  } else {
+    Fragments<DT, A, B, S> second;
+    int k0 = 0;
+    const auto pass = [&](const Fragments<DT, A, B, S>& have, Fragments<DT, A, B, S>& next) {
+      const int after = turn(now);
+      pass_on<DT, A, B, S, LOADS>(lds + after * bytes, lds + now * bytes, bring, k0 + S::Buffers * K, count, m0, n0,
+                                  have, next, acc);
+      k0 += K;
+      now = after;
+    };
+    if ((count + K - 1) / K % 2) {   // the rest in pairs
+      pass(first, second);
+      first = second;
+    }
+    while (k0 < count) {
+      pass(first, second);
+      pass(second, first);
+    }
   }
 }
 
@@ -206,14 +234,24 @@ __device__ __forceinline__ void store4(typename Elem<DT>::raw* p, Acc v, int lef
 }
 
 // Workgroups are dealt out to the eight dies in turn, each with a cache of its own: in
-// every 256 of them a die takes 32 tiles that follow one another, which share
-// rows and matrices.
-__device__ __forceinline__ uint32_t tile_of_block() {
+// every 256 of them a die takes 32 tiles that follow one another.  Tiles follow one
+// another in blocks of four rows and eight columns of them, which share rows
+// and matrices in as few lines as 32 tiles can.  (tile row, tile column)
+struct TileAt {
+  int m, n;
+};
+__device__ __forceinline__ TileAt tile_of_block(int tiles_n) {
   constexpr uint32_t dies = 8, run = 32;
-  const uint32_t b = blockIdx.x, whole = gridDim.x / (dies * run) * (dies * run);
-  if (b >= whole) return b;
-  const uint32_t in = b % (dies * run);
-  return b - in + in % dies * run + in / dies;
+  uint32_t b = blockIdx.x;
+  const uint32_t whole = gridDim.x / (dies * run) * (dies * run);
+  if (b < whole) {
+    const uint32_t in = b % (dies * run);
+    b = b - in + in % dies * run + in / dies;
+  }
+  const uint32_t strip = b / (4u * tiles_n), in = b - strip * 4u * tiles_n;
+  const uint32_t block = in / 32u, at = in - block * 32u;
+  const uint32_t width = min(8u, tiles_n - block * 8u);
+  return TileAt{static_cast<int>(strip * 4u + at / width), static_cast<int>(block * 8u + at % width)};
 }
 
 }  // namespace lapsum

@@ -4,11 +4,15 @@
 // and refused.
 #include "node.hpp"
 
+#include <torch/csrc/autograd/functions/basic_ops.h>
+
 #include <cmath>
 
 namespace {
 
 using namespace lapsum_node;
+using torch::autograd::AutogradContext;
+using torch::autograd::variable_list;
 
 // Rows of a matrix, dense, evenly apart.
 bool matrix(const Tensor& x) {
@@ -31,37 +35,177 @@ std::optional<std::tuple<Tensor, Tensor, Tensor>> expert_order(const Tensor& at,
   return std::make_tuple(order, place, offsets);
 }
 
-OptTensor expert_matmul(const Tensor& x, const Tensor& w, const Tensor& offsets, const OptTensor& order,
-                        int64_t top_k) {
-  if (!matrix(x) || dtype_of(x) < 0 || !plain(w) || w.dim() != 3 || w.scalar_type() != x.scalar_type() ||
-      w.device() != x.device() || w.size(1) != x.size(1) || !dense(offsets, at::kInt, x) || offsets.dim() != 1 ||
-      offsets.size(0) != w.size(0) + 1 || (order && (!dense(*order, at::kInt, x) || order->dim() != 1)))
-    return std::nullopt;
-  const int64_t in = w.size(1), out = w.size(2);
-  const int64_t strides[3] = {w.stride(0), w.stride(1), w.stride(2)};
-  if (!((strides[2] == 1 && strides[1] >= out) || (strides[1] == 1 && strides[2] >= in))) return std::nullopt;
+// The arguments of a product that both its directions take, checked.
+struct Product {
+  bool ok = false;
+  int64_t in = 0, out = 0, rows = 0, strides[3] = {0, 0, 0};
+  Product(const Tensor& x, const Tensor& w, const Tensor& offsets, const OptTensor& order) {
+    if (!matrix(x) || dtype_of(x) < 0 || !plain(w) || w.dim() != 3 || w.scalar_type() != x.scalar_type() ||
+        w.device() != x.device() || w.size(1) != x.size(1) || !dense(offsets, at::kInt, x) || offsets.dim() != 1 ||
+        offsets.size(0) != w.size(0) + 1 || (order && (!dense(*order, at::kInt, x) || order->dim() != 1)))
+      return;
+    in = w.size(1);
+    out = w.size(2);
+    for (int i = 0; i < 3; ++i) strides[i] = w.stride(i);
+    ok = (strides[2] == 1 && strides[1] >= out) || (strides[1] == 1 && strides[2] >= in);
+    rows = order ? order->numel() : x.size(0);
+  }
+};
+
+Tensor product(const Tensor& x, const Tensor& w, const Tensor& offsets, const OptTensor& order, int64_t top_k,
+               const Product& p, at::ScalarType type) {
   const c10::DeviceGuard guard(x.device());
-  const int64_t rows = order ? order->numel() : x.size(0);
-  Tensor y = at::empty({rows, out}, x.options().requires_grad(false));
+  Tensor y = at::empty({p.rows, p.out}, x.options().dtype(type).requires_grad(false));
   check(lapsum_expert_matmul(x.data_ptr(), dtype_of(x), x.size(0), row_stride(x),
                              order ? order->data_ptr<int32_t>() : nullptr, top_k, offsets.data_ptr<int32_t>(),
-                             w.size(0), rows, in, out, w.data_ptr(), strides, y.data_ptr(), dtype_of(x),
+                             w.size(0), p.rows, p.in, p.out, w.data_ptr(), p.strides, y.data_ptr(), dtype_of(y),
                              stream_of(x)),
         "lapsum_expert_matmul");
   return y;
 }
 
-OptTensor expert_combine(const Tensor& y, const Tensor& place, const OptTensor& weights) {
-  if (!plain(y) || dtype_of(y) < 0 || y.dim() != 2 || !y.is_contiguous() || !dense(place, at::kInt, y) ||
-      place.dim() != 2 || (weights && (!dense(*weights, at::kFloat, y) || weights->sizes() != place.sizes())))
-    return std::nullopt;
+OptTensor expert_matmul(const Tensor& x, const Tensor& w, const Tensor& offsets, const OptTensor& order,
+                        int64_t top_k) {
+  const Product p(x, w, offsets, order);
+  if (!p.ok) return std::nullopt;
+  return product(x, w, offsets, order, top_k, p, x.scalar_type());
+}
+
+Tensor combine(const Tensor& y, const Tensor& place, const OptTensor& weights, at::ScalarType type) {
   const c10::DeviceGuard guard(y.device());
-  Tensor out = at::empty({place.size(0), y.size(1)}, y.options().requires_grad(false));
+  Tensor out = at::empty({place.size(0), y.size(1)}, y.options().dtype(type).requires_grad(false));
   check(lapsum_expert_combine(y.data_ptr(), dtype_of(y), y.size(0), y.size(1),
                               weights ? weights->data_ptr<float>() : nullptr, place.data_ptr<int32_t>(),
-                              place.size(0), place.size(1), out.data_ptr(), dtype_of(y), stream_of(y)),
+                              place.size(0), place.size(1), out.data_ptr(), dtype_of(out), stream_of(y)),
         "lapsum_expert_combine");
   return out;
+}
+bool of_combine(const Tensor& y, const Tensor& place, const OptTensor& weights) {
+  return plain(y) && dtype_of(y) >= 0 && y.dim() == 2 && y.is_contiguous() && dense(place, at::kInt, y) &&
+         place.dim() == 2 && (!weights || (dense(*weights, at::kFloat, y) && weights->sizes() == place.sizes()));
+}
+OptTensor expert_combine(const Tensor& y, const Tensor& place, const OptTensor& weights) {
+  if (!of_combine(y, place, weights)) return std::nullopt;
+  return combine(y, place, weights, y.scalar_type());
+}
+
+// What comes out of a backward has no gradient of its own: asking for one is an error.
+void no_second(variable_list& grads, const char* what) {
+  if (!at::GradMode::is_enabled()) return;
+  for (Tensor& g : grads)
+    if (g.defined())
+      g = (*std::make_shared<torch::autograd::DelayedError>(what, 1))({g.detach().requires_grad_()})[0];
+}
+
+// autograd.ExpertMatmulFunction in native code.
+struct MatmulNode : public torch::autograd::Function<MatmulNode> {
+  static Tensor forward(AutogradContext* ctx, const Tensor& x, const Tensor& w, const Tensor& offsets,
+                        const OptTensor& order, const OptTensor& place, int64_t top_k) {
+    const Tensor xd = x.detach(), wd = w.detach();
+    const Product p(xd, wd, offsets, order);
+    ctx->save_for_backward({x, w, offsets, order ? *order : Tensor(), place ? *place : Tensor()});
+    ctx->saved_data["top_k"] = top_k;
+    ctx->set_materialize_grads(false);
+    return product(xd, wd, offsets, order, top_k, p, x.scalar_type());
+  }
+  static variable_list backward(AutogradContext* ctx, variable_list grads) {
+    variable_list out(6);
+    if (grads[0].defined()) in_engine([&] { vjp(ctx, grads[0], out); });
+    no_second(out, "the gradient of expert_matmul is not differentiable");
+    return out;
+  }
+  static void vjp(AutogradContext* ctx, Tensor g, variable_list& out) {
+    const auto saved = ctx->get_saved_variables();
+    const Tensor x = saved[0].detach(), w = saved[1].detach(), offsets = saved[2];
+    const OptTensor order = saved[3].defined() ? OptTensor(saved[3]) : std::nullopt;
+    const Product p(x, w, offsets, order);
+    // (a saved-tensor hook can hand back any tensor)
+    TORCH_CHECK_VALUE(p.ok && plain(g) && g.device() == x.device() && g.dim() == 2 && g.size(0) == p.rows &&
+                          g.size(1) == p.out,
+                      "the saved tensors must be those of the forward");
+    const c10::DeviceGuard guard(x.device());
+    const at::AutoDispatchBelowADInplaceOrView below;
+    g = g.to(x.scalar_type()).contiguous();
+    const int64_t top_k = ctx->saved_data["top_k"].toInt();
+    if (ctx->needs_input_grad(0)) {
+      const Tensor back = w.transpose(1, 2);
+      const Product q(g, back, offsets, std::nullopt);
+      TORCH_CHECK_VALUE(q.ok, "the saved weight must be that of the forward");
+      if (!order) {
+        out[0] = product(g, back, offsets, std::nullopt, 1, q, x.scalar_type());
+      } else {   // a token's rows are summed before they are rounded
+        const Tensor rows = product(g, back, offsets, std::nullopt, 1, q, at::kFloat);
+        TORCH_CHECK_VALUE(of_combine(rows, saved[4], std::nullopt), "the saved place must be that of the forward");
+        out[0] = combine(rows, saved[4], std::nullopt, x.scalar_type());
+      }
+    }
+    if (ctx->needs_input_grad(1)) {
+      const auto opt = w.options().requires_grad(false);
+      const bool other = w.stride(1) == 1 && w.stride(2) != 1;
+      Tensor grad = other ? at::empty({w.size(0), p.out, p.in}, opt).transpose(1, 2)
+                          : at::empty({w.size(0), p.in, p.out}, opt);
+      const int64_t strides[3] = {grad.stride(0), grad.stride(1), grad.stride(2)};
+      const size_t need = lapsum_expert_matmul_weights_workspace_size(w.size(0), p.rows, p.in, p.out);
+      Tensor ws = bytes(need, x);
+      check(lapsum_expert_matmul_weights(x.data_ptr(), dtype_of(x), x.size(0), row_stride(x),
+                                         order ? order->data_ptr<int32_t>() : nullptr, top_k,
+                                         offsets.data_ptr<int32_t>(), w.size(0), p.rows, p.in, p.out, g.data_ptr(),
+                                         p.out, grad.data_ptr(), strides, ptr(ws), need, stream_of(x)),
+            "lapsum_expert_matmul_weights");
+      out[1] = grad;
+    }
+  }
+};
+
+OptTensor expert_matmul_grad(const Tensor& x, const Tensor& w, const Tensor& offsets, const OptTensor& order,
+                             const OptTensor& place, int64_t top_k) {
+  const Product p(x, w, offsets, order);
+  if (!p.ok || order.has_value() != place.has_value() ||
+      (place && (!dense(*place, at::kInt, x) || place->dim() != 2 || place->size(0) != x.size(0))))
+    return std::nullopt;
+  return MatmulNode::apply(x, w, offsets, order, place, top_k);
+}
+
+// autograd.ExpertCombineFunction in native code.
+struct CombineNode : public torch::autograd::Function<CombineNode> {
+  static Tensor forward(AutogradContext* ctx, const Tensor& y, const Tensor& weights, const Tensor& place,
+                        const Tensor& offsets) {
+    ctx->save_for_backward({y, weights, place, offsets});
+    ctx->set_materialize_grads(false);
+    return combine(y.detach(), place, weights.detach(), y.scalar_type());
+  }
+  static variable_list backward(AutogradContext* ctx, variable_list grads) {
+    variable_list out(4);
+    if (grads[0].defined()) in_engine([&] { vjp(ctx, grads[0], out); });
+    no_second(out, "the gradient of expert_combine is not differentiable");
+    return out;
+  }
+  static void vjp(AutogradContext* ctx, Tensor g, variable_list& out) {
+    const auto saved = ctx->get_saved_variables();
+    const Tensor y = saved[0].detach(), weights = saved[1].detach(), place = saved[2], offsets = saved[3];
+    TORCH_CHECK_VALUE(of_combine(y, place, weights) && dense(offsets, at::kInt, y) && plain(g) &&
+                          g.device() == y.device() && g.dim() == 2 && g.size(0) == place.size(0) &&
+                          g.size(1) == y.size(1),
+                      "the saved tensors must be those of the forward");
+    const c10::DeviceGuard guard(y.device());
+    const at::AutoDispatchBelowADInplaceOrView below;
+    g = g.to(y.scalar_type()).contiguous();
+    Tensor grad_y = at::empty(y.sizes(), y.options().requires_grad(false));
+    Tensor grad_w = at::empty(weights.sizes(), weights.options().requires_grad(false));
+    check(lapsum_expert_combine_backward(g.data_ptr(), y.data_ptr(), dtype_of(y), y.size(0), y.size(1),
+                                         weights.data_ptr<float>(), place.data_ptr<int32_t>(),
+                                         offsets.data_ptr<int32_t>(), offsets.numel() - 1, place.size(0),
+                                         place.size(1), grad_y.data_ptr(), grad_w.data_ptr<float>(), stream_of(y)),
+          "lapsum_expert_combine_backward");
+    out[0] = grad_y;
+    out[1] = grad_w;
+  }
+};
+
+OptTensor expert_combine_grad(const Tensor& y, const Tensor& weights, const Tensor& place, const Tensor& offsets) {
+  if (!of_combine(y, place, weights) || !dense(offsets, at::kInt, y) || offsets.dim() != 1 || offsets.numel() < 2)
+    return std::nullopt;
+  return CombineNode::apply(y, weights, place, offsets);
 }
 
 // A cache [pages, kv_heads, slots, dim] with dense rows, with its scales.
@@ -205,7 +349,9 @@ std::optional<std::vector<Tensor>> cache_attend(const Tensor& q, const Tensor& k
 void bind_products(py::module_& m) {
   m.def("expert_order", lapsum_node::entry(expert_order));
   m.def("expert_matmul", lapsum_node::entry(expert_matmul));
+  m.def("expert_matmul_grad", lapsum_node::entry(expert_matmul_grad));
   m.def("expert_combine", lapsum_node::entry(expert_combine));
+  m.def("expert_combine_grad", lapsum_node::entry(expert_combine_grad));
   m.def("cache_append", lapsum_node::entry(cache_append));
   m.def("cache_read", lapsum_node::entry(cache_read));
   m.def("cache_attend", lapsum_node::entry(cache_attend));

@@ -84,11 +84,26 @@ def _by_expert(rows, offsets):
     return [(e, a, b) for e, (a, b) in enumerate(zip(ends, ends[1:])) if a < b]
 
 
+# those of the largest tiles, of gradients in tiles of each size, and of both ways to LDS
+LARGE = [(8200, 2, 3, 2600, 2056), (8200, 2, 3, 1504, 2056), (8200, 2, 3, 72, 2056), (8200, 2, 3, 1501, 2055)]
+
+
+@pytest.mark.parametrize("layout", ["in_out", "out_in"])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", LARGE)
+def test_large_products_and_their_gradients(lib, shape, dtype, layout):
+    _products(lib, shape, dtype, layout, True)
+
+
 @pytest.mark.parametrize("gather", [True, False])
 @pytest.mark.parametrize("layout", ["in_out", "out_in"])
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("shape", SHAPES)
 def test_products_and_their_gradients(lib, shape, dtype, layout, gather):
+    _products(lib, shape, dtype, layout, gather)
+
+
+def _products(lib, shape, dtype, layout, gather):
     import paper_2608_06912_amd.autograd as A
     torch = _torch()
     tokens, top_k, experts, n_in, n_out = shape
