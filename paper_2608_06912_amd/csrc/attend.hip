@@ -41,18 +41,14 @@ __device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) {
   return __builtin_amdgcn_perm(b, a, 0x07060302u);
 }
 
-// N elements of a cache as they lie in memory; the elements past `left` are 0.
+// N elements of a cache as they lie in memory.
 template <int KIND, int N, bool VEC>
 struct Raw {
-  static constexpr int Words = N * kCacheBytes<KIND> / 4;
+  static constexpr int B = kCacheBytes<KIND>, Words = N * B / 4;
   uint32_t w[Words];
-  __device__ __forceinline__ void load(const void* data, int64_t at, int left) {
-    constexpr int B = kCacheBytes<KIND>;
-    const char* p = static_cast<const char*>(data) + at * B;
-#pragma unroll
-    for (int i = 0; i < Words; ++i) w[i] = 0u;
+  // VEC: all of them, at a multiple of their bytes; else the elements from `left` on are 0.
+  __device__ __forceinline__ void load(const char* p, int left) {
     if constexpr (VEC) {
-      if (left <= 0) return;
       if constexpr (Words % 4 == 0) {
 #pragma unroll
         for (int i = 0; i < Words; i += 4) {
@@ -68,6 +64,7 @@ struct Raw {
         w[0] = *reinterpret_cast<const uint32_t*>(p);
       }
     } else {
+      clear();
 #pragma unroll
       for (int j = 0; j < N; ++j)
         if (j < left) {
@@ -84,9 +81,15 @@ struct Raw {
   }
   // Elements 2 i and 2 i + 1 in 16 bits each.
   __device__ __forceinline__ void halves(uint32_t (&h)[N / 2]) const {
-    if constexpr (kCacheBytes<KIND> == 2) {
+    if constexpr (B == 2) {
 #pragma unroll
       for (int i = 0; i < N / 2; ++i) h[i] = w[i];
+    } else if constexpr (KIND == kE4m3) {
+#pragma unroll
+      for (int i = 0; i < Words; ++i) {
+        h[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], 1.0f, false));
+        h[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], 1.0f, true));
+      }
     } else {
 #pragma unroll
       for (int i = 0; i < Words; ++i) {
@@ -126,17 +129,30 @@ __device__ __forceinline__ float across_rows(float x, Op op) {
   return op(x, __shfl_xor(x, 32));
 }
 
-// dim at most 32 ND.
+// What a step has on its way: 32 keys' and values' elements and scales.
 template <int QT, int KIND, int ND, bool VEC>
-__global__ __launch_bounds__(AT) void cache_attend_kernel(AttendArgs a) {
-  constexpr bool F32 = KIND == 0;
+struct Step {
+  static constexpr bool F32 = KIND == 0;
+  static constexpr int KN = F32 ? 4 : 8;           // dims of a lane in a part of the first product
+  static constexpr int KS = ND * 32 / (4 * KN);    // its parts
+  static constexpr int VN = F32 || ND <= 2 ? 4 : 8;   // dims of a lane in a piece of a value row
+  static constexpr int VC = (ND * 32 + 16 * VN - 1) / (16 * VN);
+  Raw<KIND, KN, VEC> k[2][KS];
+  Raw<KIND, VN, VEC> v[VC][2][4];
+  float ks[2][4], vs[2][4];
+  bool there[2][4];                                // the keys' pages exist
+};
+
+// dim at most 32 ND.  UNIFORM: sixteen keys that begin at a multiple of 16 are in one page, and
+// 15 slots are less than 2^31 bytes.
+template <int QT, int KIND, int ND, bool VEC, bool UNIFORM>
+__global__ __launch_bounds__(AT, ND == 8 || (QT == 0 && ND > 2) ? 1 : 2) void cache_attend_kernel(AttendArgs a) {
+  using St = Step<QT, KIND, ND, VEC>;
+  constexpr bool F32 = St::F32;
   constexpr int MT = KIND <= 2 ? KIND : 1;
   constexpr int TQ = KIND <= 2 ? 1 : QT == 1 ? 1 : QT == 2 ? 2 : 3;   // terms of a query
   constexpr int TP = QT == 0 ? 3 : 2;                                   // and of a weight
-  constexpr int KN = F32 ? 4 : 8;                  // dims of a lane in a step of the first product
-  constexpr int KS = ND * 32 / (4 * KN);           // its steps
-  constexpr int VN = F32 || ND <= 2 ? 4 : 8;       // dims of a lane in a piece of a value row
-  constexpr int VC = (ND * 32 + 16 * VN - 1) / (16 * VN);
+  constexpr int KN = St::KN, KS = St::KS, VN = St::VN, VC = St::VC, B = kCacheBytes<KIND>;
   // float16 weights are scaled to the upper end of their range, where small ones keep their bits
   constexpr float kUp = MT == 2 ? 15.0f : 0.0f;
   __shared__ float parts[AW][16][ND * 32 + 2];
@@ -160,14 +176,26 @@ __global__ __launch_bounds__(AT) void cache_attend_kernel(AttendArgs a) {
 #pragma unroll
   for (int s = 0; s < KS; ++s) {
     const int d = s * 4 * KN + KN * g;
-    const int64_t from_q = b * a.q_b + (head0 + i16) * a.q_h + d;
     const int left = i16 < live ? a.dim - d : 0;
     using raw = typename Elem<QT>::raw;
-    const raw* p = static_cast<const raw*>(a.q) + from_q;
+    const raw* p = static_cast<const raw*>(a.q) + b * a.q_b + (head0 + i16) * a.q_h + d;
     float x[8] = {};
+    if (a.q_whole) {
+      if (left > 0) {
+        constexpr int N = 16 / sizeof(raw);
 #pragma unroll
-    for (int j = 0; j < KN; ++j)
-      if (j < left) x[j] = Elem<QT>::get(p[j]);
+        for (int j0 = 0; j0 < KN; j0 += N) {
+          const Move16 v = *reinterpret_cast<const Move16*>(p + j0);
+#pragma unroll
+          for (int j = 0; j < N && j < KN; ++j)
+            x[j0 + j] = Elem<QT>::get(QT == 0 ? v[j % 4] : (v[j / 2 % 4] >> (16 * (j % 2))) & 0xffffu);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < KN; ++j)
+        if (j < left) x[j] = Elem<QT>::get(p[j]);
+    }
     if constexpr (F32) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) q[s][0][j] = __float_as_uint(x[j]);
@@ -176,84 +204,110 @@ __global__ __launch_bounds__(AT) void cache_attend_kernel(AttendArgs a) {
     }
   }
 
-  float m = -INFINITY, l = 0.0f;
-  Acc out[VC][VN] = {};
-  const float scale2 = a.scale * static_cast<float>(kLog2e);
-  const bool uniform = !a.t.table || a.t.size % 16 == 0;   // sixteen keys are in one page
-  float* scores = a.weights ? a.weights + (static_cast<int64_t>(b) * a.heads + head0 + i16) * a.room : nullptr;
+  // A lane's dims within a row, in bytes; dims that do not exist are the last ones
+  // again (their part of q is 0, and their results are not stored).
+  int k_dim[KS], v_dim[VC];
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    const int d = s * 4 * KN + KN * g;
+    k_dim[s] = (VEC ? min(d, a.dim - KN) : d) * B;
+  }
+#pragma unroll
+  for (int c = 0; c < VC; ++c) {
+    const int d = c * 16 * VN + VN * i16;
+    v_dim[c] = (VEC ? min(d, a.dim - VN) : d) * B;
+  }
+  const int slot_k = static_cast<int>(a.k.slot) * B, slot_v = static_cast<int>(a.v.slot) * B;
+  const char* head_k = static_cast<const char*>(a.k.data) + h * a.k.head * B;
+  const char* head_v = static_cast<const char*>(a.v.data) + h * a.v.head * B;
+  const float* scale_k = KIND > 2 ? a.k.scale + h * a.k.scale_head : nullptr;
+  const float* scale_v = KIND > 2 ? a.v.scale + h * a.v.scale_head : nullptr;
 
-  for (int64_t k0 = base + AK * wave; k0 < to; k0 += AK * AW) {
-    const int key0 = static_cast<int>(k0);
-    // where the rows are; a row that does not exist is read as the cache's first, and not used
-    int64_t k_at[2], v_at[2][4], ks_at[2][4], vs_at[2][4];
-    bool ok[2][4];
+  // the pages of a step, looked up a step before its loads
+  const int32_t* table = a.t.table ? a.t.table + static_cast<int64_t>(b) * a.t.width : nullptr;
+  int32_t page_of[2] = {b, b};
+  const auto look = [&](int64_t k0) {
+    if (UNIFORM && table) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int64_t p = divide(static_cast<uint32_t>(min(k0 + 16 * u, a.room)), a.by);
+        page_of[u] = p < a.t.width ? table[p] : -1;
+      }
+    }
+  };
+  const auto load = [&](St& st, int key0) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      int page, slot;
-      if (uniform) {
-        find_slot(a.t, b, key0 + 16 * u, &page, &slot);
-        const bool in = page >= 0;
-        const int64_t pk = in ? page * a.k.page + slot * a.k.slot : 0;
-        const int64_t pv = in ? page * a.v.page + slot * a.v.slot : 0;
-        const int key = key0 + 16 * u + i16;
-        k_at[u] = in && key < to ? pk + i16 * a.k.slot : 0;
+      if constexpr (UNIFORM) {
+        const int key = key0 + 16 * u;
+        int page = page_of[u];
+        int slot = key;
+        if (table) slot = key - static_cast<int>(divide(static_cast<uint32_t>(key), a.by)) * a.t.size;
+        else page = key < a.t.size ? b : -1;
+        page = __builtin_amdgcn_readfirstlane(page);
+        const bool in = page >= 0 && page < a.t.pages;
+        if (!in) page = slot = 0;
+        // (without a table the last rows of sixteen may be past the cache's end)
+        const int last = a.t.size - 1 - slot;
+        const int rk = min(i16, last) * slot_k;
+        const char* pk = head_k + (page * a.k.page + slot * a.k.slot) * B;
+        const char* pv = head_v + (page * a.v.page + slot * a.v.slot) * B;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) st.k[u][s].load(pk + (rk + k_dim[s]), a.dim - (s * 4 * KN + KN * g));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int r = 4 * g + i, kv = key0 + 16 * u + r;
-          ok[u][i] = in && kv >= from && kv < to;
-          v_at[u][i] = in && kv < to ? pv + r * a.v.slot : 0;
+          const int r = min(4 * g + i, last);
+          st.there[u][i] = in;
+#pragma unroll
+          for (int c = 0; c < VC; ++c)
+            st.v[c][u][i].load(pv + (r * slot_v + v_dim[c]), a.dim - (c * 16 * VN + VN * i16));
           if constexpr (KIND > 2) {
-            ks_at[u][i] = in && kv < to ? page * a.k.scale_page + slot + r : 0;
-            vs_at[u][i] = in && kv < to ? page * a.v.scale_page + slot + r : 0;
+            st.ks[u][i] = scale_k[page * a.k.scale_page + slot + r];
+            st.vs[u][i] = scale_v[page * a.v.scale_page + slot + r];
           }
         }
       } else {
-        const int key = key0 + 16 * u + i16;
-        find_slot(a.t, b, key, &page, &slot);
-        k_at[u] = page >= 0 && key < to ? page * a.k.page + slot * a.k.slot : 0;
+        const auto find = [&](int key, int* slot) {
+          int page;
+          if (table) {
+            const int p = static_cast<int>(divide(static_cast<uint32_t>(key), a.by));
+            *slot = key - p * a.t.size;
+            page = p < a.t.width ? table[p] : -1;
+          } else {
+            *slot = key;
+            page = key < a.t.size ? b : -1;
+          }
+          return page >= 0 && page < a.t.pages && key < to ? page : -1;
+        };
+        int slot;
+        int page = find(key0 + 16 * u + i16, &slot);
+        if (page < 0) page = slot = 0;
+        const char* pk = head_k + (page * a.k.page + slot * a.k.slot) * B;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) st.k[u][s].load(pk + k_dim[s], a.dim - (s * 4 * KN + KN * g));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int kv = key0 + 16 * u + 4 * g + i;
-          find_slot(a.t, b, kv, &page, &slot);
-          const bool in = page >= 0 && kv < to;
-          ok[u][i] = in && kv >= from;
-          v_at[u][i] = in ? page * a.v.page + slot * a.v.slot : 0;
+          page = find(key0 + 16 * u + 4 * g + i, &slot);
+          st.there[u][i] = page >= 0;
+          if (page < 0) page = slot = 0;
+          const char* pv = head_v + (page * a.v.page + slot * a.v.slot) * B;
+#pragma unroll
+          for (int c = 0; c < VC; ++c) st.v[c][u][i].load(pv + v_dim[c], a.dim - (c * 16 * VN + VN * i16));
           if constexpr (KIND > 2) {
-            ks_at[u][i] = in ? page * a.k.scale_page + slot : 0;
-            vs_at[u][i] = in ? page * a.v.scale_page + slot : 0;
+            st.ks[u][i] = scale_k[page * a.k.scale_page + slot];
+            st.vs[u][i] = scale_v[page * a.v.scale_page + slot];
           }
         }
       }
     }
-    Raw<KIND, KN, VEC> kr[2][KS];
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        const int d = s * 4 * KN + KN * g;
-        kr[u][s].load(a.k.data, k_at[u] + h * a.k.head + d, a.dim - d);
-      }
-    Raw<KIND, VN, VEC> vr[VC][2][4];
-#pragma unroll
-    for (int c = 0; c < VC; ++c)
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int d = c * 16 * VN + VN * i16;
-          vr[c][u][i].load(a.v.data, v_at[u][i] + h * a.v.head + d, a.dim - d);
-        }
-    float ks[2][4], vs[2][4];
-    if constexpr (KIND > 2) {
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          ks[u][i] = a.k.scale[h * a.k.scale_head + ks_at[u][i]] * scale2;
-          vs[u][i] = a.v.scale[h * a.v.scale_head + vs_at[u][i]];
-        }
-    }
+  };
 
+  float m = -INFINITY, l = 0.0f;
+  Acc out[VC][VN] = {};
+  const float scale2 = a.scale * static_cast<float>(kLog2e);
+  float* scores = a.weights ? a.weights + (static_cast<int64_t>(b) * a.heads + head0 + i16) * a.room : nullptr;
+
+  const auto use = [&](St& st, int key0) {
     Acc sc[2] = {};
 #pragma unroll
     for (int u = 0; u < 2; ++u)
@@ -261,21 +315,25 @@ __global__ __launch_bounds__(AT) void cache_attend_kernel(AttendArgs a) {
       for (int s = 0; s < KS; ++s) {
         Move16 f;
         if constexpr (F32) {
-          f = Move16{kr[u][s].w[0], kr[u][s].w[1], kr[u][s].w[2], kr[u][s].w[3]};
+          f = Move16{st.k[u][s].w[0], st.k[u][s].w[1], st.k[u][s].w[2], st.k[u][s].w[3]};
         } else {
           uint32_t hv[4];
-          kr[u][s].halves(hv);
+          st.k[u][s].halves(hv);
           f = Move16{hv[0], hv[1], hv[2], hv[3]};
         }
 #pragma unroll
         for (int t = 0; t < TQ; ++t) sc[u] = mma<MT>(f, q[s][t], sc[u]);
       }
+    bool ok[2][4], all = true;
     float most = -INFINITY;
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float x = KIND > 2 ? sc[u][i] * ks[u][i] : sc[u][i] * scale2;
+        const int key = key0 + 16 * u + 4 * g + i;
+        ok[u][i] = st.there[u][i] && key >= from && key < to;
+        all = all && ok[u][i];
+        const float x = KIND > 2 ? sc[u][i] * (st.ks[u][i] * scale2) : sc[u][i] * scale2;
         sc[u][i] = ok[u][i] ? x : -INFINITY;
         most = fmaxf(most, sc[u][i]);
       }
@@ -309,14 +367,9 @@ __global__ __launch_bounds__(AT) void cache_attend_kernel(AttendArgs a) {
         const float x = exp2_fast(sc[u][i] - ref);
         l += x;
         p[4 * u + i] = x;
-        if constexpr (KIND > 2) p[4 * u + i] = ok[u][i] ? x * vs[u][i] : 0.0f;
+        if constexpr (KIND > 2) p[4 * u + i] = ok[u][i] ? x * st.vs[u][i] : 0.0f;
       }
     // (a value that is not there may hold anything, and 0 of it may be NaN)
-    bool all = true;
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) all = all && ok[u][i];
     if (!__all(all)) {
 #pragma unroll
       for (int c = 0; c < VC; ++c)
@@ -324,7 +377,7 @@ __global__ __launch_bounds__(AT) void cache_attend_kernel(AttendArgs a) {
         for (int u = 0; u < 2; ++u)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (!ok[u][i]) vr[c][u][i].clear();
+            if (!ok[u][i]) st.v[c][u][i].clear();
     }
     if constexpr (F32) {
 #pragma unroll
@@ -335,7 +388,7 @@ __global__ __launch_bounds__(AT) void cache_attend_kernel(AttendArgs a) {
           for (int c = 0; c < VC; ++c)
 #pragma unroll
             for (int e = 0; e < VN; ++e)
-              out[c][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(p[4 * u + i], __uint_as_float(vr[c][u][i].w[e]),
+              out[c][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(p[4 * u + i], __uint_as_float(st.v[c][u][i].w[e]),
                                                                out[c][e], 0, 0, 0);
     } else {
       Move16 w[TP];
@@ -344,7 +397,7 @@ __global__ __launch_bounds__(AT) void cache_attend_kernel(AttendArgs a) {
       for (int c = 0; c < VC; ++c) {
         uint32_t hv[8][VN / 2];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) vr[c][j / 4][j % 4].halves(hv[j]);
+        for (int j = 0; j < 8; ++j) st.v[c][j / 4][j % 4].halves(hv[j]);
 #pragma unroll
         for (int e = 0; e < VN; ++e) {
           Move16 f;
@@ -356,6 +409,43 @@ __global__ __launch_bounds__(AT) void cache_attend_kernel(AttendArgs a) {
           for (int t = 0; t < TP; ++t) out[c][e] = mma<MT>(w[t], f, out[c][e]);
         }
       }
+    }
+  };
+
+  // a step's loads go out before the step before it is used
+  constexpr int stride = AK * AW;
+  // (a step's registers are too many to have two of the widest rows)
+  constexpr bool two = QT == 0 ? ND <= 2 : ND <= 4;
+  int64_t k0 = base + AK * wave;
+  if constexpr (two) {
+    St even, odd;
+    if (k0 < to) {
+      look(k0);
+      load(even, static_cast<int>(k0));
+      look(k0 + stride);
+    }
+    while (k0 < to) {
+      if (k0 + stride < to) {
+        load(odd, static_cast<int>(k0 + stride));
+        look(k0 + 2 * stride);
+      }
+      use(even, static_cast<int>(k0));
+      k0 += stride;
+      if (k0 >= to) break;
+      if (k0 + stride < to) {
+        load(even, static_cast<int>(k0 + stride));
+        look(k0 + 2 * stride);
+      }
+      use(odd, static_cast<int>(k0));
+      k0 += stride;
+    }
+  } else {
+    St st;
+    if (k0 < to) look(k0);
+    for (; k0 < to; k0 += stride) {
+      load(st, static_cast<int>(k0));
+      look(k0 + stride);
+      use(st, static_cast<int>(k0));
     }
   }
 
@@ -409,33 +499,57 @@ __global__ __launch_bounds__(AT) void cache_attend_kernel(AttendArgs a) {
   }
 }
 
-// The parts of a row (b, head) joined; a wave to each.
+// The parts of a row (b, head) joined: their factors e^(m - top) in LDS, then a wave to every
+// fourth part, its lanes to the dims.
+constexpr int JT = 256;
 template <int QT>
-__global__ __launch_bounds__(kWave) void cache_attend_join_kernel(AttendArgs a, float up) {
+__global__ __launch_bounds__(JT) void cache_attend_join_kernel(AttendArgs a, float up) {
+  extern __shared__ float lds[];
+  float* factor = lds;                                  // [splits]
+  float* sums = lds + a.splits;                         // [4][dim]
+  __shared__ float shared[2][JT / kWave];
   const int64_t row = blockIdx.x, rows = static_cast<int64_t>(a.batch) * a.heads;
-  const int lane = lane_id();
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int64_t step = rows * (a.dim + 2);
   const float* part = a.part + row * (a.dim + 2);
   float top = -INFINITY;
-  for (int s = lane; s < a.splits; s += kWave) top = fmaxf(top, part[s * step + a.dim]);
+  for (int s = threadIdx.x; s < a.splits; s += JT) {
+    factor[s] = part[s * step + a.dim];
+    top = fmaxf(top, factor[s]);
+  }
   top = wave_max(top, -INFINITY);
+  if (lane == 0) shared[0][wave] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < JT / kWave; ++w) top = fmaxf(top, shared[0][w]);
   float sum = 0.0f;
-  for (int s = lane; s < a.splits; s += kWave) {
-    const float m = part[s * step + a.dim];
-    if (m != -INFINITY) sum += exp2_fast(m - top) * part[s * step + a.dim + 1];
+  for (int s = threadIdx.x; s < a.splits; s += JT) {
+    const float m = factor[s], f = m == -INFINITY ? 0.0f : exp2_fast(m - top);
+    factor[s] = f;
+    // (a part without keys is all zeros)
+    sum += f * part[s * step + a.dim + 1];
   }
   sum = wave_sum(sum);
-  using raw = typename Elem<QT>::raw;
+  if (lane == 0) shared[1][wave] = sum;
+  __syncthreads();
+  sum = 0.0f;
+#pragma unroll
+  for (int w = 0; w < JT / kWave; ++w) sum += shared[1][w];
   for (int d = lane; d < a.dim; d += kWave) {
     float y = 0.0f;
-#pragma unroll 4
-    for (int s = 0; s < a.splits; ++s) {
-      const float m = part[s * step + a.dim];
-      y += (m == -INFINITY ? 0.0f : exp2_fast(m - top)) * part[s * step + d];
-    }
+#pragma unroll 8
+    for (int s = wave; s < a.splits; s += JT / kWave) y = fmaf(factor[s], part[s * step + d], y);
+    sums[wave * a.dim + d] = y;
+  }
+  __syncthreads();
+  using raw = typename Elem<QT>::raw;
+  for (int d = threadIdx.x; d < a.dim; d += JT) {
+    float y = 0.0f;
+#pragma unroll
+    for (int w = 0; w < JT / kWave; ++w) y += sums[w * a.dim + d];
     static_cast<raw*>(a.out)[row * a.dim + d] = Elem<QT>::put(sum == 0.0f ? 0.0f : y / sum);
   }
-  if (lane == 0 && a.lse)
+  if (threadIdx.x == 0 && a.lse)
     a.lse[row] = sum == 0.0f ? -INFINITY : (top + __log2f(sum) - up) * static_cast<float>(1.0 / kLog2e);
 }
 
@@ -461,7 +575,7 @@ void attend_plan(int64_t batch, int64_t heads, int64_t kv, int64_t room, int64_t
   constexpr int64_t step = AK * AW;
   const int64_t rows = batch * kv * ((heads / kv + 15) / 16);
   const int64_t keys = window > 0 && window < room ? (window + AK < room ? window + AK : room) : room;
-  int64_t each = (keys * rows + 2047) / 2048;
+  int64_t each = (keys * rows + 4095) / 4096;
   each = (each + step - 1) / step * step;
   if (each < step) each = step;
   *chunk = static_cast<int>(each);
@@ -470,15 +584,26 @@ void attend_plan(int64_t batch, int64_t heads, int64_t kv, int64_t room, int64_t
 
 hipError_t launch_cache_attend(const AttendArgs& a, int dtype, int kind, bool vec, hipStream_t s) {
   const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(a.splits) * a.batch * a.kv * a.tiles));
+  const int64_t bytes = kind == 0 ? 4 : kind <= 2 ? 2 : 1;
+  const bool uniform = (!a.t.table || a.t.size % 16 == 0) && 16 * a.k.slot * bytes < (int64_t(1) << 31) - 65536 &&
+                       16 * a.v.slot * bytes < (int64_t(1) << 31) - 65536;
   {
     ProfScope ps_("cache_attend", s);
     const auto launch = [&](auto qt, auto kd) {
       constexpr int QT = decltype(qt)::value, KIND = decltype(kd)::value;
-      if (!vec) hipLaunchKernelGGL((cache_attend_kernel<QT, KIND, 8, false>), grid, dim3(AT), 0, s, a);
-      else if (a.dim <= 64) hipLaunchKernelGGL((cache_attend_kernel<QT, KIND, 2, true>), grid, dim3(AT), 0, s, a);
-      else if (a.dim <= 96) hipLaunchKernelGGL((cache_attend_kernel<QT, KIND, 3, true>), grid, dim3(AT), 0, s, a);
-      else if (a.dim <= 128) hipLaunchKernelGGL((cache_attend_kernel<QT, KIND, 4, true>), grid, dim3(AT), 0, s, a);
-      else hipLaunchKernelGGL((cache_attend_kernel<QT, KIND, 8, true>), grid, dim3(AT), 0, s, a);
+      const auto go = [&](auto nd, auto uni) {
+        hipLaunchKernelGGL((cache_attend_kernel<QT, KIND, decltype(nd)::value, true, decltype(uni)::value>), grid,
+                           dim3(AT), 0, s, a);
+      };
+      const auto dims = [&](auto uni) {
+        if (a.dim <= 64) go(std::integral_constant<int, 2>{}, uni);
+        else if (a.dim <= 96) go(std::integral_constant<int, 3>{}, uni);
+        else if (a.dim <= 128) go(std::integral_constant<int, 4>{}, uni);
+        else go(std::integral_constant<int, 8>{}, uni);
+      };
+      if (!vec) hipLaunchKernelGGL((cache_attend_kernel<QT, KIND, 8, false, false>), grid, dim3(AT), 0, s, a);
+      else if (uniform) dims(std::true_type{});
+      else dims(std::false_type{});
     };
     const auto of = [&](auto qt) {
       if (kind == kInt8) launch(qt, std::integral_constant<int, kInt8>{});
@@ -495,9 +620,10 @@ hipError_t launch_cache_attend(const AttendArgs& a, int dtype, int kind, bool ve
   if (a.part) {
     ProfScope ps_("cache_attend_join", s);
     const float up = kind == 2 ? 15.0f : 0.0f;
-    if (dtype == 0) hipLaunchKernelGGL((cache_attend_join_kernel<0>), dim3(rows), dim3(kWave), 0, s, a, up);
-    else if (dtype == 1) hipLaunchKernelGGL((cache_attend_join_kernel<1>), dim3(rows), dim3(kWave), 0, s, a, up);
-    else hipLaunchKernelGGL((cache_attend_join_kernel<2>), dim3(rows), dim3(kWave), 0, s, a, up);
+    const size_t lds = sizeof(float) * (static_cast<size_t>(a.splits) + 4 * static_cast<size_t>(a.dim));
+    if (dtype == 0) hipLaunchKernelGGL((cache_attend_join_kernel<0>), dim3(rows), dim3(JT), lds, s, a, up);
+    else if (dtype == 1) hipLaunchKernelGGL((cache_attend_join_kernel<1>), dim3(rows), dim3(JT), lds, s, a, up);
+    else hipLaunchKernelGGL((cache_attend_join_kernel<2>), dim3(rows), dim3(JT), lds, s, a, up);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

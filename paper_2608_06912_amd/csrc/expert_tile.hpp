@@ -76,8 +76,7 @@ struct Staged : Chunks<Op, T> {
 // product with floor(2^shift / top_k) + 1, exact for places below 2^31 (shift = 31 +
 // the bits of top_k - 1).
 __device__ __forceinline__ int64_t place_row(int32_t place, const Divider& by, int64_t count) {
-  const uint64_t q = static_cast<uint64_t>(static_cast<uint32_t>(place)) * by.factor >> by.shift;
-  const int64_t r = static_cast<int64_t>(q);
+  const int64_t r = divide(static_cast<uint32_t>(place), by);
   return place >= 0 && r < count ? r : -1;
 }
 __device__ __forceinline__ int64_t source_row(const int32_t* order, const Divider& by, int64_t count, int i) {

@@ -499,6 +499,23 @@ struct StepArgs {
 };
 hipError_t launch_cache_step(const StepArgs& a, int dtype, hipStream_t s);
 
+// Division by a number as a product and a shift.
+struct Divider {
+  uint32_t factor;
+  int shift;
+};
+inline Divider divider(int64_t by) {
+  int bits = 0;
+  while ((int64_t(1) << bits) < by) ++bits;
+  return Divider{static_cast<uint32_t>((uint64_t(1) << (31 + bits)) / static_cast<uint64_t>(by) + 1), 31 + bits};
+}
+#ifdef __HIPCC__
+// n / by, for n below 2^31.
+__device__ __forceinline__ uint32_t divide(uint32_t n, const Divider& by) {
+  return static_cast<uint32_t>(static_cast<uint64_t>(n) * by.factor >> by.shift);
+}
+#endif
+
 // -------------------------------------------------------- experts' rows ----
 constexpr int kExpertMost = 2048;
 struct OrderArgs {
@@ -532,16 +549,6 @@ struct CombineGradArgs {
 };
 hipError_t launch_expert_combine_backward(const CombineGradArgs& a, int dtype, bool vec, hipStream_t s);
 
-// Division by a number as a product and a shift.
-struct Divider {
-  uint32_t factor;
-  int shift;
-};
-inline Divider divider(int64_t by) {
-  int bits = 0;
-  while ((int64_t(1) << bits) < by) ++bits;
-  return Divider{static_cast<uint32_t>((uint64_t(1) << (31 + bits)) / static_cast<uint64_t>(by) + 1), 31 + bits};
-}
 // Products grouped by expert.  Rows: y[i] = x[row(i)] w_e for the rows of each
 // expert.  Grad: c_e[m][n] = sum over the expert's rows of a[row][m] b[row][n].
 struct RowsArgs {
@@ -581,6 +588,7 @@ struct PageTable {
   const int32_t* table;      // [batch, width], or null: page b is sequence b's
   int64_t pages;
   int width, size;           // pages of a sequence, slots of a page
+  Divider by;                // of positions by size
 };
 struct AppendArgs {
   const void* src[2];
@@ -610,7 +618,9 @@ struct AttendArgs {
   void* out;                 // [batch, heads, dim]
   float *lse, *weights;      // [batch, heads], [batch, heads, room], or null
   float* part;               // [splits][batch][heads][dim + 2]: sum, maximum, total
+  Divider by;                // t.by
   int batch, heads, kv, dim, group, tiles, window, splits, chunk;
+  int q_whole;               // queries are whole vectors of 16 bytes
   int64_t room;
   float scale;
 };

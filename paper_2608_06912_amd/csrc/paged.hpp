@@ -18,7 +18,7 @@ __device__ __forceinline__ void find_slot(const PageTable& t, int b, int at, int
     *slot = at;
     return;
   }
-  const int p = static_cast<int>(static_cast<uint32_t>(at) / static_cast<uint32_t>(t.size));
+  const int p = static_cast<int>(divide(static_cast<uint32_t>(at), t.by));
   *slot = at - p * t.size;
   int64_t page_no = -1;
   if (p < t.width) page_no = t.table[static_cast<int64_t>(b) * t.width + p];

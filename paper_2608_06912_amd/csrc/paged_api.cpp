@@ -43,7 +43,8 @@ int64_t room_of(const lapsum_paged* c, const int32_t* table, int64_t width, int6
   return width * c->slots;
 }
 PageTable table_of(const lapsum_paged* c, const int32_t* table, int64_t width) {
-  return PageTable{table, c->pages, static_cast<int>(table ? width : 1), static_cast<int>(c->slots)};
+  return PageTable{table, c->pages, static_cast<int>(table ? width : 1), static_cast<int>(c->slots),
+                   divider(c->slots)};
 }
 
 }  // namespace
@@ -176,6 +177,9 @@ int lapsum_cache_attend(const void* q, int64_t q_stride_batch, int64_t q_stride_
   a.tiles = (a.group + 15) / 16;
   a.window = static_cast<int>(window);
   a.room = room;
+  a.by = a.t.by;
+  a.q_whole = dim % 8 == 0 && vector_width(bits_of(q) | static_cast<uint64_t>((q_stride_batch | q_stride_head) *
+                                                                              bytes_of(dtype))) == 16;
   a.scale = static_cast<float>(scale);
   attend_plan(batch, heads, kv_heads, room, window, &a.splits, &a.chunk);
   a.part = a.splits > 1 ? static_cast<float*>(workspace) : nullptr;
