@@ -140,7 +140,8 @@ struct Step {
   Raw<KIND, KN, VEC> k[2][KS];
   Raw<KIND, VN, VEC> v[VC][2][4];
   float ks[2][4], vs[2][4];
-  bool there[2][4];                                // the keys' pages exist
+  // the keys' pages exist: of a tile (UNIFORM), or of a lane's own four
+  bool page[2], there[2][4];
 };
 
 // dim at most 32 ND.  UNIFORM: sixteen keys that begin at a multiple of 16 are in one page, and
@@ -196,6 +197,10 @@ __global__ __launch_bounds__(AT, ND == 8 || (QT == 0 && ND > 2) ? 1 : 2) void ca
       for (int j = 0; j < KN; ++j)
         if (j < left) x[j] = Elem<QT>::get(p[j]);
     }
+    if (a.scale <= 0.0f) {   // (so that larger products are larger scores)
+#pragma unroll
+      for (int j = 0; j < KN; ++j) x[j] = a.scale < 0.0f ? -x[j] : 0.0f;
+    }
     if constexpr (F32) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) q[s][0][j] = __float_as_uint(x[j]);
@@ -204,20 +209,27 @@ __global__ __launch_bounds__(AT, ND == 8 || (QT == 0 && ND > 2) ? 1 : 2) void ca
     }
   }
 
-  // A lane's dims within a row, in bytes; dims that do not exist are the last ones
-  // again (their part of q is 0, and their results are not stored).
-  int k_dim[KS], v_dim[VC];
+  // A lane's dims within a row, in bytes; dims that may not exist are the last ones
+  // again (their part of q is 0, and their results are not stored).  UNIFORM: with the
+  // lane's row of the sixteen, or the first of its four.
+  constexpr int kSure = ND == 2 ? 0 : ND == 8 ? 128 : 32 * (ND - 1);   // the smallest dim of this ND, less 1
+  const int slot_k = static_cast<int>(a.k.slot) * B, slot_v = static_cast<int>(a.v.slot) * B;
+  const uint32_t row_k = UNIFORM ? i16 * slot_k : 0, row_v = UNIFORM ? 4 * g * slot_v : 0;
+  const uint32_t first_k = row_k + KN * g * B;
+  uint32_t k_end[KS], v_at[VC];
 #pragma unroll
   for (int s = 0; s < KS; ++s) {
     const int d = s * 4 * KN + KN * g;
-    k_dim[s] = (VEC ? min(d, a.dim - KN) : d) * B;
+    k_end[s] = row_k + static_cast<uint32_t>((VEC ? min(d, a.dim - KN) : d) * B);
   }
+  const auto k_at = [&](int s) {
+    return 4 * KN * (s + 1) <= kSure ? first_k + static_cast<uint32_t>(4 * KN * B * s) : k_end[s];
+  };
 #pragma unroll
   for (int c = 0; c < VC; ++c) {
     const int d = c * 16 * VN + VN * i16;
-    v_dim[c] = (VEC ? min(d, a.dim - VN) : d) * B;
+    v_at[c] = row_v + static_cast<uint32_t>((VEC ? min(d, a.dim - VN) : d) * B);
   }
-  const int slot_k = static_cast<int>(a.k.slot) * B, slot_v = static_cast<int>(a.v.slot) * B;
   const char* head_k = static_cast<const char*>(a.k.data) + h * a.k.head * B;
   const char* head_v = static_cast<const char*>(a.v.data) + h * a.v.head * B;
   const float* scale_k = KIND > 2 ? a.k.scale + h * a.k.scale_head : nullptr;
@@ -245,25 +257,39 @@ __global__ __launch_bounds__(AT, ND == 8 || (QT == 0 && ND > 2) ? 1 : 2) void ca
         if (table) slot = key - static_cast<int>(divide(static_cast<uint32_t>(key), a.by)) * a.t.size;
         else page = key < a.t.size ? b : -1;
         page = __builtin_amdgcn_readfirstlane(page);
-        const bool in = page >= 0 && page < a.t.pages;
-        if (!in) page = slot = 0;
-        // (without a table the last rows of sixteen may be past the cache's end)
-        const int last = a.t.size - 1 - slot;
-        const int rk = min(i16, last) * slot_k;
+        st.page[u] = page >= 0 && page < a.t.pages;
+        if (!st.page[u]) page = slot = 0;
         const char* pk = head_k + (page * a.k.page + slot * a.k.slot) * B;
         const char* pv = head_v + (page * a.v.page + slot * a.v.slot) * B;
+        const float* sk = KIND > 2 ? scale_k + (page * a.k.scale_page + slot) : nullptr;
+        const float* sv = KIND > 2 ? scale_v + (page * a.v.scale_page + slot) : nullptr;
+        const int last = a.t.size - 1 - slot;
+        if (last >= 15) {
 #pragma unroll
-        for (int s = 0; s < KS; ++s) st.k[u][s].load(pk + (rk + k_dim[s]), a.dim - (s * 4 * KN + KN * g));
+          for (int s = 0; s < KS; ++s) st.k[u][s].load(pk + k_at(s), 0);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = min(4 * g + i, last);
-          st.there[u][i] = in;
+          for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int c = 0; c < VC; ++c)
-            st.v[c][u][i].load(pv + (r * slot_v + v_dim[c]), a.dim - (c * 16 * VN + VN * i16));
+            for (int c = 0; c < VC; ++c) st.v[c][u][i].load(pv + i * slot_v + v_at[c], 0);
           if constexpr (KIND > 2) {
-            st.ks[u][i] = scale_k[page * a.k.scale_page + slot + r];
-            st.vs[u][i] = scale_v[page * a.v.scale_page + slot + r];
+            const float4 fk = load_quad(sk + 4 * g), fv = load_quad(sv + 4 * g);
+            st.ks[u][0] = fk.x, st.ks[u][1] = fk.y, st.ks[u][2] = fk.z, st.ks[u][3] = fk.w;
+            st.vs[u][0] = fv.x, st.vs[u][1] = fv.y, st.vs[u][2] = fv.z, st.vs[u][3] = fv.w;
+          }
+        } else {   // (the end of a cache without a table: its last row stands for those past it)
+          const uint32_t back = static_cast<uint32_t>((i16 - min(i16, last)) * slot_k);
+#pragma unroll
+          for (int s = 0; s < KS; ++s) st.k[u][s].load(pk + (k_at(s) - back), 0);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int r = min(4 * g + i, last);
+#pragma unroll
+            for (int c = 0; c < VC; ++c)
+              st.v[c][u][i].load(pv + (v_at[c] + static_cast<uint32_t>((r - 4 * g) * slot_v)), 0);
+            if constexpr (KIND > 2) {
+              st.ks[u][i] = sk[r];
+              st.vs[u][i] = sv[r];
+            }
           }
         }
       } else {
@@ -284,7 +310,7 @@ __global__ __launch_bounds__(AT, ND == 8 || (QT == 0 && ND > 2) ? 1 : 2) void ca
         if (page < 0) page = slot = 0;
         const char* pk = head_k + (page * a.k.page + slot * a.k.slot) * B;
 #pragma unroll
-        for (int s = 0; s < KS; ++s) st.k[u][s].load(pk + k_dim[s], a.dim - (s * 4 * KN + KN * g));
+        for (int s = 0; s < KS; ++s) st.k[u][s].load(pk + k_at(s), a.dim - (s * 4 * KN + KN * g));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           page = find(key0 + 16 * u + 4 * g + i, &slot);
@@ -292,7 +318,7 @@ __global__ __launch_bounds__(AT, ND == 8 || (QT == 0 && ND > 2) ? 1 : 2) void ca
           if (page < 0) page = slot = 0;
           const char* pv = head_v + (page * a.v.page + slot * a.v.slot) * B;
 #pragma unroll
-          for (int c = 0; c < VC; ++c) st.v[c][u][i].load(pv + v_dim[c], a.dim - (c * 16 * VN + VN * i16));
+          for (int c = 0; c < VC; ++c) st.v[c][u][i].load(pv + v_at[c], a.dim - (c * 16 * VN + VN * i16));
           if constexpr (KIND > 2) {
             st.ks[u][i] = scale_k[page * a.k.scale_page + slot];
             st.vs[u][i] = scale_v[page * a.v.scale_page + slot];
@@ -304,7 +330,7 @@ __global__ __launch_bounds__(AT, ND == 8 || (QT == 0 && ND > 2) ? 1 : 2) void ca
 
   float m = -INFINITY, l = 0.0f;
   Acc out[VC][VN] = {};
-  const float scale2 = a.scale * static_cast<float>(kLog2e);
+  const float scale2 = (a.scale == 0.0f ? 1.0f : fabsf(a.scale)) * static_cast<float>(kLog2e);
   float* scores = a.weights ? a.weights + (static_cast<int64_t>(b) * a.heads + head0 + i16) * a.room : nullptr;
 
   const auto use = [&](St& st, int key0) {
@@ -324,29 +350,54 @@ __global__ __launch_bounds__(AT, ND == 8 || (QT == 0 && ND > 2) ? 1 : 2) void ca
 #pragma unroll
         for (int t = 0; t < TQ; ++t) sc[u] = mma<MT>(f, q[s][t], sc[u]);
       }
-    bool ok[2][4], all = true;
+    if constexpr (KIND > 2) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sc[u][i] *= st.ks[u][i];
+    }
+    // Keys that are not there count for nothing, whatever was read for them (and 0 of
+    // that may be NaN).
+    bool whole = key0 >= from && key0 + AK <= to;
+    if constexpr (UNIFORM) {
+      whole = whole && st.page[0] && st.page[1];
+    } else {
+      bool all = true;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) all = all && st.there[u][i];
+      whole = whole && __all(all);
+    }
+    if (!whole) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int key = key0 + 16 * u + 4 * g + i;
+          if (key >= from && key < to && (UNIFORM ? st.page[u] : st.there[u][i])) continue;
+          sc[u][i] = -INFINITY;
+          st.vs[u][i] = 0.0f;
+#pragma unroll
+          for (int c = 0; c < VC; ++c) st.v[c][u][i].clear();
+        }
+    }
+    // (the running maximum is one of products, which `scale2` times are powers of two)
     float most = -INFINITY;
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int key = key0 + 16 * u + 4 * g + i;
-        ok[u][i] = st.there[u][i] && key >= from && key < to;
-        all = all && ok[u][i];
-        const float x = KIND > 2 ? sc[u][i] * (st.ks[u][i] * scale2) : sc[u][i] * scale2;
-        sc[u][i] = ok[u][i] ? x : -INFINITY;
-        most = fmaxf(most, sc[u][i]);
-      }
+      for (int i = 0; i < 4; ++i) most = fmaxf(most, sc[u][i]);
     if (scores && i16 < live) {
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (key0 + 16 * u + 4 * g + i < to) scores[key0 + 16 * u + 4 * g + i] = sc[u][i];
+          if (key0 + 16 * u + 4 * g + i < to) scores[key0 + 16 * u + 4 * g + i] = sc[u][i] * scale2;
     }
     if (__any(most > m)) {
       const float now = across_rows(fmaxf(m, most), [](float x, float y) { return fmaxf(x, y); });
-      const float shrink = now == -INFINITY ? 1.0f : exp2_fast(m - now);
+      const float shrink = now == -INFINITY ? 1.0f : exp2_fast((m - now) * scale2);
       m = now;
       l *= shrink;
 #pragma unroll
@@ -358,27 +409,17 @@ __global__ __launch_bounds__(AT, ND == 8 || (QT == 0 && ND > 2) ? 1 : 2) void ca
           for (int e = 0; e < VN; ++e) out[c][e][i] *= f;
       }
     }
-    const float ref = m == -INFINITY ? 0.0f : m - kUp;
+    const float ref = m == -INFINITY ? 0.0f : m;
     float p[8];
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float x = exp2_fast(sc[u][i] - ref);
+        // (a difference first: what is far from zero is near the maximum)
+        const float x = exp2_fast(fmaf(sc[u][i] - ref, scale2, kUp));
         l += x;
-        p[4 * u + i] = x;
-        if constexpr (KIND > 2) p[4 * u + i] = ok[u][i] ? x * st.vs[u][i] : 0.0f;
+        p[4 * u + i] = KIND > 2 ? x * st.vs[u][i] : x;
       }
-    // (a value that is not there may hold anything, and 0 of it may be NaN)
-    if (!__all(all)) {
-#pragma unroll
-      for (int c = 0; c < VC; ++c)
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (!ok[u][i]) st.v[c][u][i].clear();
-    }
     if constexpr (F32) {
 #pragma unroll
       for (int u = 0; u < 2; ++u)
@@ -452,7 +493,7 @@ __global__ __launch_bounds__(AT, ND == 8 || (QT == 0 && ND > 2) ? 1 : 2) void ca
   // the waves' parts, joined
   l = across_rows(l, [](float x, float y) { return x + y; });
   if (g == 0) {
-    parts[wave][i16][ND * 32] = m;
+    parts[wave][i16][ND * 32] = m * scale2;   // (in powers of two; scale2 is above 0)
     parts[wave][i16][ND * 32 + 1] = l;
   }
 #pragma unroll

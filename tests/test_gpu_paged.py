@@ -306,6 +306,25 @@ def test_attend_large_scores(lib):
         assert float((got.double() - want).abs().max()) < 4 * (1500 * 6 * 2.0 ** -24 + torch.finfo(dtype).eps)
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("scale", [-0.4, 0.0, 1e-30])
+def test_attend_scales(lib, scale, kind):
+    """Scores that fall as the products grow, and scores that are all the same."""
+    torch = _torch()
+    gen = _gen(6)
+    q = torch.randn(2, 6, 96, generator=gen, device="cuda")
+    lens = torch.tensor([70, 3], dtype=torch.int32, device="cuda")
+    x = torch.randn(2, 2, 70, 96, generator=gen, device="cuda")
+    c, s = (x, None) if kind == "same" else [t.cuda() for t in _quantised(x, kind)]
+    full = c.double() if s is None else c.double() * s.double()[..., None]
+    got, lse, w = lib.lapsum_cache_attend(q, c, c, lens, k_scale=s, v_scale=s, scale=scale, lse=True, weights=True)
+    keep = torch.arange(70, device="cuda") < lens[:, None]
+    want, total, ws, _, _ = _attend(q.double(), full, full, scale, keep)
+    # scores below 50 in float32, sums of 96 products: 200 roundings of it at most
+    for a, b in ((got, want), (lse, total), (w, ws)):
+        assert float((a.double() - b).abs().max()) < 50 * 200 * 2.0 ** -24
+
+
 def test_weights_feed_the_bounded_cache(lib):
     """evict, attend with weights, step: as the plain sums have it."""
     torch = _torch()
