@@ -21,7 +21,6 @@ namespace {
 
 constexpr int OW = 8;                  // waves of a workgroup of the order
 constexpr int OT = OW * kWave;
-constexpr int kOrderRun = 16 * OT;     // places of a workgroup, where there are several
 
 __device__ __forceinline__ int bin_of(const int32_t* indices, int64_t i, int experts) {
   const int e = indices[i];
@@ -34,8 +33,8 @@ __global__ __launch_bounds__(OT) void expert_count_kernel(OrderArgs a) {
   const int bins = a.experts + 1;
   for (int e = threadIdx.x; e < bins; e += OT) lds[e] = 0;
   __syncthreads();
-  const int64_t lo = static_cast<int64_t>(blockIdx.x) * kOrderRun;
-  const int64_t hi = lo + kOrderRun < a.count ? lo + kOrderRun : a.count;
+  const int64_t lo = static_cast<int64_t>(blockIdx.x) * a.run;
+  const int64_t hi = lo + a.run < a.count ? lo + a.run : a.count;
   for (int64_t i = lo + threadIdx.x; i < hi; i += OT) atomicAdd(&lds[bin_of(a.indices, i, a.experts)], 1);
   __syncthreads();
   for (int e = threadIdx.x; e < bins; e += OT) a.parts[static_cast<int64_t>(blockIdx.x) * bins + e] = lds[e];
@@ -52,7 +51,7 @@ __global__ __launch_bounds__(OT) void expert_order_kernel(OrderArgs a) {
   int* before = total + bins;
   for (int e = threadIdx.x; e < (OW + 2) * bins; e += OT) lds[e] = 0;
   __syncthreads();
-  const int64_t run = blocks == 1 ? (a.count + OT - 1) / OT * kWave : kOrderRun / OW;
+  const int64_t run = a.run / OW;
   const int64_t lo = (static_cast<int64_t>(blockIdx.x) * OW + wave) * run;
   const int64_t hi = lo + run < a.count ? lo + run : a.count;
   for (int64_t i = lo + lane; i < hi; i += kWave) atomicAdd(&mine[bin_of(a.indices, i, a.experts)], 1);
@@ -263,10 +262,21 @@ __global__ __launch_bounds__(256) void expert_combine_backward_kernel(CombineGra
 }  // namespace
 
 // ------------------------------------------------------------- launchers ---
-int64_t order_blocks(int64_t count) { return count <= kOrderRun ? 1 : (count + kOrderRun - 1) / kOrderRun; }
+// One workgroup up to 8192 places, which is one launch less; else 2048 places to one,
+// more where that would be more than 256 of them: each reads all others' counts.
+int64_t order_run(int64_t count) {
+  const int64_t want = count <= 16 * OT ? count : (count + 255) / 256;
+  const int64_t least = count <= 16 * OT ? OT : 4 * OT;
+  return (want < least ? least : want + OT - 1) / OT * OT;
+}
+int64_t order_blocks(int64_t count) {
+  const int64_t run = order_run(count);
+  return (count + run - 1) / run;
+}
 
-hipError_t launch_expert_order(const OrderArgs& a, hipStream_t s) {
+hipError_t launch_expert_order(OrderArgs a, hipStream_t s) {
   const unsigned blocks = static_cast<unsigned>(order_blocks(a.count));
+  a.run = order_run(a.count);
   const size_t bins = static_cast<size_t>(a.experts) + 1;
   if (blocks > 1) {
     ProfScope ps_("expert_count", s);

@@ -520,13 +520,13 @@ __device__ __forceinline__ uint32_t divide(uint32_t n, const Divider& by) {
 constexpr int kExpertMost = 2048;
 struct OrderArgs {
   const int32_t* indices;
-  int64_t count;
+  int64_t count, run;        // places; those of a workgroup, set by the launcher
   int experts;
   int32_t *order, *place, *offsets;
   int* parts;                // [order_blocks][experts + 1], where that is above one
 };
 int64_t order_blocks(int64_t count);
-hipError_t launch_expert_order(const OrderArgs& a, hipStream_t s);
+hipError_t launch_expert_order(OrderArgs a, hipStream_t s);
 
 struct CombineArgs {
   const void* y;             // [rows, dim]
@@ -606,7 +606,7 @@ struct ReadArgs {
   const int32_t* lens;
   void* out;                 // [batch, kv, room, dim]
   int batch, kv, room, dim;
-  int chunks;
+  int chunks;                // set by the launcher
 };
 hipError_t launch_cache_read(ReadArgs a, int dtype, int kind, bool vec, hipStream_t s);
 struct AttendArgs {

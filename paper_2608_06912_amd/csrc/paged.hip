@@ -4,7 +4,7 @@
 // A row x in 8 bits is codes c and a scale s = max(r max |x|, 2^-126), r the float32
 // nearest 1 / M, M = 127 (int8) or 448 (e4m3): c is x / s rounded to the nearest
 // code, ties to even, and stands for c s.  (The largest |x| / s is M to within two
-// roundings, which the code rounds away.)  The division is exact to rounding, as
+// roundings, which the code rounds away.)  The quotient is exact to rounding, as
 // a code off by one is off by a whole step.  (2^-126 keeps s a normal number; such a row is below every use.)  A row
 // with an infinity or NaN gets the scale NaN and codes 0, so that it reads back as
 // NaN and not as numbers.
@@ -108,100 +108,207 @@ __device__ __forceinline__ uint32_t team_most(uint32_t v) {
   return v;
 }
 
-template <int DT, int KIND, int TEAM, bool VEC>
+// The codes of eight elements over the scale.  One division gives 1 / scale to rounding,
+// and with it three operations give each quotient so: with r = x - q scale, exact, and q
+// the product with 1 / scale, q + r / scale rounds to the quotient's own rounding
+// (P. Markstein, Computation of elementary functions on the IBM RISC System/6000,
+// 1990; r has to be a number, so `tiny` scales, near the smallest, are divided by).
+template <int KIND>
+__device__ __forceinline__ Move8 encode8(const float (&x)[PN], float scale, bool tiny) {
+  const float inverse = 1.0f / scale;
+  float y[PN];
+#pragma unroll
+  for (int j = 0; j < PN; ++j) {
+    const float q = x[j] * inverse;
+    y[j] = copysignf(fmaf(fmaf(-q, scale, x[j]), inverse, q), x[j]);   // (zeros keep their sign)
+  }
+  if (__any(tiny)) {
+    asm volatile("");   // (a branch, not eight divisions and a choice)
+#pragma unroll
+    for (int j = 0; j < PN; ++j) y[j] = x[j] / scale;
+  }
+  if constexpr (KIND == kE4m3) {
+    return Move8{encode4<KIND>(y), encode4<KIND>(y + 4)};
+  } else {
+    // 1.5 2^23 more is a whole number, to the nearest, whose low byte is the code
+    uint32_t u[PN];
+#pragma unroll
+    for (int j = 0; j < PN; ++j) u[j] = __float_as_uint(y[j] + 12582912.0f);
+    Move8 codes;
+#pragma unroll
+    for (int w = 0; w < 2; ++w)
+      codes[w] = __builtin_amdgcn_perm(u[4 * w + 1], u[4 * w], 0x0c0c0400u) |
+                 __builtin_amdgcn_perm(u[4 * w + 3], u[4 * w + 2], 0x04000c0cu);
+    return codes;
+  }
+}
+
+// Where a team's rows are.  ROWS 1: teams take rows as they come.  Else a workgroup takes
+// ROWS times its teams' rows of one (sequence, head), so that sequence and head are the
+// workgroup's and the loads of ROWS rows are on their way together.
+template <int TEAM, int ROWS>
+struct Place {
+  int b, h, i[ROWS];
+  bool there[ROWS];
+  __device__ __forceinline__ Place(int batch, int kv, int rows, int chunks) {
+    constexpr int teams = PT / TEAM;
+    const int team = threadIdx.x / TEAM;
+    uint32_t bh;
+    if constexpr (ROWS == 1) {
+      const uint32_t row = blockIdx.x * static_cast<uint32_t>(teams) + team;
+      there[0] = row < static_cast<uint32_t>(batch) * static_cast<uint32_t>(kv) * static_cast<uint32_t>(rows);
+      bh = there[0] ? row / static_cast<uint32_t>(rows) : 0;
+      i[0] = there[0] ? static_cast<int>(row - bh * static_cast<uint32_t>(rows)) : 0;
+    } else {
+      bh = blockIdx.x / static_cast<uint32_t>(chunks);
+      const int first = static_cast<int>(blockIdx.x - bh * static_cast<uint32_t>(chunks)) * ROWS * teams + team;
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r) {
+        i[r] = first + r * teams;
+        there[r] = i[r] < rows;
+      }
+    }
+    b = static_cast<int>(bh / static_cast<uint32_t>(kv));
+    h = static_cast<int>(bh) - b * kv;
+  }
+};
+
+template <int DT, int KIND, int TEAM, int ROWS, bool VEC>
 __global__ __launch_bounds__(PT) void cache_append_kernel(AppendArgs a) {
   const int lane = threadIdx.x % TEAM;
-  const uint32_t row = blockIdx.x * static_cast<uint32_t>(PT / TEAM) + threadIdx.x / TEAM;
-  const uint32_t total = static_cast<uint32_t>(a.batch) * static_cast<uint32_t>(a.kv) * static_cast<uint32_t>(a.fresh);
-  const bool there = row < total;
-  const uint32_t bh = there ? row / static_cast<uint32_t>(a.fresh) : 0;
-  const int i = there ? static_cast<int>(row - bh * static_cast<uint32_t>(a.fresh)) : 0;
-  const int b = static_cast<int>(bh / static_cast<uint32_t>(a.kv));
-  const int h = static_cast<int>(bh) - b * a.kv;
-  int page = -1, slot = 0;
-  const int64_t at = static_cast<int64_t>(a.seen[b]) + i;
-  if (there && (!a.count || i < a.count[b]) && at >= 0 && at <= 2147483647LL)
-    find_slot(a.t, b, static_cast<int>(at), &page, &slot);
-  // (the whole wave goes on: teams reduce together)
-  const int left = page >= 0 ? a.dim - PN * lane : 0;
-  float x[2][PN] = {};
+  const Place<TEAM, ROWS> at(a.batch, a.kv, a.fresh, a.chunks);
+  const int64_t seen = a.seen[at.b];
+  const int count = a.count ? a.count[at.b] : a.fresh;
+  int page[ROWS], slot[ROWS], left[ROWS];
+  float x[ROWS][2][PN] = {};
 #pragma unroll
-  for (int n = 0; n < 2; ++n)
-    load8<DT, VEC>(a.src[n], b * a.src_b[n] + h * a.src_h[n] + i * a.src_i[n] + PN * lane, left, x[n]);
+  for (int r = 0; r < ROWS; ++r) {
+    page[r] = -1;
+    slot[r] = 0;
+    const int64_t pos = seen + at.i[r];
+    if (at.there[r] && at.i[r] < count && pos >= 0 && pos <= 2147483647LL)
+      find_slot(a.t, at.b, static_cast<int>(pos), &page[r], &slot[r]);
+    // (the whole wave goes on: teams reduce together)
+    left[r] = page[r] >= 0 ? a.dim - PN * lane : 0;
 #pragma unroll
-  for (int n = 0; n < 2; ++n) {
-    const PagedCache& c = a.cache[n];
-    const int64_t to = page * c.page + h * c.head + slot * c.slot + PN * lane;
-    if constexpr (KIND <= 2) {
-      store8<DT, VEC>(c.data, to, left, x[n]);
-    } else {
-      constexpr float unit = 1.0f / (KIND == kInt8 ? 127.0f : 448.0f);
-      // (magnitudes as whole numbers: infinities and NaN are the largest)
-      uint32_t m = 0;
+    for (int n = 0; n < 2; ++n)
+      load8<DT, VEC>(a.src[n], at.b * a.src_b[n] + at.h * a.src_h[n] + at.i[r] * a.src_i[n] + PN * lane, left[r],
+                     x[r][n]);
+  }
 #pragma unroll
-      for (int j = 0; j < PN; ++j) {
-        const uint32_t u = __float_as_uint(x[n][j]) & 0x7fffffffu;
-        m = u > m ? u : m;
+  for (int r = 0; r < ROWS; ++r) {
+    if (!__any(page[r] >= 0)) continue;
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      const PagedCache& c = a.cache[n];
+      const int64_t to = page[r] * c.page + at.h * c.head + slot[r] * c.slot + PN * lane;
+      if constexpr (KIND <= 2) {
+        store8<DT, VEC>(c.data, to, left[r], x[r][n]);
+      } else {
+        constexpr float unit = 1.0f / (KIND == kInt8 ? 127.0f : 448.0f);
+        // (magnitudes as whole numbers: infinities and NaN are the largest)
+        uint32_t m = 0;
+#pragma unroll
+        for (int j = 0; j < PN; ++j) {
+          const uint32_t u = __float_as_uint(x[r][n][j]) & 0x7fffffffu;
+          m = u > m ? u : m;
+        }
+        m = team_most<TEAM>(m);
+        const bool odd = m >= 0x7f800000u;
+        const float scale = fmaxf(__uint_as_float(odd ? 0u : m) * unit, 1.17549435e-38f);
+        Move8 codes = encode8<KIND>(x[r][n], scale, m != 0u && scale < 0x1p-90f);
+        if (odd) codes = Move8{0u, 0u};
+        store_codes<VEC>(c.data, to, left[r], codes);
+        if (lane == 0 && page[r] >= 0)
+          c.scale[page[r] * c.scale_page + at.h * c.scale_head + slot[r]] = odd ? NAN : scale;
       }
-      m = team_most<TEAM>(m);
-      const bool odd = m >= 0x7f800000u;
-      const float scale = fmaxf(__uint_as_float(odd ? 0u : m) * unit, 1.17549435e-38f);
-      float y[PN];
-#pragma unroll
-      for (int j = 0; j < PN; ++j) y[j] = odd ? 0.0f : x[n][j] / scale;
-      const Move8 codes = {encode4<KIND>(y), encode4<KIND>(y + 4)};
-      store_codes<VEC>(c.data, to, left, codes);
-      if (lane == 0 && page >= 0)
-        c.scale[page * c.scale_page + h * c.scale_head + slot] = odd ? NAN : scale;
     }
   }
 }
 
-template <int KIND, int DO, int TEAM, bool VEC>
+template <int KIND, int DO, int TEAM, int ROWS, bool VEC>
 __global__ __launch_bounds__(PT) void cache_read_kernel(ReadArgs a) {
   const int lane = threadIdx.x % TEAM;
-  const uint32_t row = blockIdx.x * static_cast<uint32_t>(PT / TEAM) + threadIdx.x / TEAM;
-  const uint32_t total = static_cast<uint32_t>(a.batch) * static_cast<uint32_t>(a.kv) * static_cast<uint32_t>(a.room);
-  if (row >= total) return;
-  const uint32_t bh = row / static_cast<uint32_t>(a.room);
-  const int i = static_cast<int>(row - bh * static_cast<uint32_t>(a.room));
-  const int b = static_cast<int>(bh / static_cast<uint32_t>(a.kv));
-  const int h = static_cast<int>(bh) - b * a.kv;
-  int page = -1, slot = 0;
-  if (i < a.lens[b]) find_slot(a.t, b, i, &page, &slot);
+  const Place<TEAM, ROWS> at(a.batch, a.kv, a.room, a.chunks);
+  const int len = a.lens[at.b];
   const int left = a.dim - PN * lane;
-  float x[PN] = {};
-  if (page >= 0) {
-    const PagedCache& c = a.cache;
-    const int64_t from = page * c.page + h * c.head + slot * c.slot + PN * lane;
-    if constexpr (KIND <= 2) {
-      load8<KIND, VEC>(c.data, from, left, x);
-    } else {
-      const Move8 codes = load_codes<VEC>(c.data, from, left);
-      const float scale = c.scale[page * c.scale_page + h * c.scale_head + slot];
-      decode4<KIND>(codes[0], x);
-      decode4<KIND>(codes[1], x + 4);
+  const PagedCache& c = a.cache;
+  int page[ROWS], slot[ROWS];
 #pragma unroll
-      for (int j = 0; j < PN; ++j) x[j] *= scale;
+  for (int r = 0; r < ROWS; ++r) {
+    page[r] = -1;
+    slot[r] = 0;
+    if (at.there[r] && at.i[r] < len) find_slot(a.t, at.b, at.i[r], &page[r], &slot[r]);
+  }
+  float x[ROWS][PN] = {};
+  Move8 codes[ROWS];
+  float scale[ROWS];
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    codes[r] = Move8{0u, 0u};
+    scale[r] = 0.0f;
+    if (page[r] < 0) continue;
+    const int64_t from = page[r] * c.page + at.h * c.head + slot[r] * c.slot + PN * lane;
+    if constexpr (KIND <= 2) {
+      load8<KIND, VEC>(c.data, from, left, x[r]);
+    } else {
+      codes[r] = load_codes<VEC>(c.data, from, left);
+      scale[r] = c.scale[page[r] * c.scale_page + at.h * c.scale_head + slot[r]];
     }
   }
-  store8<DO, VEC>(a.out, static_cast<int64_t>(row) * a.dim + PN * lane, left, x);
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    if (!at.there[r]) continue;
+    if constexpr (KIND > 2) {
+      decode4<KIND>(codes[r][0], x[r]);
+      decode4<KIND>(codes[r][1], x[r] + 4);
+#pragma unroll
+      for (int j = 0; j < PN; ++j) {
+        x[r][j] *= scale[r];
+        // (a product of float32, not one rounded at once to 16 bits)
+        asm("" : "+v"(x[r][j]));
+      }
+    }
+    const int64_t row = (static_cast<int64_t>(at.b) * a.kv + at.h) * a.room + at.i[r];
+    store8<DO, VEC>(a.out, row * a.dim + PN * lane, left, x[r]);
+  }
 }
 
 }  // namespace
 
 // ------------------------------------------------------------- launchers ---
+// Several rows to a team where a (sequence, head) has enough of them for whole workgroups
+// and the launch fills the chip.
+bool in_chunks(int64_t heads, int64_t rows, int per, int* chunks, int64_t* blocks) {
+  const int64_t all = (rows + 4 * per - 1) / (4 * per);
+  *chunks = static_cast<int>(all);
+  *blocks = heads * all;
+  return rows >= 4 * per && *blocks >= 1024 && *blocks <= 2147483647LL;
+}
+
 hipError_t launch_cache_append(AppendArgs a, int dtype, int kind, bool vec, hipStream_t s) {
-  const int team = a.dim <= 16 * PN ? 16 : 32;
-  const int64_t rows = static_cast<int64_t>(a.batch) * a.kv * a.fresh;
-  const dim3 grid(static_cast<unsigned>((rows + PT / team - 1) / (PT / team)));
+  const int team = a.dim <= 16 * PN ? 16 : 32, per = PT / team;
+  const int64_t heads = static_cast<int64_t>(a.batch) * a.kv;
+  int64_t blocks;
+  const bool four = in_chunks(heads, a.fresh, per, &a.chunks, &blocks);
+  if (!four) blocks = (heads * a.fresh + per - 1) / per;
+  const dim3 grid(static_cast<unsigned>(blocks));
   ProfScope ps_("cache_append", s);
   const auto launch = [&](auto dt, auto kd) {
     constexpr int DT = decltype(dt)::value, KIND = decltype(kd)::value;
-    if (team == 16 && vec) hipLaunchKernelGGL((cache_append_kernel<DT, KIND, 16, true>), grid, dim3(PT), 0, s, a);
-    else if (team == 16) hipLaunchKernelGGL((cache_append_kernel<DT, KIND, 16, false>), grid, dim3(PT), 0, s, a);
-    else if (vec) hipLaunchKernelGGL((cache_append_kernel<DT, KIND, 32, true>), grid, dim3(PT), 0, s, a);
-    else hipLaunchKernelGGL((cache_append_kernel<DT, KIND, 32, false>), grid, dim3(PT), 0, s, a);
+    const auto rows = [&](auto wide, auto n) {
+      constexpr int TEAM = decltype(wide)::value, ROWS = decltype(n)::value;
+      if (vec) hipLaunchKernelGGL((cache_append_kernel<DT, KIND, TEAM, ROWS, true>), grid, dim3(PT), 0, s, a);
+      else hipLaunchKernelGGL((cache_append_kernel<DT, KIND, TEAM, ROWS, false>), grid, dim3(PT), 0, s, a);
+    };
+    const std::integral_constant<int, 1> one;
+    const std::integral_constant<int, 4> more;
+    const std::integral_constant<int, 16> narrow;
+    const std::integral_constant<int, 32> wide;
+    if (team == 16 && four) rows(narrow, more);
+    else if (team == 16) rows(narrow, one);
+    else if (four) rows(wide, more);
+    else rows(wide, one);
   };
   const auto of = [&](auto dt) {
     constexpr int DT = decltype(dt)::value;
@@ -216,16 +323,28 @@ hipError_t launch_cache_append(AppendArgs a, int dtype, int kind, bool vec, hipS
 }
 
 hipError_t launch_cache_read(ReadArgs a, int dtype, int kind, bool vec, hipStream_t s) {
-  const int team = a.dim <= 16 * PN ? 16 : 32;
-  const int64_t rows = static_cast<int64_t>(a.batch) * a.kv * a.room;
-  const dim3 grid(static_cast<unsigned>((rows + PT / team - 1) / (PT / team)));
+  const int team = a.dim <= 16 * PN ? 16 : 32, per = PT / team;
+  const int64_t heads = static_cast<int64_t>(a.batch) * a.kv;
+  int64_t blocks;
+  const bool four = in_chunks(heads, a.room, per, &a.chunks, &blocks);
+  if (!four) blocks = (heads * a.room + per - 1) / per;
+  const dim3 grid(static_cast<unsigned>(blocks));
   ProfScope ps_("cache_read", s);
   const auto launch = [&](auto kd, auto dout) {
     constexpr int KIND = decltype(kd)::value, DO = decltype(dout)::value;
-    if (team == 16 && vec) hipLaunchKernelGGL((cache_read_kernel<KIND, DO, 16, true>), grid, dim3(PT), 0, s, a);
-    else if (team == 16) hipLaunchKernelGGL((cache_read_kernel<KIND, DO, 16, false>), grid, dim3(PT), 0, s, a);
-    else if (vec) hipLaunchKernelGGL((cache_read_kernel<KIND, DO, 32, true>), grid, dim3(PT), 0, s, a);
-    else hipLaunchKernelGGL((cache_read_kernel<KIND, DO, 32, false>), grid, dim3(PT), 0, s, a);
+    const auto rows = [&](auto wide, auto n) {
+      constexpr int TEAM = decltype(wide)::value, ROWS = decltype(n)::value;
+      if (vec) hipLaunchKernelGGL((cache_read_kernel<KIND, DO, TEAM, ROWS, true>), grid, dim3(PT), 0, s, a);
+      else hipLaunchKernelGGL((cache_read_kernel<KIND, DO, TEAM, ROWS, false>), grid, dim3(PT), 0, s, a);
+    };
+    const std::integral_constant<int, 1> one;
+    const std::integral_constant<int, 4> more;
+    const std::integral_constant<int, 16> narrow;
+    const std::integral_constant<int, 32> wide;
+    if (team == 16 && four) rows(narrow, more);
+    else if (team == 16) rows(narrow, one);
+    else if (four) rows(wide, more);
+    else rows(wide, one);
   };
   const auto to = [&](auto dout) {
     constexpr int DO = decltype(dout)::value;

@@ -44,17 +44,10 @@ __device__ __forceinline__ void decode4(uint32_t w, float* x) {
 // Four floats within the codes' range, each to the nearest code, ties to even.
 template <int KIND>
 __device__ __forceinline__ uint32_t encode4(const float* x) {
-  if constexpr (KIND == kInt8) {
-    uint32_t w = 0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      w |= (static_cast<uint32_t>(static_cast<int>(rintf(x[j]))) & 0xffu) << (8 * j);
-    return w;
-  } else {
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
-    w = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], w, true);
-    return static_cast<uint32_t>(w);
-  }
+  static_assert(KIND == kE4m3, "the others are whole numbers");
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
+  w = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], w, true);
+  return static_cast<uint32_t>(w);
 }
 
 }  // namespace lapsum

@@ -103,6 +103,30 @@ def test_append_and_read(lib, batch, kv, new, dim, slots, paged, dtype, kind):
                 assert bool(torch.equal(_bits(got[b].cpu()), _bits(line.to(getattr(torch, to)))))
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim", [40, 128, 200])
+def test_many_entries(lib, dim, dtype, kind):
+    """Rows in whole workgroups, and every rounding of a few hundred thousand elements."""
+    torch = _torch()
+    gen = _gen(dim)
+    batch, kv, new, slots = 4, 4, 4500, 16
+    pages, table = _pages(batch, 282, slots, 1)
+    x = torch.randn(2, batch, kv, new, dim, generator=gen, device="cuda").to(getattr(torch, dtype))
+    seen = torch.tensor([0, 3, 12, 11], dtype=torch.int32, device="cuda")
+    k, ks = _empty((pages, kv, slots, dim), kind, dtype)
+    v, vs = _empty((pages, kv, slots, dim), kind, dtype)
+    lib.lapsum_cache_append(x[0], x[1], seen, k, v, table=table, k_scale=ks, v_scale=vs)
+    for c, s, rows in ((k, ks, x[0]), (v, vs, x[1])):
+        want, scale = (rows.cpu(), None) if kind == "same" else _quantised(rows, kind)
+        back = lib.lapsum_cache_read(c, seen + new, 4512, table=table, scale=s)
+        value = want if scale is None else want.float() * scale[..., None]
+        for b in range(batch):
+            at = int(seen[b])
+            assert bool(torch.equal(_bits(back[b, :, at:at + new].cpu()), _bits(value[b])))
+            assert not back[b, :, at + new:].any()
+
+
 @pytest.mark.parametrize("kind", ["int8", "float8_e4m3fn"])
 def test_rows_at_the_ends_of_the_range(lib, kind):
     torch = _torch()
