@@ -149,11 +149,11 @@ __global__ __launch_bounds__(S::T, S::M >= 128 ? 2 : 4) void expert_grad_kernel(
       const int n = n0 + wn + 16 * j + 4 * (lane >> 4);
       if (n >= a.n) continue;
       if (a.splits > 1)
-        store4<0, DIRECT>(reinterpret_cast<uint32_t*>(a.part) +
+        store4<0>(reinterpret_cast<uint32_t*>(a.part) +
                               ((static_cast<int64_t>(split) * a.experts + e) * a.m + m) * a.n + n,
                           acc[i][j], a.n - n);
       else
-        store4<DT, DIRECT>(static_cast<raw*>(a.c) + a.c_expert * e + m * a.c_row + n, acc[i][j], a.n - n);
+        store4<DT>(static_cast<raw*>(a.c) + a.c_expert * e + m * a.c_row + n, acc[i][j], a.n - n);
     }
   }
 }
@@ -175,12 +175,13 @@ __global__ __launch_bounds__(256) void expert_grad_join_kernel(GradArgs a) {
 }  // namespace
 
 // ------------------------------------------------------------- launchers ---
-// How many workgroups share an expert's rows: enough for two of 64 x 64 results per
+// How many workgroups share an expert's rows: enough for eight of 64 x 64 results per
 // compute unit, as long as each has 256 rows.
 int grad_splits(int64_t experts, int64_t rows, int64_t m, int64_t n) {
   const int64_t tiles = experts * ((m + 63) / 64) * ((n + 63) / 64);
+  if (tiles >= 1024) return 1;
   const int64_t most = rows / experts / 256;
-  const int64_t want = (511 + tiles) / tiles;
+  const int64_t want = (2047 + tiles) / tiles;
   return static_cast<int>(want < most ? (want < 1 ? 1 : want) : (most < 1 ? 1 : most));
 }
 

@@ -156,7 +156,7 @@ __global__ __launch_bounds__(S::T, S::M >= 128 ? 2 : 4) void expert_rows_kernel(
 #pragma unroll
     for (int j = 0; j < S::TN / 16; ++j) {
       const int n = n0 + wn + 16 * j + 4 * (lane >> 4);
-      if (n < a.n) store4<DO, DIRECT>(y + n, acc[i][j], a.n - n);
+      if (n < a.n) store4<DO>(y + n, acc[i][j], a.n - n);
     }
   }
 }
@@ -183,6 +183,8 @@ hipError_t launch_expert_rows(RowsArgs a, int dtype, bool w_n_dense, bool out_f3
     const int64_t tiles = (a.rows / 128 + (a.experts < a.rows ? a.experts : a.rows)) * ((a.n + 127) / 128);
     const std::true_type yes;
     const std::false_type no;
+    // (most of a taller tile would be rows of none)
+    const bool few = a.rows <= static_cast<int64_t>(a.experts) * 16;
     // Few large tiles leave compute units idle, small ones read more than the die's
     // cache delivers.  Rows of 128 bytes are two steps of 64 and want both at
     // once; where w is dense along n one step's rows of it are long.  16384 rows of
@@ -193,8 +195,10 @@ hipError_t launch_expert_rows(RowsArgs a, int dtype, bool w_n_dense, bool out_f3
       launch(dt, dout, dense, yes, Shape<128, 256, 128, 64, 1, 3>{});
     else if (DT != 0 && direct && !w_n_dense && tiles >= 2048 && a.rows / a.experts >= 256)
       launch(dt, dout, dense, yes, Shape<256, 256, 128, 64, 2, 2>{});
-    else if (direct && tiles >= 512) launch(dt, dout, dense, yes, Shape<128, 128, 64, 64, 2, 2>{});
-    else if (direct) launch(dt, dout, dense, yes, Shape<64, 64, 32, 32, 2, 2>{});
+    else if (direct && tiles >= 512 && !few) launch(dt, dout, dense, yes, Shape<128, 128, 64, 64, 2, 2>{});
+    else if (direct && !few) launch(dt, dout, dense, yes, Shape<64, 64, 32, 32, 2, 2>{});
+    else if (direct) launch(dt, dout, dense, yes, Shape<16, 64, 16, 32, 2, 2>{});
+    else if (few) launch(dt, dout, dense, no, Shape<16, 64, 16, 32, 2, 1>{});
     else if (tiles >= 512) launch(dt, dout, dense, no, Shape<128, 128, 64, 64, 2, 1>{});
     else launch(dt, dout, dense, no, Shape<64, 64, 32, 32, 2, 1>{});
   };

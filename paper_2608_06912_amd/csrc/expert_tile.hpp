@@ -211,24 +211,23 @@ __device__ __forceinline__ void contract(char* lds, Bring& bring, int count, int
   }
 }
 
-// Four results of a row that lie side by side.
-template <int DT, bool VEC>
+// Four results of a row that lie side by side (memory serves vectors at any alignment of
+// their elements).
+template <int DT>
 __device__ __forceinline__ void store4(typename Elem<DT>::raw* p, Acc v, int left) {
-  if (VEC && left >= 4) {
-    if constexpr (DT == 0) {
-      *reinterpret_cast<Acc*>(p) = v;
-    } else {
-      Move8 u;
+  using raw = typename Elem<DT>::raw;
+  struct __attribute__((packed, aligned(sizeof(raw)))) Any {
+    raw x[4];
+  };
+  Any u;
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
-        u[j] = static_cast<uint32_t>(Elem<DT>::put(v[2 * j])) |
-               (static_cast<uint32_t>(Elem<DT>::put(v[2 * j + 1])) << 16);
-      *reinterpret_cast<Move8*>(p) = u;
-    }
+  for (int j = 0; j < 4; ++j) u.x[j] = Elem<DT>::put(v[j]);
+  if (left >= 4) {
+    *reinterpret_cast<Any*>(p) = u;
   } else {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (j < left) p[j] = Elem<DT>::put(v[j]);
+      if (j < left) p[j] = u.x[j];
   }
 }
 

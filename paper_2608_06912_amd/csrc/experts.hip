@@ -144,6 +144,16 @@ __device__ __forceinline__ void load_row(const void* p, int64_t at, int left, fl
         x[2 * j + 1] = Elem<DT>::get(v[j] >> 16);
       }
     }
+  } else if (left == N) {
+    // (global memory serves vectors at any alignment of their elements)
+    struct __attribute__((packed, aligned(sizeof(raw)))) Any {
+      uint32_t w[N * sizeof(raw) / 4];
+    };
+    const Any v = *reinterpret_cast<const Any*>(q);
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      x[j] = DT == 0 ? __uint_as_float(v.w[j % (N * sizeof(raw) / 4)])
+                     : Elem<DT>::get((v.w[j / 2] >> (16 * (j % 2))) & 0xffffu);
   } else {
 #pragma unroll
     for (int j = 0; j < N; ++j) x[j] = j < left ? Elem<DT>::get(q[j]) : 0.0f;
@@ -170,6 +180,18 @@ __device__ __forceinline__ void store_row(void* p, int64_t at, int left, const f
                (static_cast<uint32_t>(Elem<DT>::put(x[2 * j + 1])) << 16);
       *reinterpret_cast<Move16*>(q) = v;
     }
+  } else if (left == N) {
+    struct __attribute__((packed, aligned(sizeof(raw)))) Any {
+      uint32_t w[N * sizeof(raw) / 4];
+    };
+    Any v;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      if constexpr (DT == 0) v.w[j] = __float_as_uint(x[j]);
+      else if (j % 2 == 0) v.w[j / 2] = Elem<DT>::put(x[j]);
+      else v.w[j / 2] |= static_cast<uint32_t>(Elem<DT>::put(x[j])) << 16;
+    }
+    *reinterpret_cast<Any*>(q) = v;
   } else {
 #pragma unroll
     for (int j = 0; j < N; ++j)
@@ -317,7 +339,9 @@ hipError_t launch_expert_combine_backward(const CombineGradArgs& a, int dtype, b
   ProfScope ps_("expert_combine_backward", s);
   const auto launch = [&](auto dt) {
     constexpr int DT = decltype(dt)::value;
-    if (!vec) hipLaunchKernelGGL((expert_combine_backward_kernel<DT, 1, false>), grid, dim3(256), 0, s, a);
+    if (!vec && a.dim <= CW)
+      hipLaunchKernelGGL((expert_combine_backward_kernel<DT, 1, false>), grid, dim3(256), 0, s, a);
+    else if (!vec) hipLaunchKernelGGL((expert_combine_backward_kernel<DT, 4, false>), grid, dim3(256), 0, s, a);
     else if (a.dim <= CW) hipLaunchKernelGGL((expert_combine_backward_kernel<DT, 1, true>), grid, dim3(256), 0, s, a);
     else if (a.dim <= 2 * CW) hipLaunchKernelGGL((expert_combine_backward_kernel<DT, 2, true>), grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL((expert_combine_backward_kernel<DT, 4, true>), grid, dim3(256), 0, s, a);
