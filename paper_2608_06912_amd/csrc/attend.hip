@@ -173,6 +173,14 @@ __global__ __launch_bounds__(AT, ND == 8 || (QT == 0 && ND > 2) ? 1 : 2) void ca
   const int from = static_cast<int>(max(start, base));
   const int to = static_cast<int>(min(len, base + a.chunk));
 
+  const int64_t first_row = static_cast<int64_t>(b) * a.heads + head0;
+  if (a.part && from >= to) {
+    float* part = a.part + (static_cast<int64_t>(split) * a.batch * a.heads + first_row) * (a.dim + 2);
+    for (int r = wave; r < live; r += AW)
+      for (int d = lane; d < a.dim + 2; d += kWave) part[r * (a.dim + 2) + d] = d == a.dim ? -INFINITY : 0.0f;
+    return;
+  }
+
   Move16 q[KS][TQ];
 #pragma unroll
   for (int s = 0; s < KS; ++s) {
@@ -248,22 +256,34 @@ __global__ __launch_bounds__(AT, ND == 8 || (QT == 0 && ND > 2) ? 1 : 2) void ca
     }
   };
   const auto load = [&](St& st, int key0) {
+    const char *pk = nullptr, *pv = nullptr;
+    const float *sk = nullptr, *sv = nullptr;
+    int last = 0;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       if constexpr (UNIFORM) {
-        const int key = key0 + 16 * u;
-        int page = page_of[u];
-        int slot = key;
-        if (table) slot = key - static_cast<int>(divide(static_cast<uint32_t>(key), a.by)) * a.t.size;
-        else page = key < a.t.size ? b : -1;
-        page = __builtin_amdgcn_readfirstlane(page);
-        st.page[u] = page >= 0 && page < a.t.pages;
-        if (!st.page[u]) page = slot = 0;
-        const char* pk = head_k + (page * a.k.page + slot * a.k.slot) * B;
-        const char* pv = head_v + (page * a.v.page + slot * a.v.slot) * B;
-        const float* sk = KIND > 2 ? scale_k + (page * a.k.scale_page + slot) : nullptr;
-        const float* sv = KIND > 2 ? scale_v + (page * a.v.scale_page + slot) : nullptr;
-        const int last = a.t.size - 1 - slot;
+        if (u == 1 && last >= 31) {   // the second sixteen follow the first
+          st.page[1] = st.page[0];
+          pk += 16 * slot_k;
+          pv += 16 * slot_v;
+          sk += 16;
+          sv += 16;
+          last -= 16;
+        } else {
+          const int key = key0 + 16 * u;
+          int page = page_of[u];
+          int slot = key;
+          if (table) slot = key - static_cast<int>(divide(static_cast<uint32_t>(key), a.by)) * a.t.size;
+          else page = key < a.t.size ? b : -1;
+          page = __builtin_amdgcn_readfirstlane(page);
+          st.page[u] = page >= 0 && page < a.t.pages;
+          if (!st.page[u]) page = slot = 0;
+          pk = head_k + (page * a.k.page + slot * a.k.slot) * B;
+          pv = head_v + (page * a.v.page + slot * a.v.slot) * B;
+          sk = KIND > 2 ? scale_k + (page * a.k.scale_page + slot) : nullptr;
+          sv = KIND > 2 ? scale_v + (page * a.v.scale_page + slot) : nullptr;
+          last = a.t.size - 1 - slot;
+        }
         if (last >= 15) {
 #pragma unroll
           for (int s = 0; s < KS; ++s) st.k[u][s].load(pk + k_at(s), 0);
@@ -331,7 +351,7 @@ __global__ __launch_bounds__(AT, ND == 8 || (QT == 0 && ND > 2) ? 1 : 2) void ca
   float m = -INFINITY, l = 0.0f;
   Acc out[VC][VN] = {};
   const float scale2 = (a.scale == 0.0f ? 1.0f : fabsf(a.scale)) * static_cast<float>(kLog2e);
-  float* scores = a.weights ? a.weights + (static_cast<int64_t>(b) * a.heads + head0 + i16) * a.room : nullptr;
+  float* scores = a.weights ? a.weights + (first_row + i16) * a.room : nullptr;
 
   const auto use = [&](St& st, int key0) {
     Acc sc[2] = {};
@@ -520,7 +540,7 @@ __global__ __launch_bounds__(AT, ND == 8 || (QT == 0 && ND > 2) ? 1 : 2) void ca
       mw[w] = mw[w] == -INFINITY ? 0.0f : exp2_fast(mw[w] - top);
       sum += mw[w] * parts[w][r][ND * 32 + 1];
     }
-    const int64_t row = static_cast<int64_t>(b) * a.heads + head0 + r;
+    const int64_t row = first_row + r;
     float* part = a.part ? a.part + (static_cast<int64_t>(split) * a.batch * a.heads + row) * (a.dim + 2) : nullptr;
     for (int d = lane; d < a.dim; d += kWave) {
       float y = 0.0f;
@@ -567,8 +587,7 @@ __global__ __launch_bounds__(JT) void cache_attend_join_kernel(AttendArgs a, flo
   for (int s = threadIdx.x; s < a.splits; s += JT) {
     const float m = factor[s], f = m == -INFINITY ? 0.0f : exp2_fast(m - top);
     factor[s] = f;
-    // (a part without keys is all zeros)
-    sum += f * part[s * step + a.dim + 1];
+    sum += f * part[s * step + a.dim + 1];   // (a part without keys is all zeros)
   }
   sum = wave_sum(sum);
   if (lane == 0) shared[1][wave] = sum;

@@ -140,20 +140,28 @@ __global__ __launch_bounds__(S::T, S::M >= 128 ? 2 : 4) void expert_grad_kernel(
   if constexpr (DIRECT) direct<DT, WAY, S>(a, lo, hi, m0, n0, wm, wn, acc);
   else staged<DT, S>(a, lo, hi, m0, n0, wm, wn, acc);
   using raw = typename Elem<DT>::raw;
+  constexpr bool lines = DIRECT && DT != 0 && S::TN % 64 == 0;   // (such tiles have no splits)
 #pragma unroll
   for (int i = 0; i < S::TM / 16; ++i) {
     const int m = m0 + wm + 16 * i + (lane & 15);
-    if (m >= a.m) continue;
+    raw* c = static_cast<raw*>(a.c) + a.c_expert * e + m * a.c_row;
+    if constexpr (lines) {
 #pragma unroll
-    for (int j = 0; j < S::TN / 16; ++j) {
-      const int n = n0 + wn + 16 * j + 4 * (lane >> 4);
-      if (n >= a.n) continue;
-      if (a.splits > 1)
-        store4<0>(reinterpret_cast<uint32_t*>(a.part) +
-                              ((static_cast<int64_t>(split) * a.experts + e) * a.m + m) * a.n + n,
-                          acc[i][j], a.n - n);
-      else
-        store4<DT>(static_cast<raw*>(a.c) + a.c_expert * e + m * a.c_row + n, acc[i][j], a.n - n);
+      for (int j = 0; j < S::TN / 16; j += 4) {
+        const int n = n0 + wn + 16 * j;
+        store_line<DT>(c + n, &acc[i][j], m < a.m ? a.n - n : 0);
+      }
+    } else if (m < a.m) {
+#pragma unroll
+      for (int j = 0; j < S::TN / 16; ++j) {
+        const int n = n0 + wn + 16 * j + 4 * (lane >> 4);
+        if (n >= a.n) continue;
+        if (a.splits > 1)
+          store4<0>(reinterpret_cast<uint32_t*>(a.part) +
+                        ((static_cast<int64_t>(split) * a.experts + e) * a.m + m) * a.n + n,
+                    acc[i][j], a.n - n);
+        else store4<DT>(c + n, acc[i][j], a.n - n);
+      }
     }
   }
 }
@@ -203,9 +211,13 @@ hipError_t launch_expert_grad(GradArgs a, int dtype, bool vec, hipStream_t s) {
     const auto big = [&](auto yes) {
       // the training layer's 8 matrices of 2048 x 4096 (and 128 of 2048 x 1536 from 131072
       // rows), us: 256 x 256 338 (1072), 128 x 256 266 (956), 128 x 128 301 (1168)
-      if (decltype(dt)::value != 0 && tiles >= 1024 && a.splits == 1)
-        launch(dt, yes, Shape<128, 256, 128, 64, 1, 3>{});
-      else if (tiles >= 512 && a.splits == 1) launch(dt, yes, Shape<128, 128, 64, 64, 2, 2>{});
+      if constexpr (decltype(dt)::value != 0) {
+        if (tiles >= 1024 && a.splits == 1) {
+          launch(dt, yes, Shape<128, 256, 128, 64, 1, 3>{});
+          return;
+        }
+      }
+      if (tiles >= 512 && a.splits == 1) launch(dt, yes, Shape<128, 128, 64, 64, 2, 2>{});
       else launch(dt, yes, Shape<64, 64, 32, 32, 2, 2>{});
     };
     {

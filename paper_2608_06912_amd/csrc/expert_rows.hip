@@ -148,15 +148,24 @@ __global__ __launch_bounds__(S::T, S::M >= 128 ? 2 : 4) void expert_rows_kernel(
     else staged<DT, N_DENSE, S>(a, t, n0, wm, wn, acc);
   }
   using out = typename Elem<DO>::raw;
+  constexpr bool lines = DIRECT && DO != 0 && S::TN % 64 == 0;
 #pragma unroll
   for (int i = 0; i < S::TM / 16; ++i) {
     const int r = t.row + wm + 16 * i + (lane & 15);
-    if (r >= t.end) continue;
+    const bool in = r < t.end;   // (all lanes take part in an exchange)
     out* y = static_cast<out*>(a.y) + static_cast<int64_t>(r) * a.n;
+    if constexpr (lines) {
 #pragma unroll
-    for (int j = 0; j < S::TN / 16; ++j) {
-      const int n = n0 + wn + 16 * j + 4 * (lane >> 4);
-      if (n < a.n) store4<DO>(y + n, acc[i][j], a.n - n);
+      for (int j = 0; j < S::TN / 16; j += 4) {
+        const int n = n0 + wn + 16 * j;
+        store_line<DO>(y + n, &acc[i][j], in ? a.n - n : 0);
+      }
+    } else if (in) {
+#pragma unroll
+      for (int j = 0; j < S::TN / 16; ++j) {
+        const int n = n0 + wn + 16 * j + 4 * (lane >> 4);
+        if (n < a.n) store4<DO>(y + n, acc[i][j], a.n - n);
+      }
     }
   }
 }
@@ -191,11 +200,17 @@ hipError_t launch_expert_rows(RowsArgs a, int dtype, bool w_n_dense, bool out_f3
     // 8 experts 2048 -> 4096 in bfloat16 (and 131072 of 128, 2048 -> 1536), us:
     //   w dense along n   256 x 256 307 (854), 128 x 256 284 (856), 128 x 128 301 (1001)
     //   w dense along k   256 x 256 284 (847), 128 x 256 316 (942), 128 x 128 290 (990)
-    if (DT != 0 && direct && w_n_dense && tiles >= 1024 && a.rows / a.experts >= 128)
-      launch(dt, dout, dense, yes, Shape<128, 256, 128, 64, 1, 3>{});
-    else if (DT != 0 && direct && !w_n_dense && tiles >= 2048 && a.rows / a.experts >= 256)
-      launch(dt, dout, dense, yes, Shape<256, 256, 128, 64, 2, 2>{});
-    else if (direct && tiles >= 512 && !few) launch(dt, dout, dense, yes, Shape<128, 128, 64, 64, 2, 2>{});
+    const int64_t each = a.rows / a.experts;
+    const bool large = DT != 0 && direct && (dense ? tiles >= 1024 && each >= 128 : tiles >= 2048 && each >= 256);
+    if constexpr (DT != 0) {
+      if constexpr (dense) {
+        if (large) launch(dt, dout, dense, yes, Shape<128, 256, 128, 64, 1, 3>{});
+      } else {
+        if (large) launch(dt, dout, dense, yes, Shape<256, 256, 128, 64, 2, 2>{});
+      }
+    }
+    if (large) return;
+    if (direct && tiles >= 512 && !few) launch(dt, dout, dense, yes, Shape<128, 128, 64, 64, 2, 2>{});
     else if (direct && !few) launch(dt, dout, dense, yes, Shape<64, 64, 32, 32, 2, 2>{});
     else if (direct) launch(dt, dout, dense, yes, Shape<16, 64, 16, 32, 2, 2>{});
     else if (few) launch(dt, dout, dense, no, Shape<16, 64, 16, 32, 2, 1>{});

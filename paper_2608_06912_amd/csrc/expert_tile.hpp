@@ -216,19 +216,54 @@ __device__ __forceinline__ void contract(char* lds, Bring& bring, int count, int
 template <int DT>
 __device__ __forceinline__ void store4(typename Elem<DT>::raw* p, Acc v, int left) {
   using raw = typename Elem<DT>::raw;
+  constexpr int words = sizeof(raw);
   struct __attribute__((packed, aligned(sizeof(raw)))) Any {
-    raw x[4];
+    uint32_t w[words];
   };
   Any u;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) u.x[j] = Elem<DT>::put(v[j]);
+  for (int j = 0; j < words; ++j) {
+    if constexpr (DT == 0) u.w[j] = __float_as_uint(v[j]);
+    else
+      u.w[j] = static_cast<uint32_t>(Elem<DT>::put(v[2 * j])) |
+               (static_cast<uint32_t>(Elem<DT>::put(v[2 * j + 1])) << 16);
+  }
   if (left >= 4) {
     *reinterpret_cast<Any*>(p) = u;
   } else {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (j < left) p[j] = u.x[j];
+      if (j < left) p[j] = Elem<DT>::put(v[j]);
   }
+}
+
+// The results of a row in four tiles side by side, 16-bit and in whole vectors: lanes
+// exchange quarters, so that each has 16 neighbouring ones and a row's four lanes a line
+// of 128 bytes (32 bytes of it at a time otherwise).  p: the first tile's first column,
+// of which `left` exist.
+template <int DT>
+__device__ __forceinline__ void store_line(typename Elem<DT>::raw* p, const Acc* v, int left) {
+  uint32_t w[4][2];
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      w[j][h] = static_cast<uint32_t>(Elem<DT>::put(v[j][2 * h])) |
+                (static_cast<uint32_t>(Elem<DT>::put(v[j][2 * h + 1])) << 16);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const auto a = __builtin_amdgcn_permlane32_swap(w[0][h], w[2][h], false, false);
+    const auto b = __builtin_amdgcn_permlane32_swap(w[1][h], w[3][h], false, false);
+    const auto c = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false);
+    const auto d = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
+    w[0][h] = c[0];
+    w[1][h] = c[1];
+    w[2][h] = d[0];
+    w[3][h] = d[1];
+  }
+  const int first = 16 * (lane_id() >> 4);
+  if (first < left) *reinterpret_cast<Move16*>(p + first) = Move16{w[0][0], w[0][1], w[1][0], w[1][1]};
+  if (first + 8 < left) *reinterpret_cast<Move16*>(p + first + 8) = Move16{w[2][0], w[2][1], w[3][0], w[3][1]};
 }
 
 // Workgroups are dealt out to the eight dies in turn, each with a cache of its own: in
