@@ -630,12 +630,15 @@ __global__ __launch_bounds__(256) void cache_weights_kernel(AttendArgs a) {
 }  // namespace
 
 // ------------------------------------------------------------- launchers ---
+// A workgroup's keys: as many workgroups as are on the chip twice over, of at least a step
+// for each wave.  More of them begin and end more often: four contexts of 131072 take
+// 335 us with 1024 workgroups, 346 with 2048, 361 with 4096, 382 with 8192.
 void attend_plan(int64_t batch, int64_t heads, int64_t kv, int64_t room, int64_t window, int* splits,
                  int* chunk) {
   constexpr int64_t step = AK * AW;
   const int64_t rows = batch * kv * ((heads / kv + 15) / 16);
   const int64_t keys = window > 0 && window < room ? (window + AK < room ? window + AK : room) : room;
-  int64_t each = (keys * rows + 4095) / 4096;
+  int64_t each = (keys * rows + 1023) / 1024;
   each = (each + step - 1) / step * step;
   if (each < step) each = step;
   *chunk = static_cast<int>(each);
