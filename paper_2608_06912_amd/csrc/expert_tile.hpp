@@ -5,6 +5,9 @@
 // (16 bytes a lane, at the wave's address and on), so the next stages are on their way
 // while one is multiplied, in buffers of their own, and take no registers.  Elements
 // that do not exist are asked for beyond the buffer's end, where loads give 0.
+// The fragments of a step are read from LDS while the step before it is multiplied, also
+// across the barrier that a stage ends with: reading them when they are due cost
+// 131072 rows of 128 experts 2048 -> 1536 973 us, ahead 880.
 // That needs whole vectors, and operands of less than 4 GiB.  Else: through
 // registers, element by element at the ends.
 #pragma once

@@ -11,9 +11,13 @@
 // nothing.  Places without an expert are those of one expert more, so they come
 // last.
 //
+// 131072 places of 128 experts take 17 us in two launches, 64 places of 64 2.9 in one:
+// chains of loads, counts and ballots.
+//
 // Sum.  out_t = sum_j w_tj y_row(t, j): a gather of rows, without atomics, in the order
 // of the slots.  Backward: dy_row(t, j) = w_tj g_t and dw_tj = <g_t, y_row(t, j)>
-// from one read of g_t and y.
+// from one read of g_t and y.  Both are bound by memory: 16384 tokens of 8 rows of 2048
+// in bfloat16 take 140 us (4.3 TB/s) and 214 us (5.3 TB/s).
 #include "select_common.hpp"
 
 namespace lapsum {
