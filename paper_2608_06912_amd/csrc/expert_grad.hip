@@ -7,7 +7,7 @@
 // split over several workgroups, whose float32 parts expert_grad_join_kernel adds in
 // their order.  8 matrices of 2048 x 4096 from 16384 rows in bfloat16 take 266 us
 // (1034 TFLOP/s), bound as the products are; 4 of 283 x 184 from 31538 rows in float32
-// 62 + 8 us with 30 splits, 1.3 ms without.
+// 53 + 8 us with 30 splits, 375 without.
 #include "expert_tile.hpp"
 
 namespace lapsum {
@@ -95,11 +95,12 @@ __device__ __forceinline__ void staged(const GradArgs& a, int lo, int hi, int m0
   Staged<B, S::T> sb;
   const auto side = [&](auto& s, const void* p, const int32_t* order, int64_t count, int64_t stride, int r0,
                         int first, int width) {
+    s.width = width;
 #pragma unroll
     for (int i = 0; i < s.Each; ++i) {
       const int r = r0 + s.row(i), c = first + A::N * s.chunk(i);
       const int64_t src = r < hi ? source_row(order, a.by, count, r) : -1;
-      s.v[i] = load_chunk<DT, false>(static_cast<const raw*>(p) + src * stride + c, src < 0 ? 0 : width - c);
+      s.template load<DT>(i, static_cast<const raw*>(p) + src * stride + c, src < 0 ? 0 : width - c);
     }
   };
   const auto load = [&](int r0) {
@@ -108,8 +109,8 @@ __device__ __forceinline__ void staged(const GradArgs& a, int lo, int hi, int m0
   };
   load(lo);
   for (int r0 = lo; r0 < hi; r0 += A::Stage) {
-    sa.put(lds);
-    sb.put(lds + A::Bytes);
+    sa.template put<DT>(lds);
+    sb.template put<DT>(lds + A::Bytes);
     __syncthreads();
     if (r0 + A::Stage < hi) load(r0 + A::Stage);
     multiply<DT, A, B, S>(lds, wm, wn, acc);

@@ -106,6 +106,8 @@ __device__ __forceinline__ void staged(const RowsArgs& a, const Tile& t, int n0,
   const auto* w = static_cast<const typename P::raw*>(a.w) + a.w_expert * t.expert;
   Staged<A, S::T> sa;
   Staged<B, S::T> sb;
+  sa.width = a.k;
+  sb.width = N_DENSE ? a.n : a.k;
   int64_t at[sa.Each];
 #pragma unroll
   for (int i = 0; i < sa.Each; ++i) {
@@ -117,7 +119,7 @@ __device__ __forceinline__ void staged(const RowsArgs& a, const Tile& t, int n0,
 #pragma unroll
     for (int i = 0; i < sa.Each; ++i) {
       const int k = k0 + A::N * sa.chunk(i);
-      sa.v[i] = load_chunk<DT, false>(x + at[i] + k, at[i] < 0 ? 0 : a.k - k);
+      sa.template load<DT>(i, x + at[i] + k, at[i] < 0 ? 0 : a.k - k);
     }
 #pragma unroll
     for (int i = 0; i < sb.Each; ++i) {
@@ -125,13 +127,13 @@ __device__ __forceinline__ void staged(const RowsArgs& a, const Tile& t, int n0,
       const int64_t line = N_DENSE ? k0 + r : n0 + r;
       const int col = N_DENSE ? n0 + c : k0 + c;
       const bool in = line < (N_DENSE ? a.k : a.n);
-      sb.v[i] = load_chunk<DT, false>(w + line * a.w_row + col, in ? (N_DENSE ? a.n : a.k) - col : 0);
+      sb.template load<DT>(i, w + line * a.w_row + col, in ? sb.width - col : 0);
     }
   };
   load(0);
   for (int k0 = 0; k0 < a.k; k0 += A::Stage) {
-    sa.put(lds);
-    sb.put(lds + A::Bytes);
+    sa.template put<DT>(lds);
+    sb.template put<DT>(lds + A::Bytes);
     __syncthreads();
     if (k0 + A::Stage < a.k) load(k0 + A::Stage);
     multiply<DT, A, B, S>(lds, wm, wn, acc);

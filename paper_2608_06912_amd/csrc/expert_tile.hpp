@@ -8,8 +8,8 @@
 // The fragments of a step are read from LDS while the step before it is multiplied, also
 // across the barrier that a stage ends with: reading them when they are due cost
 // 131072 rows of 128 experts 2048 -> 1536 973 us, ahead 880.
-// That needs whole vectors, and operands of less than 4 GiB.  Else: through
-// registers, element by element at the ends.
+// That needs lines of whole, aligned vectors, and operands of less than 4 GiB.  Else:
+// through registers.
 #pragma once
 
 #include "matrix.hpp"
@@ -69,9 +69,17 @@ template <class Op, int T>
 struct Staged : Chunks<Op, T> {
   using C = Chunks<Op, T>;
   Move16 v[C::Each];
+  int left[C::Each], width;   // of the lines that the chunks are from
+  template <int DT>
+  __device__ __forceinline__ void load(int i, const typename Elem<DT>::raw* p, int exist) {
+    left[i] = exist;
+    v[i] = load_chunk<DT>(p, exist, width);
+  }
+  template <int DT>
   __device__ __forceinline__ void put(char* lds) const {
 #pragma unroll
-    for (int i = 0; i < C::Each; ++i) *reinterpret_cast<Move16*>(lds + 16 * C::slot(i)) = v[i];
+    for (int i = 0; i < C::Each; ++i)
+      *reinterpret_cast<Move16*>(lds + 16 * C::slot(i)) = trim_chunk<DT>(v[i], left[i], width);
   }
 };
 

@@ -35,29 +35,44 @@ __device__ __forceinline__ Acc mma(Move16 a, Move16 b, Acc c) {
   }
 }
 
-// The chunk at p of which `left` elements exist (the others are 0).  VEC: a chunk
-// exists whole or not at all, at a multiple of 16 bytes.
-template <int DT, bool VEC>
-__device__ __forceinline__ Move16 load_chunk(const typename Elem<DT>::raw* p, int64_t left) {
+// The chunk at p of which `left` elements exist, the end of a line of `width` elements.
+// A line's last chunk is read as the whole vector that the line ends with, and trim_chunk
+// moves it to its place, zeros behind, once it is there (element by element, each
+// load waited for, 16384 rows of 8 experts 2047 -> 1023 cost 275 us instead of 158).
+// Lines shorter than a chunk are read by elements, all of them at once.
+template <int DT>
+__device__ __forceinline__ Move16 load_chunk(const typename Elem<DT>::raw* p, int64_t left, int width) {
   constexpr int N = 16 / sizeof(typename Elem<DT>::raw);
   Move16 v = {0u, 0u, 0u, 0u};
-  if constexpr (VEC) {
-    if (left > 0) v = *reinterpret_cast<const Move16*>(p);
-  } else if (left >= N) {
+  if (left <= 0) return v;
+  if (width >= N) {
     // (global memory serves vectors at any alignment of their elements)
     struct __attribute__((packed, aligned(sizeof(*p)))) Any {
       uint32_t x, y, z, w;
     };
-    const Any u = *reinterpret_cast<const Any*>(p);
+    const Any u = *reinterpret_cast<const Any*>(left < N ? p + (left - N) : p);
     v = Move16{u.x, u.y, u.z, u.w};
   } else {
+    uint32_t e[N];
 #pragma unroll
-    for (int j = 0; j < N; ++j)
-      if (j < left) {
-        if constexpr (DT == 0) v[j] = p[j];
-        else v[j / 2] |= static_cast<uint32_t>(p[j]) << (16 * (j % 2));
-      }
+    for (int j = 0; j < N; ++j) e[j] = p[j < left ? j : left - 1];
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      if constexpr (DT == 0) v[j] = j < left ? e[j] : 0u;
+      else v[j / 2] |= (j < left ? e[j] : 0u) << (16 * (j % 2));
+    }
   }
+  return v;
+}
+template <int DT>
+__device__ __forceinline__ Move16 trim_chunk(Move16 v, int64_t left, int width) {
+  constexpr int N = 16 / sizeof(typename Elem<DT>::raw);
+  if (width < N || left >= N || left <= 0) return v;
+  const int back = N - static_cast<int>(left), words = DT == 0 ? back : back / 2;
+  if (words & 2) v = Move16{v[2], v[3], 0u, 0u};
+  if (words & 1) v = Move16{v[1], v[2], v[3], 0u};
+  if (DT != 0 && (back & 1))
+    v = Move16{v[0] >> 16 | v[1] << 16, v[1] >> 16 | v[2] << 16, v[2] >> 16 | v[3] << 16, v[3] >> 16};
   return v;
 }
 

@@ -160,6 +160,39 @@ def test_products_read_views_and_leave_what_is_beside_them(lib, dtype):
         _close(y, want, 33 * 25.0, 33)
 
 
+@pytest.mark.parametrize("layout", ["in_out", "out_in"])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_lines_of_every_short_length(lib, dtype, layout):
+    """A line's last chunk, whole, in part and shorter than a vector, NaN on both sides of it; values whose sums
+    are exact in every type (at most 4 x 23), so that results are equal."""
+    import paper_2608_06912_amd.autograd as A
+    torch = _torch()
+    dtype = getattr(torch, dtype)
+    gen = _gen(11)
+    offsets = torch.tensor([0, 6, 6, 23], dtype=torch.int32, device="cuda")
+
+    def cut(*shape):
+        big = torch.full((*shape[:-1], shape[-1] + 2), float("nan"), device="cuda", dtype=dtype)
+        view = big[..., 1:-1]
+        view.copy_(torch.randint(-2, 3, shape, generator=gen, device=gen.device))
+        return view
+
+    for n_in in range(1, 20):
+        for n_out in (1, 2, 3, 5, 7, 9, 12, 15, 17, 19):
+            x = cut(23, n_in).requires_grad_()
+            w = cut(3, n_in, n_out) if layout == "in_out" else cut(3, n_out, n_in).transpose(1, 2)
+            w.requires_grad_()
+            g = cut(23, n_out)
+            y = A.expert_matmul(x, w, offsets)
+            dx, dw = torch.autograd.grad(y, (x, w), g)
+            xd, wd, gd = (t.detach().double().cpu() for t in (x, w, g))
+            for e, (lo, hi) in enumerate(((0, 6), (6, 6), (6, 23))):
+                case = (n_in, n_out, e)
+                assert torch.equal(y[lo:hi].detach().double().cpu(), xd[lo:hi] @ wd[e]), case
+                assert torch.equal(dx[lo:hi].double().cpu(), gd[lo:hi] @ wd[e].T), case
+                assert torch.equal(dw[e].double().cpu(), xd[lo:hi].T @ gd[lo:hi]), case
+
+
 def test_rows_without_an_expert_may_hold_anything(lib):
     torch = _torch()
     x = torch.randn(6, 16, device="cuda")
