@@ -18,10 +18,10 @@
 // (unnormalised sums, m and l) cache_attend_join_kernel joins.
 //
 // A 16-bit cache is read at the memory's rate (four of 131072 keys 331 us, 5.7 TB/s).
-// 64 ragged ones of up to 8192 keys in int8 take 144 us (3.9 TB/s): 528 vector and
-// 290 scalar instructions a step, half of the former the codes' conversion.  The next
-// step's loads go out before a step is used (212 us without), and the table is looked
-// up a step before them.
+// 64 ragged ones of up to 8192 keys in int8 take 144 us (3.9 TB/s): 451 vector and
+// 173 scalar instructions a step, some 190 of the former the codes' conversion.  The
+// next step's loads go out before a step is used, and the table is looked up a step
+// before them (with a join by four waves 163 us, 214 without).
 //
 // Types.  Scores, m, l and sums are float32.  The weights go into the second
 // product as 16-bit terms of their own sum (two, which is 16 bits or more; three

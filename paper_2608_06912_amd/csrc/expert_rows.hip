@@ -9,8 +9,8 @@
 // them.
 //
 // Many rows are bound by the way into LDS and by the ends of tiles (131072 rows of 128
-// experts 2048 -> 1536 in float16 854 us, 966 TFLOP/s; without loads 1390), few rows by the
-// matrices' bytes (64 rows of 41 experts 2048 -> 1024 in bfloat16 29 us, 5.8 TB/s: a
+// experts 2048 -> 1536 in float16 835 us, 988 TFLOP/s; 128 x 128 tiles without loads 1390), few rows by the
+// matrices' bytes (64 rows of 41 experts 2048 -> 1024 in bfloat16 29 us, 5.9 TB/s: a
 // tile of 16 rows and 64 columns, so that 650 workgroups read them).
 #include "expert_tile.hpp"
 
