@@ -627,7 +627,10 @@ int lapsum_cache_step(const void* weights, int dtype, int64_t stride_batch,
  *   w          by three strides (expert, in, out), of which that of `in` or of
  *              `out` is 1: matrices stored either way round
  *   y          [rows, out] dense, of type y_dtype: that of x, or float32
- *   rows <= 2^30 (at most x_rows without an order), in and out <= 2^24
+ *   rows <= 2^30 (at most x_rows without an order), in and out <= 2^24;
+ *              (rows / 128 + experts) out / 128 < 2^24 (grad_w: experts in out
+ *              < 2^38), and up to 16 rows an expert (rows / 16 + experts) out / 64
+ *              < 2^25, all rounded up
  *
  * lapsum_expert_matmul_weights: its gradient with respect to w,
  * grad_w[e] = sum over e's rows of x[row(i)]^T grad_y[i], 0 for an expert
@@ -710,6 +713,7 @@ int lapsum_expert_combine_backward(const void* grad_out, const void* y,
  *   seen           [batch] int32;  count  [batch] int32, or NULL
  *   table          [batch, width] int32, or NULL.  No two positions that one
  *                  call writes may be one slot (a page of two sequences' ends)
+ *   k and v may be one cache only where k_new and v_new are one tensor
  *
  * lapsum_cache_read: out[b, h, p] = the entry of position p < lens[b], in float32 and
  * rounded once to dtype; 0 for the positions from lens[b] on and those not there.
@@ -728,7 +732,9 @@ int lapsum_expert_combine_backward(const void* grad_out, const void* y,
  *             a table), or NULL; with it lse is needed too
  *   scale     finite
  *   workspace lapsum_cache_attend_workspace_size bytes
- * batch, fresh and lengths may be 0; batch * heads <= 2^23; room <= 2^30.
+ * batch, fresh and lengths may be 0; batch * heads <= 2^23; room <= 2^30; append and
+ * read take batch * kv_heads * (fresh or room) < 2^31 rows, and below 2^27 (dim <= 128:
+ * 2^28) where a sequence's are less than 64.
  * ------------------------------------------------------------------------ */
 typedef struct lapsum_paged {
     void* data;

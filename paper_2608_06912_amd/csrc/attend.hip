@@ -621,16 +621,18 @@ __global__ __launch_bounds__(JT) void cache_attend_join_kernel(AttendArgs a, flo
 
 // Scores in powers of two to weights, by the row's lse; 0 outside its keys.
 __global__ __launch_bounds__(256) void cache_weights_kernel(AttendArgs a) {
-  const int64_t pieces = (a.room + 255) / 256;
-  const int64_t row = blockIdx.x / pieces, j = blockIdx.x % pieces * 256 + threadIdx.x;
-  if (j >= a.room) return;
-  const int b = static_cast<int>(row / a.heads);
-  const int64_t len = min(static_cast<int64_t>(max(a.lens[b], 0)), a.room);
-  const int64_t start = a.window > 0 && len > a.window ? len - a.window : 0;
-  const float lse = a.lse[row] * static_cast<float>(kLog2e);
-  float w = 0.0f;
-  if (j >= start && j < len && a.lse[row] != -INFINITY) w = exp2_fast(a.weights[row * a.room + j] - lse);
-  a.weights[row * a.room + j] = w;
+  const int64_t pieces = (a.room + 255) / 256, all = static_cast<int64_t>(a.batch) * a.heads * pieces;
+  for (int64_t at = blockIdx.x; at < all; at += gridDim.x) {
+    const int64_t row = at / pieces, j = at % pieces * 256 + threadIdx.x;
+    if (j >= a.room) continue;
+    const int b = static_cast<int>(row / a.heads);
+    const int64_t len = min(static_cast<int64_t>(max(a.lens[b], 0)), a.room);
+    const int64_t start = a.window > 0 && len > a.window ? len - a.window : 0;
+    const float lse = a.lse[row] * static_cast<float>(kLog2e);
+    float w = 0.0f;
+    if (j >= start && j < len && a.lse[row] != -INFINITY) w = exp2_fast(a.weights[row * a.room + j] - lse);
+    a.weights[row * a.room + j] = w;
+  }
 }
 
 }  // namespace
@@ -698,8 +700,9 @@ hipError_t launch_cache_attend(const AttendArgs& a, int dtype, int kind, bool ve
   }
   if (a.weights) {
     ProfScope ps_("cache_weights", s);
-    const int64_t pieces = (a.room + 255) / 256;
-    hipLaunchKernelGGL(cache_weights_kernel, dim3(static_cast<unsigned>(rows * pieces)), dim3(256), 0, s, a);
+    const int64_t all = rows * ((a.room + 255) / 256);
+    hipLaunchKernelGGL(cache_weights_kernel, dim3(static_cast<unsigned>(all < (1 << 20) ? all : (1 << 20))), dim3(256),
+                       0, s, a);
     e = hipGetLastError();
   }
   return e;

@@ -86,7 +86,10 @@ int lapsum_expert_matmul(const void* x, int dtype, int64_t x_rows, int64_t x_str
     return LAPSUM_ERR_INVALID_ARG;
   const Matrices m(w_strides, in, out);
   if (!m.ok || (rows > 0 && (!offsets || !w || !y || (x_rows > 0 && !x)))) return LAPSUM_ERR_INVALID_ARG;
-  if ((rows / 16 + experts + 1) > kMaxBlocks * 16 / ((out + 63) / 64)) return LAPSUM_ERR_INVALID_ARG;
+  // (a launch has less than 2^32 threads: tiles of 16 x 64 by 128, or of 128 x 128 by 256)
+  const bool few = rows <= experts * 16;
+  const int64_t lines = (few ? rows / 16 : rows / 128) + (experts < rows ? experts : rows) + 4;
+  if (lines * (few ? (out + 63) / 64 : (out + 127) / 128) >= (few ? 4 : 2) * kMaxBlocks) return LAPSUM_ERR_INVALID_ARG;
   const int dst = check_device();
   if (dst != LAPSUM_OK) return dst;
   if (rows == 0) return LAPSUM_OK;
@@ -135,7 +138,7 @@ int lapsum_expert_matmul_weights(const void* x, int dtype, int64_t x_rows, int64
   if (!m.ok || !offsets || !grad_w || (rows > 0 && (!grad_y || (x_rows > 0 && !x))) ||
       (experts > 1 && w_strides[0] < (m.out_dense ? (in - 1) * m.row + out : (out - 1) * m.row + in)))
     return LAPSUM_ERR_INVALID_ARG;
-  if (experts > kMaxBlocks * 16 / ((in + 63) / 64) / ((out + 63) / 64)) return LAPSUM_ERR_INVALID_ARG;
+  if ((experts * ((in + 127) / 128) + 3) * ((out + 127) / 128) >= 2 * kMaxBlocks) return LAPSUM_ERR_INVALID_ARG;
   const int wst = check_ws(workspace, workspace_bytes,
                            lapsum_expert_matmul_weights_workspace_size(experts, rows, in, out));
   if (wst != LAPSUM_OK) return wst;

@@ -599,6 +599,7 @@ struct AppendArgs {
   int batch, kv, fresh, dim;
   int chunks;                // set by the launcher
 };
+int64_t paged_blocks(int64_t heads, int64_t rows, int64_t dim);   // of 256 threads, of the two below
 hipError_t launch_cache_append(AppendArgs a, int dtype, int kind, bool vec, hipStream_t s);
 struct ReadArgs {
   PagedCache cache;

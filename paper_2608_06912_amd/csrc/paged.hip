@@ -288,6 +288,14 @@ bool in_chunks(int64_t heads, int64_t rows, int per, int* chunks, int64_t* block
   return rows >= 4 * per && *blocks >= 1024 && *blocks <= 2147483647LL;
 }
 
+// The workgroups of a launch over so many rows.
+int64_t paged_blocks(int64_t heads, int64_t rows, int64_t dim) {
+  const int per = PT / (dim <= 16 * PN ? 16 : 32);
+  int chunks;
+  int64_t blocks;
+  return in_chunks(heads, rows, per, &chunks, &blocks) ? blocks : (heads * rows + per - 1) / per;
+}
+
 hipError_t launch_cache_append(AppendArgs a, int dtype, int kind, bool vec, hipStream_t s) {
   const int team = a.dim <= 16 * PN ? 16 : 32, per = PT / team;
   const int64_t heads = static_cast<int64_t>(a.batch) * a.kv;

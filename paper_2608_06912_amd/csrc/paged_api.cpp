@@ -1,6 +1,9 @@
 // Host side of the paged cache: argument checks, workspaces and launch order of
 // writing, reading back and attending.
 #include <math.h>
+#include <string.h>
+
+#include <algorithm>
 
 #include "host.hpp"
 #include "kernels.hpp"
@@ -22,9 +25,11 @@ bool valid_paged(const lapsum_paged* c, int kind, int64_t kv, int64_t dim) {
   return kind <= LAPSUM_F16 || (c->scale && c->scale_stride_page >= 0 && c->scale_stride_head >= 0);
 }
 // No two entries in one place (two that one call may write).
-bool apart(const lapsum_paged* c, int64_t kv, int64_t dim) {
+bool apart(const lapsum_paged* c, int kind, int64_t kv, int64_t dim) {
   return (c->slots == 1 || c->stride_slot >= dim) && (kv == 1 || c->stride_head != 0) &&
-         (c->pages == 1 || c->stride_page != 0);
+         (c->pages == 1 || c->stride_page != 0) &&
+         (kind <= LAPSUM_F16 || ((kv == 1 || c->scale_stride_head >= c->slots) &&
+                                 (c->pages == 1 || c->scale_stride_page != 0)));
 }
 bool whole(const lapsum_paged* c, int kind, int64_t dim) {
   const uint64_t size = static_cast<uint64_t>(bytes_of(kind));
@@ -58,14 +63,19 @@ int lapsum_cache_append(const void* k_new, const int64_t* k_strides, const void*
                         const int32_t* table, int64_t width, hipStream_t stream) {
   if (!valid_dtype(dtype) || !valid_kind(kind, dtype) || batch < 0 || fresh < 0 || !k_strides || !v_strides ||
       !valid_paged(k, kind, kv_heads, dim) || !valid_paged(v, kind, kv_heads, dim) || k->pages != v->pages ||
-      k->slots != v->slots || !apart(k, kv_heads, dim) || !apart(v, kv_heads, dim) ||
+      k->slots != v->slots || !apart(k, kind, kv_heads, dim) || !apart(v, kind, kv_heads, dim) ||
       room_of(k, table, width, batch) < 0)
     return LAPSUM_ERR_INVALID_ARG;
   for (int i = 0; i < 3; ++i)
     if (k_strides[i] < 0 || v_strides[i] < 0) return LAPSUM_ERR_INVALID_ARG;
   const bool work = batch > 0 && fresh > 0;
   if (work && (!k_new || !v_new || !seen || !k->data || !v->data)) return LAPSUM_ERR_INVALID_ARG;
-  if (work && (kv_heads > 2147483647LL / batch || batch * kv_heads > 2147483647LL / fresh))
+  // one cache for both takes what is one for both
+  if (work && (k->data == v->data || (kind > LAPSUM_F16 && k->scale == v->scale)) &&
+      (k_new != v_new || !std::equal(k_strides, k_strides + 3, v_strides) || memcmp(k, v, sizeof *k) != 0))
+    return LAPSUM_ERR_INVALID_ARG;
+  if (work && (kv_heads > 2147483647LL / batch || batch * kv_heads > 2147483647LL / fresh ||
+               paged_blocks(batch * kv_heads, fresh, dim) >= 2 * kMaxBlocks))
     return LAPSUM_ERR_INVALID_ARG;
   const int dst = check_device();
   if (dst != LAPSUM_OK) return dst;
@@ -103,7 +113,8 @@ int lapsum_cache_read(const lapsum_paged* cache, int kind, int64_t batch, int64_
     return LAPSUM_ERR_INVALID_ARG;
   const bool work = batch > 0 && room > 0;
   if (work && (!cache->data || !lens || !out)) return LAPSUM_ERR_INVALID_ARG;
-  if (work && (kv_heads > 2147483647LL / batch || batch * kv_heads > 2147483647LL / room))
+  if (work && (kv_heads > 2147483647LL / batch || batch * kv_heads > 2147483647LL / room ||
+               paged_blocks(batch * kv_heads, room, dim) >= 2 * kMaxBlocks))
     return LAPSUM_ERR_INVALID_ARG;
   const int dst = check_device();
   if (dst != LAPSUM_OK) return dst;
@@ -149,8 +160,6 @@ int lapsum_cache_attend(const void* q, int64_t q_stride_batch, int64_t q_stride_
   const int64_t room = room_of(k, table, width, batch);
   if (room < 0 || (weights && !lse)) return LAPSUM_ERR_INVALID_ARG;
   if (batch > 0 && (heads > kMaxBlocks / batch || !q || !lens || !out || (room > 0 && (!k->data || !v->data))))
-    return LAPSUM_ERR_INVALID_ARG;
-  if (batch > 0 && weights && batch * heads > 2147483647LL / ((room + 255) / 256 + 1))
     return LAPSUM_ERR_INVALID_ARG;
   const int wst = check_ws(workspace, workspace_bytes,
                            lapsum_cache_attend_workspace_size(batch, heads, kv_heads, dim, room, window));

@@ -67,6 +67,20 @@ def test_matmul_weights_refuses(kw):
     assert E._load().lapsum_expert_matmul_weights(*a.values(), None) == INVALID
 
 
+@pytest.mark.parametrize("kw", [
+    dict(rows=1 << 29, x_rows=1 << 29, n_out=1 << 10), dict(experts=512, rows=512, x_rows=512, n_out=1 << 24)])
+def test_matmul_refuses_launches_of_too_many_threads(kw):
+    a = {**PRODUCT, **kw, "w": P}
+    strides = _strides(a["n_in"] * a["n_out"], a["n_out"], 1)
+    assert E._load().lapsum_expert_matmul(*a.values(), strides, P, 1, None) == INVALID
+
+
+def test_matmul_weights_refuses_launches_of_too_many_threads():
+    a = {**PRODUCT, "experts": 2048, "x_stride": 1 << 14, "n_in": 1 << 14, "n_out": 1 << 13}
+    strides = _strides(1 << 27, 1 << 13, 1)
+    assert E._load().lapsum_expert_matmul_weights(*a.values(), P, 1 << 13, P, strides, 0, 0, None) == INVALID
+
+
 def test_matmul_weights_workspace():
     lib = E._load()
     assert L.lapsum_expert_matmul_weights_workspace_size(64, 10000, 2048, 1024) == 0
@@ -109,12 +123,13 @@ BAD_CACHE = [dict(pages=0), dict(slots=0), dict(slots=(1 << 30) + 1), dict(page=
 
 def _append(cache={}, **kw):
     a = dict(kn=P, ks=_strides(128, 64, 64), vn=P, vs=_strides(128, 64, 64), dtype=1, batch=2, kv=2, fresh=1, dim=64,
-             seen=P, count=0, k=_cache(**cache), v=_cache(**cache), kind=3, table=P, width=3)
+             seen=P, count=0, k=_cache(**cache), v=_cache(**{"data": P + 4096, "scale": P + 8192, **cache}), kind=3,
+             table=P, width=3)
     a.update(kw)
     return G._load().lapsum_cache_append(*a.values(), None)
 
 
-@pytest.mark.parametrize("cache", BAD_CACHE + [dict(slot=63), dict(head=0), dict(page=0)])
+@pytest.mark.parametrize("cache", BAD_CACHE + [dict(slot=63), dict(head=0), dict(page=0), dict(sh=15), dict(sp=0)])
 def test_append_refuses_caches(cache):
     assert _append(cache) == INVALID
 
@@ -123,7 +138,9 @@ def test_append_refuses_caches(cache):
     dict(kn=0), dict(vn=0), dict(ks=None), dict(vs=_strides(-1, 64, 64)), dict(dtype=3), dict(batch=-1), dict(kv=0),
     dict(fresh=-1), dict(dim=0), dict(dim=257), dict(seen=0), dict(kind=2), dict(kind=5), dict(kind=-1),
     dict(v=_cache(pages=5)), dict(v=_cache(slots=8)), dict(width=-1), dict(width=(1 << 30) // 16 + 1),
-    dict(table=0, batch=7), dict(batch=1 << 20, fresh=1 << 20)])
+    dict(table=0, batch=7), dict(batch=1 << 20, fresh=1 << 20), dict(batch=1 << 27, fresh=1),
+    dict(v=_cache(scale=P + 8192)), dict(v=_cache(data=P + 4096)), dict(v=_cache(), vn=P + 64),
+    dict(v=_cache(), vs=_strides(128, 0, 64)), dict(v=_cache(slot=128)), dict(v=_cache(scale=None), kind=1, vn=P + 64)])
 def test_append_refuses(kw):
     assert _append(**kw) == INVALID
 
@@ -135,7 +152,8 @@ def test_read_refuses_caches(cache):
 
 @pytest.mark.parametrize("kw", [
     dict(kind=5), dict(kind=0), dict(batch=-1), dict(kv=0), dict(room=-1), dict(dim=0), dict(dim=257), dict(lens=0),
-    dict(table=0, batch=7), dict(width=-1), dict(out=0), dict(dtype=3), dict(batch=1 << 20, room=1 << 20)])
+    dict(table=0, batch=7), dict(width=-1), dict(out=0), dict(dtype=3), dict(batch=1 << 20, room=1 << 20),
+    dict(batch=1 << 25, room=4)])
 def test_read_refuses(kw):
     a = dict(cache=_cache(), kind=3, batch=2, kv=2, room=48, dim=64, lens=P, table=P, width=3, out=P, dtype=1)
     a.update(kw)
