@@ -9,7 +9,7 @@
 // them.
 //
 // Many rows are bound by the way into LDS and by the ends of tiles (131072 rows of 128
-// experts 2048 -> 1536 in float16 835 us, 988 TFLOP/s; 128 x 128 tiles without loads 1390), few rows by the
+// experts 2048 -> 1536 in float16 835 to 849 us, 972 to 988 TFLOP/s; 128 x 128 tiles without loads 1390), few rows by the
 // matrices' bytes (64 rows of 41 experts 2048 -> 1024 in bfloat16 29 us, 5.9 TB/s: a
 // tile of 16 rows and 64 columns, so that 650 workgroups read them).
 #include "expert_tile.hpp"
@@ -221,8 +221,17 @@ hipError_t launch_expert_rows(RowsArgs a, int dtype, bool w_n_dense, bool out_f3
     else if (direct && !few) launch(dt, dout, dense, yes, Shape<64, 64, 32, 32, 2, 2>{});
     else if (direct) launch(dt, dout, dense, yes, Shape<16, 64, 16, 32, 2, 2>{});
     else if (few) launch(dt, dout, dense, no, Shape<16, 64, 16, 32, 2, 1>{});
-    else if (tiles >= 512) launch(dt, dout, dense, no, Shape<128, 128, 64, 64, 2, 1>{});
-    else launch(dt, dout, dense, no, Shape<64, 64, 32, 32, 2, 1>{});
+    else {
+      // (float32, 128 x 128 and 64 x 64, us: 100320 rows 75 -> 691 221 and 206, 16384 rows
+      // 2047 -> 1023 794 and 757, 32768 rows 511 -> 2049 695 and 701)
+      if constexpr (DT != 0) {
+        if (tiles >= 512) {
+          launch(dt, dout, dense, no, Shape<128, 128, 64, 64, 2, 1>{});
+          return;
+        }
+      }
+      launch(dt, dout, dense, no, Shape<64, 64, 32, 32, 2, 1>{});
+    }
   };
   const auto types = [&](auto dt, auto dout) {
     if (w_n_dense) shapes(dt, dout, std::true_type{});

@@ -123,8 +123,9 @@ def lapsum_cache_append(k_new, v_new, seen, k, v, *, table=None, count=None, k_s
     [pages, kv_heads, slots, dim] of the entries' type, int8 or float8_e4m3fn,
     those with float32 scales [pages, kv_heads, slots]; table int32 [batch, pages of
     a sequence], None where page b is sequence b's.  Positions without a page are
-    not written.  The caller advances seen.  Autograd takes k, v and the scales as
-    changed; in grad mode none of them may require grad."""
+    not written.  The caller advances seen.  k may be v, for a cache that is both, where
+    k_new is v_new.  Autograd takes k, v and the scales as changed; in grad mode none of
+    them may require grad."""
     node = _node()
     if node:
         try:
