@@ -9,9 +9,11 @@
 // them.
 //
 // Many rows are bound by the way into LDS and by the ends of tiles (131072 rows of 128
-// experts 2048 -> 1536 in float16 835 to 849 us, 972 to 988 TFLOP/s; 128 x 128 tiles without loads 1390), few rows by the
-// matrices' bytes (64 rows of 41 experts 2048 -> 1024 in bfloat16 29 us, 5.9 TB/s: a
-// tile of 16 rows and 64 columns, so that 650 workgroups read them).
+// experts 2048 -> 1536 in float16 835 to 849 us, 972 to 988 TFLOP/s; 128 x 128 tiles without
+// loads 1390), few rows by the matrices' bytes (64 rows of 41 experts 2048 -> 1024 in
+// bfloat16 29 us, 5.9 TB/s: a tile of 16 rows and 64 columns, so that 650 workgroups
+// read them).  Rows of y of odd lengths do not keep operands from the direct way (70 rows of
+// 16 experts 1512 -> 2187 and back in float16 69 us, through registers 79).
 #include "expert_tile.hpp"
 
 namespace lapsum {
@@ -161,11 +163,11 @@ __global__ __launch_bounds__(S::T, S::M >= 128 ? 2 : 4) void expert_rows_kernel(
     const int r = t.row + wm + 16 * i + (lane & 15);
     const bool in = r < t.end;   // (all lanes take part in an exchange)
     out* y = static_cast<out*>(a.y) + static_cast<int64_t>(r) * a.n;
-    if constexpr (lines) {
+    if (lines && a.y_lines) {
 #pragma unroll
       for (int j = 0; j < S::TN / 16; j += 4) {
         const int n = n0 + wn + 16 * j;
-        store_line<DO>(y + n, &acc[i][j], in ? a.n - n : 0);
+        if constexpr (lines) store_line<DO>(y + n, &acc[i][j], in ? a.n - n : 0);
       }
     } else if (in) {
 #pragma unroll

@@ -109,8 +109,10 @@ int lapsum_expert_matmul(const void* x, int dtype, int64_t x_rows, int64_t x_str
   a.experts = static_cast<int>(experts);
   a.by = divider(top_k);
   const int64_t size = size_of(dtype);
-  const bool vec = whole_vectors(dtype, bits_of(x) | bits_of(w) | bits_of(y) |
-                                 static_cast<uint64_t>((x_stride | w_strides[0] | m.row) * size), in | out);
+  a.y_lines = vector_width(bits_of(y)) == 16 && out % 8 == 0;
+  const bool vec = whole_vectors(dtype, bits_of(x) | bits_of(w) |
+                                 static_cast<uint64_t>((x_stride | w_strides[0] | m.row) * size),
+                                 m.out_dense ? in | out : in);
   LAPSUM_TRY(launch_expert_rows(a, dtype, m.out_dense, y_dtype == LAPSUM_F32, vec, stream));
   return LAPSUM_OK;
 }

@@ -560,6 +560,7 @@ struct RowsArgs {
   Divider by;                // of places by top_k
   int rows, k, n, experts;
   int tiles_n;               // set by the launcher
+  bool y_lines;              // rows of y are whole, aligned vectors
 };
 hipError_t launch_expert_rows(RowsArgs a, int dtype, bool w_n_dense, bool out_f32, bool vec, hipStream_t s);
 struct GradArgs {

@@ -193,6 +193,24 @@ def test_lines_of_every_short_length(lib, dtype, layout):
                 assert torch.equal(dw[e].double().cpu(), xd[lo:hi].T @ gd[lo:hi]), case
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,experts,n_in,n_out", [
+    (40, 8, 64, 77), (500, 3, 40, 131), (8192, 4, 64, 1021), (8192, 1, 64, 4041), (8192, 1, 64, 4044)])
+def test_whole_vectors_in_and_odd_rows_out(lib, rows, experts, n_in, n_out, dtype):
+    """Matrices stored [out, in]: what is read is in whole vectors, what is written not.  Sums of at most 64
+    products of at most 4 are exact in every type, so that results are equal."""
+    torch = _torch()
+    dtype = getattr(torch, dtype)
+    gen = _gen(12)
+    draw = lambda *s: torch.randint(-2, 3, s, generator=gen, device=gen.device).cuda().to(dtype)  # noqa: E731
+    x, w = draw(rows, n_in), draw(experts, n_out, n_in).transpose(1, 2)
+    ends = torch.linspace(0, rows - 5, experts + 1).int().cuda()
+    y = lib.lapsum_expert_matmul(x, w, ends)
+    for e, lo, hi in _by_expert(rows, ends):
+        assert torch.equal(y[lo:hi].double(), x[lo:hi].double() @ w[e].double()), e
+    assert not bool(y[rows - 5:].any())
+
+
 def test_rows_without_an_expert_may_hold_anything(lib):
     torch = _torch()
     x = torch.randn(6, 16, device="cuda")
