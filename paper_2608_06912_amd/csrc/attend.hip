@@ -268,8 +268,10 @@ __global__ __launch_bounds__(AT, ND == 8 || (QT == 0 && ND > 2) ? 1 : 2) void ca
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       if constexpr (UNIFORM) {
-        if (u == 1 && last >= 31) {   // the second sixteen follow the first
-          st.page[1] = st.page[0];
+        // The second sixteen follow the first on its page, if that is there (one that is not is
+        // read from slot 0, wherever in it the first sixteen would be).
+        if (u == 1 && st.page[0] && last >= 31) {
+          st.page[1] = true;
           pk += 16 * slot_k;
           pv += 16 * slot_v;
           sk += 16;
