@@ -649,7 +649,8 @@ void attend_plan(int64_t batch, int64_t heads, int64_t kv, int64_t room, int64_t
   const int64_t rows = batch * kv * ((heads / kv + 15) / 16);
   const int64_t keys = window > 0 && window < room ? (window + AK < room ? window + AK : room) : room;
   int64_t each = (keys * rows + 1023) / 1024;
-  each = (each + step - 1) / step * step;
+  // (no more than there are: the product is past 32 bits where rows and room are large)
+  each = ((each < keys ? each : keys) + step - 1) / step * step;
   if (each < step) each = step;
   *chunk = static_cast<int>(each);
   *splits = static_cast<int>(keys < 1 ? 1 : (keys + each - 1) / each);
