@@ -224,7 +224,8 @@ __global__ __launch_bounds__(AT, ND == 8 || (QT == 0 && ND > 2) ? 1 : 2) void ca
   }
 
   // A lane's dims within a row, in bytes; dims that may not exist are the last ones
-  // again (their part of q is 0, and their results are not stored).  UNIFORM: with the
+  // again (of keys in 16 and 32 bits they count as 0, like their part of q: a product of 0 and
+  // infinity is none; codes of 8 bits have no infinities; results of them are not stored).  UNIFORM: with the
   // lane's row of the sixteen, or the first of its four.
   constexpr int kSure = ND == 2 ? 0 : ND == 8 ? 128 : 32 * (ND - 1);   // the smallest dim of this ND, less 1
   const int slot_k = static_cast<int>(a.k.slot) * B, slot_v = static_cast<int>(a.v.slot) * B;
@@ -375,6 +376,7 @@ __global__ __launch_bounds__(AT, ND == 8 || (QT == 0 && ND > 2) ? 1 : 2) void ca
           st.k[u][s].halves(hv);
           f = Move16{hv[0], hv[1], hv[2], hv[3]};
         }
+        if (VEC && KIND <= 2 && 4 * KN * (s + 1) > kSure && s * 4 * KN + KN * g >= a.dim) f = Move16{0u, 0u, 0u, 0u};
 #pragma unroll
         for (int t = 0; t < TQ; ++t) sc[u] = mma<MT>(f, q[s][t], sc[u]);
       }
