@@ -725,6 +725,8 @@ int lapsum_expert_combine_backward(const void* grad_out, const void* y,
  *   s_p = scale <q, k_p>,  out = sum e^(s_p - m) v_p / l,  m = max s,
  *   l = sum e^(s_p - m),  lse = m + log l,  weights_p = e^(s_p - lse).
  * A row without positions (or with every score -inf) gets out 0, lse -inf, weights 0.
+ * Infinite values give what float32 gives: infinity of their sign, NaN with one of the other,
+ * and NaN where e^(s_p - m) is 0 (s_p some 87 below m, or -inf).
  *   q         [batch, heads] rows of dim elements by two strides, of type dtype
  *   out       [batch, heads, dim] dense, of type dtype
  *   lse       [batch, heads] float32, or NULL

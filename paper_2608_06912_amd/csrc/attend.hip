@@ -26,7 +26,8 @@
 // Types.  Scores, m, l and sums are float32.  The weights go into the second
 // product as 16-bit terms of their own sum (two, which is 16 bits or more; three
 // for float32 queries), which costs matrix instructions that are free here and leaves the
-// outputs' own rounding as the only one.  Codes of 8 bits are whole numbers that
+// outputs' own rounding as the only one.  (Infinity times such terms is NaN where one of them is 0
+// or below, so sums that infinite values spoil are formed anew, see infinite_values.)  Codes of 8 bits are whole numbers that
 // bfloat16 holds exactly; their scales multiply scores and weights in float32, and
 // queries of another type are split into bfloat16 terms too.  A float32 cache uses
 // the float32 instructions.
@@ -149,6 +150,54 @@ struct Step {
   // the keys' pages exist: of a tile (UNIFORM), or of a lane's own four
   bool page[2], there[2][4];
 };
+
+// Sums of a wave that values which are not numbers take part in: what these alone make of
+// them, infinity of their sign or NaN, by the whole weights.  Goes through the wave's keys one by one
+// and looks at the weights of those whose values are such; lanes share the dims.  parts: the
+// wave's sums, and each head's largest score in powers of two behind them.
+template <int QT, int KIND, int ND>
+__device__ __forceinline__ void infinite_values(const AttendArgs& a, float (*parts)[ND * 32 + 2], float up, float scale2,
+                                                int b, int h, int head0, int live, int64_t first, int from, int to) {
+  static_assert(QT == KIND, "8-bit codes are numbers");
+  using raw = typename Elem<KIND>::raw;
+  constexpr int NT = (ND * 32 + kWave - 1) / kWave;
+  const int lane = lane_id();
+  const float turn = a.scale < 0.0f ? -1.0f : a.scale > 0.0f ? 1.0f : 0.0f;
+  uint32_t before = 0;   // bit t: such a value of the lane's t-th dim has been met
+  for (int64_t k0 = first; k0 < to; k0 += AK * AW) {
+    const int last = static_cast<int>(min(k0 + AK, static_cast<int64_t>(to)));
+    for (int key = max(static_cast<int>(k0), from); key < last; ++key) {
+      int page, slot;
+      find_slot(a.t, b, key, &page, &slot);
+      if (page < 0) continue;
+      const raw* pk = static_cast<const raw*>(a.k.data) + (page * a.k.page + h * a.k.head + slot * a.k.slot);
+      const raw* pv = static_cast<const raw*>(a.v.data) + (page * a.v.page + h * a.v.head + slot * a.v.slot);
+      float v[NT];
+      uint32_t odd = 0;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const int d = lane + kWave * t;
+        v[t] = d < a.dim ? Elem<KIND>::get(pv[d]) : 0.0f;
+        odd |= fabsf(v[t]) < INFINITY ? 0u : 1u << t;
+      }
+      if (!__any(odd != 0u)) continue;
+      for (int r = 0; r < live; ++r) {
+        const raw* q = static_cast<const raw*>(a.q) + b * a.q_b + (head0 + r) * a.q_h;
+        float s = 0.0f;
+        for (int d = lane; d < a.dim; d += kWave) s = fmaf(Elem<KIND>::get(q[d]) * turn, Elem<KIND>::get(pk[d]), s);
+        const float top = parts[r][ND * 32];
+        const float p = exp2_fast(fmaf(wave_sum(s), scale2, up - (top == -INFINITY ? 0.0f : top)));
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+          if (odd >> t & 1u) {
+            float* sum = &parts[r][lane + kWave * t];
+            *sum = (before >> t & 1u ? *sum : 0.0f) + p * v[t];
+          }
+      }
+      before |= odd;
+    }
+  }
+}
 
 // dim at most 32 ND.  UNIFORM: sixteen keys that begin at a multiple of 16 are in one page, and
 // 15 slots are less than 2^31 bytes.
@@ -536,6 +585,19 @@ __global__ __launch_bounds__(AT, ND == 8 || (QT == 0 && ND > 2) ? 1 : 2) void ca
         for (int i = 0; i < 4; ++i) parts[wave][4 * g + i][d] = out[c][e][i];
       }
     }
+  if constexpr (KIND == 1 || KIND == 2) {
+    float none = 0.0f;   // NaN where a sum is not a number
+#pragma unroll
+    for (int c = 0; c < VC; ++c)
+#pragma unroll
+      for (int e = 0; e < VN; ++e)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) none = 4 * g + i < live ? fmaf(out[c][e][i], 0.0f, none) : none;
+    if (__any(none != 0.0f)) {
+      wave_lds_sync();
+      infinite_values<QT, KIND, ND>(a, parts[wave], kUp, scale2, b, h, head0, live, base + AK * wave, from, to);
+    }
+  }
   __syncthreads();
   using raw = typename Elem<QT>::raw;
   for (int r = wave; r < live; r += AW) {

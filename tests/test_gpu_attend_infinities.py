@@ -46,3 +46,58 @@ def test_keys_of_score_minus_infinity(lib, dim, dtype):
     k[1, :, :, -1] = -math.inf
     y, total = lib.lapsum_cache_attend(q, k, v, lens, lse=True)
     assert not y[1].any() and bool((total[1] == -math.inf).all()) and bool(torch.isfinite(total[0]).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim,n,paged", [(64, 1, False), (64, 50, False), (128, 700, True), (80, 5000, True),
+                                         (33, 300, False), (256, 90, True), (8, 40, False), (200, 2100, False)])
+def test_infinite_values(lib, dim, n, paged, dtype):
+    """A value of weight above 0 gives infinity of its sign, two of both signs NaN, and the other
+    dims are what they are without."""
+    import torch
+    gen = _gen(dim + n)
+    q = torch.randn(2, 4, dim, generator=gen, device="cuda").to(getattr(torch, dtype))
+    k, v = (torch.randn(2, 2, n, dim, generator=gen, device="cuda").to(q.dtype) for _ in "kv")
+    lens = torch.tensor([n, (n + 1) // 2], dtype=torch.int32, device="cuda")
+    keep = torch.arange(n, device="cuda") < lens[:, None]
+    best = _attend(q.double(), k.double(), v.double(), dim ** -0.5, keep)[2].argmax(-1)
+    for b in range(2):
+        last = int(lens[b]) - 1
+        v[b, 0, int(best[b, 0]), 1] = math.inf          # (the largest weight of a head, a power of two)
+        v[b, 0, last, dim - 1] = -math.inf
+        v[b, 0, last // 3, 3] = math.inf
+        v[b, 1, 0, 0], v[b, 1, last, 0] = math.inf, -math.inf
+        v[b, 1, last // 2, 5] = math.nan
+        v[b, 1, int(lens[b]):] = math.inf               # (past the length)
+    want, lse, _, size, sums = _attend(q.double(), k.double(), torch.where(keep[:, None, :, None], v, 0.0).double(),
+                                       dim ** -0.5, keep)
+    kw = {}
+    if paged:
+        slots = 32
+        width = -(-n // slots)
+        pad = [torch.nn.functional.pad(x, (0, 0, 0, width * slots - n)) for x in (k, v)]
+        k, v = (x.view(2, 2, width, slots, dim).transpose(1, 2).reshape(2 * width, 2, slots, dim) for x in pad)
+        kw["table"] = torch.arange(2 * width, dtype=torch.int32, device="cuda").view(2, width)
+    y, total = lib.lapsum_cache_attend(q, k, v, lens, lse=True, **kw)
+    assert bool(torch.isfinite(total).all())
+    assert int((want == math.inf).sum()) >= 4 and bool(torch.isnan(want[:, 2:, 5]).all())
+    _close(y, want, lse, size, sums, dim, n, q.dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("apart", [5.0, 12.0, 25.0, 60.0])
+def test_infinite_values_of_little_weight(lib, apart, dtype):
+    """Weights down to e^-60 are numbers above 0 in float32."""
+    import torch
+    n, dim = 200, 64
+    q = torch.zeros(1, 1, dim, device="cuda", dtype=getattr(torch, dtype))
+    k, v = (torch.zeros(1, 1, n, dim, device="cuda", dtype=q.dtype) for _ in "kv")
+    q[..., 0] = 8.0
+    k[0, 0, 137, 0] = apart
+    v[0, 0, :, 4] = 2.0
+    v[0, 0, 20, 9], v[0, 0, 180, 10] = math.inf, -math.inf
+    lens = torch.tensor([n], dtype=torch.int32, device="cuda")
+    y = lib.lapsum_cache_attend(q, k, v, lens)[0, 0].float()
+    assert y[9] == math.inf and y[10] == -math.inf and abs(float(y[4]) - 2.0) <= 2.0 ** -7
+    y[9] = y[10] = y[4] = 0.0
+    assert not y.any()
