@@ -152,51 +152,88 @@ struct Step {
 };
 
 // Sums of a wave that values which are not numbers take part in: what these alone make of
-// them, infinity of their sign or NaN, by the whole weights.  Goes through the wave's keys one by one
-// and looks at the weights of those whose values are such; lanes share the dims.  parts: the
-// wave's sums, and each head's largest score in powers of two behind them.
+// them, infinity of their sign or NaN, by the whole weights.  Goes through the wave's keys, eight
+// at once, and looks at the weights of those with infinite values; lanes share the dims.  parts:
+// the wave's sums, and each head's largest score in powers of two and total behind them.
+//
+// Four bfloat16 caches of 131072 keys with an infinity in every 64th value take 1370 us; without
+// any, and with NaN in as many or in all of them, or in keys, 335 to 345.
 template <int QT, int KIND, int ND>
 __device__ __forceinline__ void infinite_values(const AttendArgs& a, float (*parts)[ND * 32 + 2], float up, float scale2,
                                                 int b, int h, int head0, int live, int64_t first, int from, int to) {
   static_assert(QT == KIND, "8-bit codes are numbers");
   using raw = typename Elem<KIND>::raw;
-  constexpr int NT = (ND * 32 + kWave - 1) / kWave;
+  constexpr int NT = (ND * 32 + kWave - 1) / kWave, Ahead = 8;
   const int lane = lane_id();
+  // (a total that is NaN has left nothing but NaN)
+  uint32_t heads = 0;
+  for (int r = 0; r < live; ++r) heads |= parts[r][ND * 32 + 1] >= 0.0f ? 1u << r : 0u;
+  heads = __builtin_amdgcn_readfirstlane(heads);
+  if (!heads) return;
   const float turn = a.scale < 0.0f ? -1.0f : a.scale > 0.0f ? 1.0f : 0.0f;
-  uint32_t before = 0;   // bit t: such a value of the lane's t-th dim has been met
-  for (int64_t k0 = first; k0 < to; k0 += AK * AW) {
-    const int last = static_cast<int>(min(k0 + AK, static_cast<int64_t>(to)));
-    for (int key = max(static_cast<int>(k0), from); key < last; ++key) {
-      int page, slot;
-      find_slot(a.t, b, key, &page, &slot);
-      if (page < 0) continue;
-      const raw* pk = static_cast<const raw*>(a.k.data) + (page * a.k.page + h * a.k.head + slot * a.k.slot);
-      const raw* pv = static_cast<const raw*>(a.v.data) + (page * a.v.page + h * a.v.head + slot * a.v.slot);
-      float v[NT];
-      uint32_t odd = 0;
+  const auto is_nan = [](float x) { return x != x; };
+  // bit t: such a value of the lane's t-th dim has been met; one that is NaN, or there is none
+  uint32_t before = 0, done = (1u << NT) - 1u;
+  for (int r = 0; r < live; ++r)
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        const int d = lane + kWave * t;
-        v[t] = d < a.dim ? Elem<KIND>::get(pv[d]) : 0.0f;
-        odd |= fabsf(v[t]) < INFINITY ? 0u : 1u << t;
-      }
-      if (!__any(odd != 0u)) continue;
-      for (int r = 0; r < live; ++r) {
-        const raw* q = static_cast<const raw*>(a.q) + b * a.q_b + (head0 + r) * a.q_h;
-        float s = 0.0f;
-        for (int d = lane; d < a.dim; d += kWave) s = fmaf(Elem<KIND>::get(q[d]) * turn, Elem<KIND>::get(pk[d]), s);
-        const float top = parts[r][ND * 32];
-        const float p = exp2_fast(fmaf(wave_sum(s), scale2, up - (top == -INFINITY ? 0.0f : top)));
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-          if (odd >> t & 1u) {
-            float* sum = &parts[r][lane + kWave * t];
-            *sum = (before >> t & 1u ? *sum : 0.0f) + p * v[t];
-          }
-      }
-      before |= odd;
+    for (int t = 0; t < NT; ++t) {
+      const int d = lane + kWave * t;
+      if ((heads >> r & 1u) && d < a.dim && !(fabsf(parts[r][d]) < INFINITY)) done &= ~(1u << t);
     }
-  }
+  const auto load = [&](int key, const raw** k, float (&v)[NT]) {
+    int page = -1, slot = 0;
+    if (key >= from && key < to) find_slot(a.t, b, key, &page, &slot);
+    const bool there = page >= 0;
+    if (!there) page = slot = 0;
+    *k = static_cast<const raw*>(a.k.data) + (page * a.k.page + h * a.k.head + slot * a.k.slot);
+    const raw* p = static_cast<const raw*>(a.v.data) + (page * a.v.page + h * a.v.head + slot * a.v.slot);
+    uint32_t odd = 0;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int d = lane + kWave * t;
+      v[t] = Elem<KIND>::get(p[d < a.dim ? d : 0]);
+      odd |= there && !(fabsf(v[t]) < INFINITY) ? 1u << t : 0u;
+    }
+    return odd & ~done;
+  };
+  for (int64_t k0 = first; k0 < to; k0 += AK * AW)
+    for (int j0 = 0; j0 < AK; j0 += Ahead) {
+      const raw* k;
+      float v[NT];
+      uint32_t some = 0;
+#pragma unroll
+      for (int j = 0; j < Ahead; ++j) some |= load(static_cast<int>(min(k0 + j0 + j, int64_t(to))), &k, v);
+      if (!__any(some != 0u)) continue;
+      for (int j = 0; j < Ahead; ++j) {
+        const uint32_t odd = load(static_cast<int>(min(k0 + j0 + j, int64_t(to))), &k, v);
+        if (!__any(odd != 0u)) continue;
+        bool weigh = false;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) weigh = weigh || ((odd >> t & 1u) && !is_nan(v[t]));
+        weigh = __any(weigh);
+        for (int r = 0; r < live; ++r) {
+          if (!(heads >> r & 1u)) continue;
+          float p = 1.0f;
+          if (weigh) {
+            const raw* q = static_cast<const raw*>(a.q) + b * a.q_b + (head0 + r) * a.q_h;
+            float s = 0.0f;
+            for (int d = lane; d < a.dim; d += kWave) s = fmaf(Elem<KIND>::get(q[d]) * turn, Elem<KIND>::get(k[d]), s);
+            const float top = parts[r][ND * 32];
+            p = exp2_fast(fmaf(wave_sum(s), scale2, up - (top == -INFINITY ? 0.0f : top)));
+          }
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+            if (odd >> t & 1u) {
+              float* sum = &parts[r][lane + kWave * t];
+              *sum = (before >> t & 1u ? *sum : 0.0f) + p * v[t];
+            }
+        }
+        before |= odd;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) done |= (odd >> t & 1u) && is_nan(v[t]) ? 1u << t : 0u;
+        if (__all(done == (1u << NT) - 1u)) return;
+      }
+    }
 }
 
 // dim at most 32 ND.  UNIFORM: sixteen keys that begin at a multiple of 16 are in one page, and

@@ -101,3 +101,27 @@ def test_infinite_values_of_little_weight(lib, apart, dtype):
     assert y[9] == math.inf and y[10] == -math.inf and abs(float(y[4]) - 2.0) <= 2.0 ** -7
     y[9] = y[10] = y[4] = 0.0
     assert not y.any()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("heads", [2, 16, 20])
+def test_infinities_beside_numbers_that_are_none(lib, heads, dtype):
+    """One head's query is NaN, one dim's values are NaN, two are infinite now and then, and all of
+    the longest sequence: each shows where it belongs."""
+    import torch
+    n, dim = 900, 96
+    gen = _gen(heads)
+    q = torch.randn(3, heads, dim, generator=gen, device="cuda").to(getattr(torch, dtype))
+    k, v = (torch.randn(3, 1, n, dim, generator=gen, device="cuda").to(q.dtype) for _ in "kv")
+    q[:, 1, 7] = math.nan
+    v[0, 0, ::50, 2] = math.nan
+    v[0, 0, 7::70, 64], v[0, 0, 8::90, 95] = math.inf, -math.inf
+    v[0, 0, 33, 10], v[0, 0, 877, 10] = math.inf, -math.inf
+    v[1] = math.inf
+    lens = torch.tensor([n, n - 1, n - 2], dtype=torch.int32, device="cuda")
+    keep = torch.arange(n, device="cuda") < lens[:, None]
+    want, lse, _, size, sums = _attend(q.double(), k.double(), v.double(), dim ** -0.5, keep)
+    y, total = lib.lapsum_cache_attend(q, k, v, lens, lse=True)
+    assert bool(torch.isnan(y[:, 1]).all()) and bool(torch.isnan(total[:, 1]).all())
+    rest = [r for r in range(heads) if r != 1]
+    _close(y[:, rest], want[:, rest], lse[:, rest], size[:, rest], sums[:, rest], dim, n, q.dtype)
