@@ -128,6 +128,23 @@ __device__ __forceinline__ void split8(const float (&x)[8], Move16 (&f)[T]) {
     }
   }
 }
+// Any floats as T fragments of bfloat16: eight bits of each after the others, towards zero, so that
+// no term and no sum of some is larger than the whole; infinity and zeros (three are a float's 24 bits,
+// two more than float16's 11).
+template <int T>
+__device__ __forceinline__ void split8_any(const float (&x)[8], Move16 (&f)[T]) {
+  float rest[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) rest[j] = x[j];
+#pragma unroll
+  for (int t = 0; t < T; ++t) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[t][j] = high_halves(__float_as_uint(rest[2 * j]), __float_as_uint(rest[2 * j + 1]));
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      rest[j] = fabsf(rest[j]) == INFINITY ? 0.0f : rest[j] - __uint_as_float(__float_as_uint(rest[j]) & 0xffff0000u);
+  }
+}
 
 // The larger of a value and those of the lanes 16, 32 and 48 away; their sum.
 template <class Op>
@@ -305,7 +322,8 @@ __global__ __launch_bounds__(AT, ND == 8 || (QT == 0 && ND > 2) ? 1 : 2) void ca
 #pragma unroll
       for (int j = 0; j < 4; ++j) q[s][0][j] = __float_as_uint(x[j]);
     } else {
-      split8<MT, TQ>(x, q[s]);
+      if constexpr (TQ > 1) split8_any<TQ>(x, q[s]);
+      else split8<MT, TQ>(x, q[s]);
     }
   }
 

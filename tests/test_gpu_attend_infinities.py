@@ -125,3 +125,28 @@ def test_infinities_beside_numbers_that_are_none(lib, heads, dtype):
     assert bool(torch.isnan(y[:, 1]).all()) and bool(torch.isnan(total[:, 1]).all())
     rest = [r for r in range(heads) if r != 1]
     _close(y[:, rest], want[:, rest], lse[:, rest], size[:, rest], sums[:, rest], dim, n, q.dtype)
+
+
+@pytest.mark.parametrize("kind", ["int8", "float8_e4m3fn"])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_infinite_queries_of_a_cache_in_8_bits(lib, dtype, kind):
+    """Scores of -inf all of them give 0 and -inf; the largest finite queries stay finite."""
+    import torch
+    n, dim = 70, 64
+    gen = _gen(1)
+    q = torch.randn(1, 3, dim, generator=gen, device="cuda").to(getattr(torch, dtype))
+    code = torch.randint(1, 100, (1, 1, n, dim), generator=gen, device="cuda").float()
+    scale = torch.full((1, 1, n), 2.0 ** -9, device="cuda")
+    q[0, 0, 5] = -math.inf
+    q[0, 1], code[..., 7] = 0.0, 1.0       # (its one product, before the scales, is a number)
+    q[0, 1, 7] = torch.finfo(q.dtype).max
+    code = code.to(getattr(torch, kind))
+    lens = torch.tensor([n], dtype=torch.int32, device="cuda")
+    y, total, w = lib.lapsum_cache_attend(q, code, code, lens, k_scale=scale, v_scale=scale, scale=2.0 ** -12, lse=True,
+                                          weights=True)
+    assert not y[0, 0].any() and not w[0, 0].any() and float(total[0, 0]) == -math.inf
+    assert bool(torch.isfinite(y[0, 1:]).all()) and bool(torch.isfinite(total[0, 1:]).all())
+    x = code.double() * scale.double()[..., None]
+    keep = torch.ones(1, n, dtype=torch.bool, device="cuda")
+    want, lse, _, size, sums = _attend(q[:, 2:].double(), x, x, 2.0 ** -12, keep)
+    _close(y[:, 2:], want, lse, size, sums, dim, n, q.dtype)
