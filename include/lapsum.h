@@ -627,10 +627,14 @@ int lapsum_cache_step(const void* weights, int dtype, int64_t stride_batch,
  *   w          by three strides (expert, in, out), of which that of `in` or of
  *              `out` is 1: matrices stored either way round
  *   y          [rows, out] dense, of type y_dtype: that of x, or float32
- *   rows <= 2^30 (at most x_rows without an order), in and out <= 2^24;
- *              (rows / 128 + experts) out / 128 < 2^24 (grad_w: experts in out
- *              < 2^38), and up to 16 rows an expert (rows / 16 + experts) out / 64
- *              < 2^25, all rounded up
+ *   rows <= 2^30 (at most x_rows without an order), in and out <= 2^24, and
+ *              launches of less than 2^32 threads.  Tiles of 128 x 128 results have 256
+ *              threads: (rows / 128 + experts) out / 128 < 2^24, for grad_w
+ *              experts (in / 128) (out / 128) < 2^24.  Up to 16 rows an expert tiles of
+ *              16 x 64 have 128: (rows / 16 + experts) out / 64 < 2^25.  Float32 in lines that
+ *              are not whole, aligned vectors of 16 bytes has tiles of 64 x 64:
+ *              (rows / 64 + experts) out / 64 < 2^24.  Quotients are rounded up, and lines
+ *              of tiles to fours
  *
  * lapsum_expert_matmul_weights: its gradient with respect to w,
  * grad_w[e] = sum over e's rows of x[row(i)]^T grad_y[i], 0 for an expert

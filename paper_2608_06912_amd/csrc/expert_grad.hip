@@ -196,52 +196,64 @@ int grad_splits(int64_t experts, int64_t rows, int64_t m, int64_t n) {
   return static_cast<int>(want < most ? (want < 1 ? 1 : want) : (most < 1 ? 1 : most));
 }
 
-hipError_t launch_expert_grad(GradArgs a, int dtype, bool vec, hipStream_t s) {
-  const int64_t size = dtype == 0 ? 4 : 2;
+// The way and the shape of tiles of a gradient: f(way, shape).
+template <int DT, class F>
+static auto with_shape(const GradArgs& a, bool vec, F&& f) {
+  const int64_t size = DT == 0 ? 4 : 2;
   const auto spans = [&](int64_t rows, int64_t stride, bool gather) {
     return (gather ? rows : a.rows + int64_t(1)) * stride * size < kMostBytes;
   };
   const bool direct = vec && spans(a.a_rows, a.a_stride, a.gather == 1) && spans(a.b_rows, a.b_stride, a.gather == 2);
-  const auto launch = [&](auto dt, auto way, auto shape) {
-    using S = decltype(shape);
-    const int64_t lines = static_cast<int64_t>(a.experts) * a.splits * ((a.m + S::M - 1) / S::M);
-    hipLaunchKernelGGL((expert_grad_kernel<decltype(dt)::value, decltype(way)::value, S>),
-                       dim3(static_cast<unsigned>((lines + 3) / 4 * 4 * ((a.n + S::N - 1) / S::N))), dim3(S::T), 0, s, a);
+  const int64_t tiles = static_cast<int64_t>(a.experts) * ((a.m + 127) / 128) * ((a.n + 127) / 128);
+  const std::integral_constant<int, -1> no;
+  const auto big = [&](auto yes) {
+    // the training layer's 8 matrices of 2048 x 4096 (and 128 of 2048 x 1536 from 131072
+    // rows), us: 256 x 256 338 (1072), 128 x 256 266 (956), 128 x 128 301 (1168)
+    if constexpr (DT != 0) {
+      if (tiles >= 1024 && a.splits == 1) return f(yes, Shape<128, 256, 128, 64, 1, 3>{});
+    }
+    if (tiles >= 512 && a.splits == 1) return f(yes, Shape<128, 128, 64, 64, 2, 2>{});
+    return f(yes, Shape<64, 64, 32, 32, 2, 2>{});
   };
-  const auto shapes = [&](auto dt) {
-    const int64_t tiles = static_cast<int64_t>(a.experts) * ((a.m + 127) / 128) * ((a.n + 127) / 128);
-    const std::integral_constant<int, -1> no;
-    const auto big = [&](auto yes) {
-      // the training layer's 8 matrices of 2048 x 4096 (and 128 of 2048 x 1536 from 131072
-      // rows), us: 256 x 256 338 (1072), 128 x 256 266 (956), 128 x 128 301 (1168)
-      if constexpr (decltype(dt)::value != 0) {
-        if (tiles >= 1024 && a.splits == 1) {
-          launch(dt, yes, Shape<128, 256, 128, 64, 1, 3>{});
-          return;
-        }
-      }
-      if (tiles >= 512 && a.splits == 1) launch(dt, yes, Shape<128, 128, 64, 64, 2, 2>{});
-      else launch(dt, yes, Shape<64, 64, 32, 32, 2, 2>{});
-    };
+  if (direct && a.gather == 0) return big(std::integral_constant<int, 0>{});
+  if (direct && a.gather == 1) return big(std::integral_constant<int, 1>{});
+  if (direct) return big(std::integral_constant<int, 2>{});
+  if (tiles >= 512 && a.splits == 1) return f(no, Shape<128, 128, 64, 64, 2, 1>{});
+  return f(no, Shape<64, 64, 32, 32, 2, 1>{});
+}
+template <class S>
+static int64_t blocks_of(const GradArgs& a) {
+  const int64_t lines = static_cast<int64_t>(a.experts) * a.splits * ((a.m + S::M - 1) / S::M);
+  return (lines + 3) / 4 * 4 * ((a.n + S::N - 1) / S::N);
+}
+
+int64_t expert_grad_threads(const GradArgs& a, int dtype, bool vec) {
+  const auto count = [&](auto, auto shape) { return blocks_of<decltype(shape)>(a) * decltype(shape)::T; };
+  return dtype == 0 ? with_shape<0>(a, vec, count) : with_shape<1>(a, vec, count);
+}
+
+hipError_t launch_expert_grad(GradArgs a, int dtype, bool vec, hipStream_t s) {
+  const auto types = [&](auto dt) {
+    constexpr int DT = decltype(dt)::value;
     {
       ProfScope ps_("expert_grad", s);
-      if (direct && a.gather == 0) big(std::integral_constant<int, 0>{});
-      else if (direct && a.gather == 1) big(std::integral_constant<int, 1>{});
-      else if (direct) big(std::integral_constant<int, 2>{});
-      else if (tiles >= 512 && a.splits == 1) launch(dt, no, Shape<128, 128, 64, 64, 2, 1>{});
-      else launch(dt, no, Shape<64, 64, 32, 32, 2, 1>{});
+      with_shape<DT>(a, vec, [&](auto way, auto shape) {
+        using S = decltype(shape);
+        hipLaunchKernelGGL((expert_grad_kernel<DT, decltype(way)::value, S>), dim3(static_cast<unsigned>(blocks_of<S>(a))),
+                           dim3(S::T), 0, s, a);
+      });
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
     ProfScope ps_("expert_grad_join", s);
     const int64_t blocks = (static_cast<int64_t>(a.experts) * a.m * a.n + 255) / 256;
-    hipLaunchKernelGGL((expert_grad_join_kernel<decltype(dt)::value>),
-                       dim3(static_cast<unsigned>(blocks < (1 << 16) ? blocks : (1 << 16))), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((expert_grad_join_kernel<DT>), dim3(static_cast<unsigned>(blocks < (1 << 16) ? blocks : (1 << 16))),
+                       dim3(256), 0, s, a);
     return hipGetLastError();
   };
-  if (dtype == 0) return shapes(std::integral_constant<int, 0>{});
-  if (dtype == 1) return shapes(std::integral_constant<int, 1>{});
-  return shapes(std::integral_constant<int, 2>{});
+  if (dtype == 0) return types(std::integral_constant<int, 0>{});
+  if (dtype == 1) return types(std::integral_constant<int, 1>{});
+  return types(std::integral_constant<int, 2>{});
 }
 
 }  // namespace lapsum

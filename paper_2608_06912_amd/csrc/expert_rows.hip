@@ -182,62 +182,73 @@ __global__ __launch_bounds__(S::T, S::M >= 128 ? 2 : 4) void expert_rows_kernel(
 }  // namespace
 
 // ------------------------------------------------------------- launchers ---
-hipError_t launch_expert_rows(RowsArgs a, int dtype, bool w_n_dense, bool out_f32, bool vec, hipStream_t s) {
-  const int64_t size = dtype == 0 ? 4 : 2;
+// The way and the shape of tiles of a product: f(way, shape).  What is launched and what is
+// checked before come from here both.
+template <int DT, bool N_DENSE, class F>
+static auto with_shape(const RowsArgs& a, bool vec, F&& f) {
+  const int64_t size = DT == 0 ? 4 : 2;
   const bool direct = vec && (a.order ? a.x_rows * a.x_stride : 256 * a.x_stride + a.k) * size < kMostBytes &&
-                      ((w_n_dense ? a.k : a.n) + 1) * a.w_row * size < kMostBytes;
+                      ((N_DENSE ? a.k : a.n) + 1) * a.w_row * size < kMostBytes;
+  const int64_t tiles = (a.rows / 128 + (a.experts < a.rows ? a.experts : a.rows)) * ((a.n + 127) / 128);
+  const std::true_type yes;
+  const std::false_type no;
+  // (most of a taller tile would be rows of none)
+  const bool few = a.rows <= static_cast<int64_t>(a.experts) * 16;
+  // Few large tiles leave compute units idle, small ones read more than the die's
+  // cache delivers.  Rows of 128 bytes are two steps of 64 and want both at
+  // once; where w is dense along n one step's rows of it are long.  16384 rows of
+  // 8 experts 2048 -> 4096 in bfloat16 (and 131072 of 128, 2048 -> 1536), us:
+  //   w dense along n   256 x 256 307 (854), 128 x 256 284 (856), 128 x 128 301 (1001)
+  //   w dense along k   256 x 256 284 (847), 128 x 256 316 (942), 128 x 128 290 (990)
+  const int64_t each = a.rows / a.experts;
+  if constexpr (DT != 0) {
+    if (direct && (N_DENSE ? tiles >= 1024 && each >= 128 : tiles >= 2048 && each >= 256)) {
+      if constexpr (N_DENSE) return f(yes, Shape<128, 256, 128, 64, 1, 3>{});
+      else return f(yes, Shape<256, 256, 128, 64, 2, 2>{});
+    }
+  }
+  if (direct && tiles >= 512 && !few) return f(yes, Shape<128, 128, 64, 64, 2, 2>{});
+  if (direct && !few) return f(yes, Shape<64, 64, 32, 32, 2, 2>{});
+  if (direct) return f(yes, Shape<16, 64, 16, 32, 2, 2>{});
+  if (few) return f(no, Shape<16, 64, 16, 32, 2, 1>{});
+  // (float32, 128 x 128 and 64 x 64, us: 100320 rows 75 -> 691 221 and 206, 16384 rows
+  // 2047 -> 1023 794 and 757, 32768 rows 511 -> 2049 695 and 701)
+  if constexpr (DT != 0) {
+    if (tiles >= 512) return f(no, Shape<128, 128, 64, 64, 2, 1>{});
+  }
+  return f(no, Shape<64, 64, 32, 32, 2, 1>{});
+}
+template <class S>
+static int64_t blocks_of(const RowsArgs& a) {
+  // an expert's last tile is not full, and neither is that of the rows of none
+  const int64_t most = (a.rows / S::M + (a.experts + 1 < a.rows ? a.experts + 1 : a.rows) + 3) / 4 * 4;
+  return most * ((a.n + S::N - 1) / S::N);
+}
+
+int64_t expert_rows_threads(const RowsArgs& a, int dtype, bool w_n_dense, bool vec) {
+  const auto count = [&](auto, auto shape) { return blocks_of<decltype(shape)>(a) * decltype(shape)::T; };
+  const auto of = [&](auto dt) {
+    return w_n_dense ? with_shape<decltype(dt)::value, true>(a, vec, count)
+                     : with_shape<decltype(dt)::value, false>(a, vec, count);
+  };
+  return dtype == 0 ? of(std::integral_constant<int, 0>{}) : of(std::integral_constant<int, 1>{});
+}
+
+hipError_t launch_expert_rows(RowsArgs a, int dtype, bool w_n_dense, bool out_f32, bool vec, hipStream_t s) {
   ProfScope ps_("expert_rows", s);
-  const auto launch = [&](auto dt, auto dout, auto dense, auto way, auto shape) {
-    using S = decltype(shape);
-    a.tiles_n = (a.n + S::N - 1) / S::N;
-    // an expert's last tile is not full, and neither is that of the rows of none
-    const int64_t most = (a.rows / S::M + (a.experts + 1 < a.rows ? a.experts + 1 : a.rows) + 3) / 4 * 4;
-    hipLaunchKernelGGL((expert_rows_kernel<decltype(dt)::value, decltype(dout)::value, decltype(dense)::value,
-                                           decltype(way)::value, S>),
-                       dim3(static_cast<unsigned>(most * a.tiles_n)), dim3(S::T), 0, s, a);
-  };
-  const auto shapes = [&](auto dt, auto dout, auto dense) {
-    constexpr int DT = decltype(dt)::value;
-    const int64_t tiles = (a.rows / 128 + (a.experts < a.rows ? a.experts : a.rows)) * ((a.n + 127) / 128);
-    const std::true_type yes;
-    const std::false_type no;
-    // (most of a taller tile would be rows of none)
-    const bool few = a.rows <= static_cast<int64_t>(a.experts) * 16;
-    // Few large tiles leave compute units idle, small ones read more than the die's
-    // cache delivers.  Rows of 128 bytes are two steps of 64 and want both at
-    // once; where w is dense along n one step's rows of it are long.  16384 rows of
-    // 8 experts 2048 -> 4096 in bfloat16 (and 131072 of 128, 2048 -> 1536), us:
-    //   w dense along n   256 x 256 307 (854), 128 x 256 284 (856), 128 x 128 301 (1001)
-    //   w dense along k   256 x 256 284 (847), 128 x 256 316 (942), 128 x 128 290 (990)
-    const int64_t each = a.rows / a.experts;
-    const bool large = DT != 0 && direct && (dense ? tiles >= 1024 && each >= 128 : tiles >= 2048 && each >= 256);
-    if constexpr (DT != 0) {
-      if constexpr (dense) {
-        if (large) launch(dt, dout, dense, yes, Shape<128, 256, 128, 64, 1, 3>{});
-      } else {
-        if (large) launch(dt, dout, dense, yes, Shape<256, 256, 128, 64, 2, 2>{});
-      }
-    }
-    if (large) return;
-    if (direct && tiles >= 512 && !few) launch(dt, dout, dense, yes, Shape<128, 128, 64, 64, 2, 2>{});
-    else if (direct && !few) launch(dt, dout, dense, yes, Shape<64, 64, 32, 32, 2, 2>{});
-    else if (direct) launch(dt, dout, dense, yes, Shape<16, 64, 16, 32, 2, 2>{});
-    else if (few) launch(dt, dout, dense, no, Shape<16, 64, 16, 32, 2, 1>{});
-    else {
-      // (float32, 128 x 128 and 64 x 64, us: 100320 rows 75 -> 691 221 and 206, 16384 rows
-      // 2047 -> 1023 794 and 757, 32768 rows 511 -> 2049 695 and 701)
-      if constexpr (DT != 0) {
-        if (tiles >= 512) {
-          launch(dt, dout, dense, no, Shape<128, 128, 64, 64, 2, 1>{});
-          return;
-        }
-      }
-      launch(dt, dout, dense, no, Shape<64, 64, 32, 32, 2, 1>{});
-    }
-  };
   const auto types = [&](auto dt, auto dout) {
-    if (w_n_dense) shapes(dt, dout, std::true_type{});
-    else shapes(dt, dout, std::false_type{});
+    constexpr int DT = decltype(dt)::value, DO = decltype(dout)::value;
+    const auto go = [&](auto dense) {
+      constexpr bool N_DENSE = decltype(dense)::value;
+      with_shape<DT, N_DENSE>(a, vec, [&](auto way, auto shape) {
+        using S = decltype(shape);
+        a.tiles_n = (a.n + S::N - 1) / S::N;
+        hipLaunchKernelGGL((expert_rows_kernel<DT, DO, N_DENSE, decltype(way)::value, S>),
+                           dim3(static_cast<unsigned>(blocks_of<S>(a))), dim3(S::T), 0, s, a);
+      });
+    };
+    if (w_n_dense) go(std::true_type{});
+    else go(std::false_type{});
   };
   const std::integral_constant<int, 0> f32;
   const std::integral_constant<int, 1> b16;

@@ -86,13 +86,10 @@ int lapsum_expert_matmul(const void* x, int dtype, int64_t x_rows, int64_t x_str
     return LAPSUM_ERR_INVALID_ARG;
   const Matrices m(w_strides, in, out);
   if (!m.ok || (rows > 0 && (!offsets || !w || !y || (x_rows > 0 && !x)))) return LAPSUM_ERR_INVALID_ARG;
-  // (a launch has less than 2^32 threads: tiles of 16 x 64 by 128, or of 128 x 128 by 256)
+  // (the documented bound; what is launched is counted below)
   const bool few = rows <= experts * 16;
   const int64_t lines = (few ? rows / 16 : rows / 128) + (experts < rows ? experts : rows) + 4;
   if (lines * (few ? (out + 63) / 64 : (out + 127) / 128) >= (few ? 4 : 2) * kMaxBlocks) return LAPSUM_ERR_INVALID_ARG;
-  const int dst = check_device();
-  if (dst != LAPSUM_OK) return dst;
-  if (rows == 0) return LAPSUM_OK;
   RowsArgs a{};
   a.x = x;
   a.w = w;
@@ -113,6 +110,10 @@ int lapsum_expert_matmul(const void* x, int dtype, int64_t x_rows, int64_t x_str
   const bool vec = whole_vectors(dtype, bits_of(x) | bits_of(w) |
                                  static_cast<uint64_t>((x_stride | w_strides[0] | m.row) * size),
                                  m.out_dense ? in | out : in);
+  if (expert_rows_threads(a, dtype, m.out_dense, vec) >= kMaxThreads) return LAPSUM_ERR_INVALID_ARG;
+  const int dst = check_device();
+  if (dst != LAPSUM_OK) return dst;
+  if (rows == 0) return LAPSUM_OK;
   LAPSUM_TRY(launch_expert_rows(a, dtype, m.out_dense, y_dtype == LAPSUM_F32, vec, stream));
   return LAPSUM_OK;
 }
@@ -141,11 +142,6 @@ int lapsum_expert_matmul_weights(const void* x, int dtype, int64_t x_rows, int64
       (experts > 1 && w_strides[0] < (m.out_dense ? (in - 1) * m.row + out : (out - 1) * m.row + in)))
     return LAPSUM_ERR_INVALID_ARG;
   if ((experts * ((in + 127) / 128) + 3) * ((out + 127) / 128) >= 2 * kMaxBlocks) return LAPSUM_ERR_INVALID_ARG;
-  const int wst = check_ws(workspace, workspace_bytes,
-                           lapsum_expert_matmul_weights_workspace_size(experts, rows, in, out));
-  if (wst != LAPSUM_OK) return wst;
-  const int dst = check_device();
-  if (dst != LAPSUM_OK) return dst;
   GradArgs a{};
   const bool swap = !m.out_dense;   // the gradient's rows are those of w in memory
   a.a = swap ? grad_y : x;
@@ -171,6 +167,12 @@ int lapsum_expert_matmul_weights(const void* x, int dtype, int64_t x_rows, int64
   const bool vec = whole_vectors(dtype, bits_of(x) | bits_of(grad_y) | bits_of(grad_w) |
                                  static_cast<uint64_t>((x_stride | grad_stride | w_strides[0] | m.row) * size),
                                  in | out);
+  if (expert_grad_threads(a, dtype, vec) >= kMaxThreads) return LAPSUM_ERR_INVALID_ARG;
+  const int wst = check_ws(workspace, workspace_bytes,
+                           lapsum_expert_matmul_weights_workspace_size(experts, rows, in, out));
+  if (wst != LAPSUM_OK) return wst;
+  const int dst = check_device();
+  if (dst != LAPSUM_OK) return dst;
   LAPSUM_TRY(launch_expert_grad(a, dtype, vec, stream));
   return LAPSUM_OK;
 }

@@ -53,6 +53,7 @@ inline int check_ws(void* ws, size_t have, size_t need) {
 
 // -------------------------------------------------------- argument checks --
 constexpr int64_t kMaxBlocks = int64_t(1) << 23;   // workgroups of a launch
+constexpr int64_t kMaxThreads = int64_t(1) << 32;  // a launch has less
 
 inline bool valid_dtype(int dtype) { return dtype >= LAPSUM_F32 && dtype <= LAPSUM_F16; }
 

@@ -562,6 +562,8 @@ struct RowsArgs {
   int tiles_n;               // set by the launcher
   bool y_lines;              // rows of y are whole, aligned vectors
 };
+// The threads of that launch, which are less than 2^32.
+int64_t expert_rows_threads(const RowsArgs& a, int dtype, bool w_n_dense, bool vec);
 hipError_t launch_expert_rows(RowsArgs a, int dtype, bool w_n_dense, bool out_f32, bool vec, hipStream_t s);
 struct GradArgs {
   const void *a, *b;         // the side by expert's row order comes through order where gather says so
@@ -574,6 +576,7 @@ struct GradArgs {
   float* part;               // [splits][experts][m][n], where that is above one
 };
 int grad_splits(int64_t experts, int64_t rows, int64_t m, int64_t n);
+int64_t expert_grad_threads(const GradArgs& a, int dtype, bool vec);
 hipError_t launch_expert_grad(GradArgs a, int dtype, bool vec, hipStream_t s);
 
 // ---------------------------------------------------------- paged cache ----

@@ -37,3 +37,34 @@ def test_every_key_is_some_split_s(batch, heads, kv):
         rows = batch * kv * -(-(heads // kv) // 16)
         assert splits == 1 or splits * rows <= 1024 + rows
         assert (L.lapsum_cache_attend_workspace_size(batch, heads, kv, 64, room, window) > 0) == (splits > 1)
+
+
+# Launches of 2^32 threads or more are refused, by the tiles that would be launched: P is a pointer
+# that is never read, as the refusal comes before any HIP call.
+INVALID, P = 1, 256
+
+
+def _strides(*s):
+    return (ctypes.c_int64 * 3)(*s)
+
+
+@pytest.mark.parametrize("dtype,rows,experts,n_in,out,strides", [
+    # float32 off the direct way to LDS: tiles of 64 x 64
+    (0, 1 << 30, 1, 8, 1, (8, 1, 1)), (0, 1 << 29, 3, 8, 75, (600, 75, 1)),
+    (0, 40000, 2048, 3, 405000, (3 * 405000, 405000, 1)), (0, 1 << 28, 1, 7, 200, (1400, 1, 7)),
+    # tiles of 128 x 128 and 256 x 256
+    (1, 1 << 29, 3, 8, 1 << 10, (1 << 13, 1 << 10, 1)), (2, 1 << 30, 1, 7, 130 * 128, (7 * 130 * 128, 1, 7))])
+def test_products_of_too_many_threads(dtype, rows, experts, n_in, out, strides):
+    import paper_2608_06912_amd.experts as E
+    call = E._load().lapsum_expert_matmul
+    assert call(P, dtype, rows, n_in, 0, 1, P, experts, rows, n_in, out, P, _strides(*strides), P, dtype, None) == INVALID
+
+
+@pytest.mark.parametrize("dtype,experts,n_in,out,strides", [
+    # matrices stored the other way round: their lines in memory are tiled as rows, four lines of tiles at once
+    (1, 127, 1 << 24, 2, (1 << 25, 1, 1 << 24)), (0, 127, 1 << 24, 3, (3 << 24, 1, 1 << 24)),
+    (1, 2048, 1 << 14, 1 << 13, (1 << 27, 1 << 13, 1))])
+def test_gradients_of_too_many_threads(dtype, experts, n_in, out, strides):
+    import paper_2608_06912_amd.experts as E
+    call = E._load().lapsum_expert_matmul_weights
+    assert call(P, dtype, 10, n_in, 0, 1, P, experts, 10, n_in, out, P, out, P, _strides(*strides), 0, 0, None) == INVALID
