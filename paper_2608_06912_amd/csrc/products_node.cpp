@@ -292,6 +292,20 @@ bool cache_append(const Tensor& k_new, const Tensor& v_new, const Tensor& seen, 
   return true;
 }
 
+// What has no gradient, from inputs of which one requires it in grad mode: asking for it is an error.
+bool recorded(std::initializer_list<const Tensor*> inputs) {
+  if (!at::GradMode::is_enabled()) return false;
+  for (const Tensor* t : inputs)
+    if (t && t->requires_grad()) return true;
+  return false;
+}
+const Tensor* maybe(const OptTensor& t) { return t ? &*t : nullptr; }
+variable_list no_gradient(variable_list outputs, const char* what) {
+  for (Tensor& t : outputs) t = t.detach().requires_grad_();
+  const auto count = static_cast<int64_t>(outputs.size());
+  return (*std::make_shared<torch::autograd::DelayedError>(what, count))(std::move(outputs));
+}
+
 OptTensor cache_read(const Tensor& x, const Tensor& lens, int64_t room, const OptTensor& table,
                      const OptTensor& scale, const std::optional<at::ScalarType>& dtype) {
   const Paged c(x, scale, false);
@@ -307,6 +321,7 @@ OptTensor cache_read(const Tensor& x, const Tensor& lens, int64_t room, const Op
                           pages_of(table), table ? table->size(1) : 0,
                           out.data_ptr(), dtype_of(out), stream_of(x)),
         "lapsum_cache_read");
+  if (recorded({&x, maybe(scale)})) return no_gradient({out}, "lapsum_cache_read has no gradient")[0];
   return out;
 }
 
@@ -341,6 +356,8 @@ std::optional<std::vector<Tensor>> cache_attend(const Tensor& q, const Tensor& k
         "lapsum_cache_attend");
   if (lse) found.push_back(total);
   if (weights) found.push_back(w);
+  if (recorded({&q, &k, &v, maybe(k_scale), maybe(v_scale)}))
+    return no_gradient(std::move(found), "lapsum_cache_attend has no gradient");
   return found;
 }
 

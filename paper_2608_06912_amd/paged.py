@@ -12,6 +12,10 @@ check and marshal their arguments.
 Without a table the cache is [batch, kv_heads, slots, dim], as
 lapsum_cache_evict returns it; the attention's weights are then what
 lapsum_cache_step takes.
+
+None of this is differentiable.  Entries are written without their history, and what
+is read back or attended to from inputs that require grad, in grad mode, raises where its
+gradient is asked for.
 """
 from __future__ import annotations
 
@@ -116,6 +120,17 @@ def _pair(k, v, k_scale, v_scale, written=False):
     return ck, cv, kind
 
 
+def _no_gradient(outs, inputs, where):
+    """outs, such that asking for a gradient through them is an error, if autograd would
+    record a call with these inputs."""
+    torch = _torch()
+    if not torch.is_grad_enabled() or not any(t is not None and t.requires_grad for t in inputs):
+        return outs
+    error = torch._C._functions.DelayedError(f"{where} has no gradient".encode(), len(outs))
+    found = error(*[t.detach().requires_grad_() for t in outs])
+    return [found] if isinstance(found, torch.Tensor) else list(found)
+
+
 def lapsum_cache_append(k_new, v_new, seen, k, v, *, table=None, count=None, k_scale=None, v_scale=None):
     """Write new entries into a cache, in place: entry i of sequence b, k_new and v_new
     [batch, kv_heads, new, dim] (or [batch, kv_heads, dim], one each), at position
@@ -125,7 +140,7 @@ def lapsum_cache_append(k_new, v_new, seen, k, v, *, table=None, count=None, k_s
     a sequence], None where page b is sequence b's.  Positions without a page are
     not written.  The caller advances seen.  k may be v, for a cache that is both, where
     k_new is v_new.  Autograd takes k, v and the scales as changed; in grad mode none of
-    them may require grad."""
+    them may require grad.  No gradient goes back to k_new and v_new."""
     node = _node()
     if node:
         try:
@@ -173,7 +188,8 @@ def lapsum_cache_read(x, lens, room: int, *, table=None, scale=None, dtype=None)
     """A cache's entries by sequence: [batch, kv_heads, room, dim], positions from
     lens[b] (int32 [batch]) on and those without a page 0.  x, table and scale as in
     lapsum_cache_append; dtype: the cache's own, or for one in 8 bits float32,
-    bfloat16 or float16 (float32 if None)."""
+    bfloat16 or float16 (float32 if None).  Not differentiable: a gradient through it
+    is an error."""
     node = _node()
     if node:
         try:
@@ -200,7 +216,7 @@ def lapsum_cache_read(x, lens, room: int, *, table=None, scale=None, dtype=None)
         _check(lib.lapsum_cache_read(ctypes.byref(c), kind, batch, x.shape[1], room, x.shape[3],
                                      _ptr(lens), table, width, _ptr(out), _dtype(out, "dtype"),
                                      _stream(dev)), "lapsum_cache_read")
-    return out
+    return _no_gradient([out], (x, scale), "lapsum_cache_read")[0]
 
 
 def lapsum_cache_attend_workspace_size(batch: int, heads: int, kv_heads: int, dim: int, room: int,
@@ -217,7 +233,8 @@ def lapsum_cache_attend(q, k, v, lens, *, table=None, k_scale=None, v_scale=None
     only the last `window` entries.  lse=True adds the log-sum-exp of the
     scores, float32 [batch, heads]; weights=True the weights, float32
     [batch, heads, room] (room: the slots of the table's pages).  A sequence
-    without entries gets zeros, and lse -inf."""
+    without entries gets zeros, and lse -inf.  Not differentiable: a gradient through
+    it is an error."""
     node = _node()
     if node and workspace is None:
         try:
@@ -263,4 +280,5 @@ def lapsum_cache_attend(q, k, v, lens, *, table=None, k_scale=None, v_scale=None
                                        table, width, scale, window, _ptr(out), _ptr(total),
                                        _ptr(w), _ptr(ws), nbytes, _stream(dev)), "lapsum_cache_attend")
     found = [out] + ([total] if lse else []) + ([w] if weights else [])
+    found = _no_gradient(found, (q, k, v, k_scale, v_scale), "lapsum_cache_attend")
     return found[0] if len(found) == 1 else tuple(found)
