@@ -18,10 +18,10 @@
 // (unnormalised sums, m and l) cache_attend_join_kernel joins.
 //
 // A 16-bit cache is read at the memory's rate (four of 131072 keys 331 us, 5.7 TB/s).
-// 64 ragged ones of up to 8192 keys in int8 take 144 us (3.9 TB/s): 451 vector and
-// 173 scalar instructions a step, some 190 of the former the codes' conversion.  The
-// next step's loads go out before a step is used, and the table is looked up a step
-// before them (with a join by four waves 163 us, 214 without).
+// 64 ragged ones of up to 8192 keys in int8 take 145 us (3.8 TB/s; longest sequences first
+// 135): 451 vector and 176 scalar instructions a step, some 190 of the former the codes'
+// conversion.  The next step's loads go out before a step is used, and the table is looked up a
+// step before them (with a join by four waves 163 us, 214 without).
 //
 // Types.  Scores, m, l and sums are float32.  The weights go into the second
 // product as 16-bit terms of their own sum (two, which is 16 bits or more; three
@@ -29,7 +29,7 @@
 // outputs' own rounding as the only one.  (Infinity times such terms is NaN where one of them is 0
 // or below, so sums that infinite values spoil are formed anew, see infinite_values.)  Codes of 8 bits are whole numbers that
 // bfloat16 holds exactly; their scales multiply scores and weights in float32, and
-// queries of another type are split into bfloat16 terms too.  A float32 cache uses
+// queries of another type are cut into bfloat16 terms too.  A float32 cache uses
 // the float32 instructions.
 #include "matrix.hpp"
 #include "paged.hpp"

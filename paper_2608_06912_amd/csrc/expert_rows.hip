@@ -9,7 +9,7 @@
 // them.
 //
 // Many rows are bound by the way into LDS and by the ends of tiles (131072 rows of 128
-// experts 2048 -> 1536 in float16 835 to 849 us, 972 to 988 TFLOP/s; 128 x 128 tiles without
+// experts 2048 -> 1536 in float16 835 to 853 us, 967 to 988 TFLOP/s; 128 x 128 tiles without
 // loads 1390), few rows by the matrices' bytes (64 rows of 41 experts 2048 -> 1024 in
 // bfloat16 29 us, 5.9 TB/s: a tile of 16 rows and 64 columns, so that 650 workgroups
 // read them).  Rows of y of odd lengths do not keep operands from the direct way (70 rows of
